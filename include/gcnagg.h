@@ -66,7 +66,8 @@ enum {
                              i < min(n_rows, n_cols) */
 };
 
-/* input element types of the aggregation calls; accumulation and output are fp32 */
+/* element types of the aggregation calls' input (accumulation and output are fp32)
+ * and of the calls that take a dtype */
 enum { GCN_DT_F32 = 0, GCN_DT_BF16 = 1 };
 
 /* gcn_aggregate_fwd_q8halo flags */
@@ -345,6 +346,89 @@ gcn_status gcn_sage3_step(const gcn_graph* g, const float* X, int64_t ldx, int64
                           const int32_t* labels, const uint8_t* lp_mask, const float* E,
                           double eps, float* const* grads, float* dE, double* loss,
                           void* stream);
+
+/* ---- typed layers: products by group, LayerNorm with weights, dropout ---- */
+
+/* Products of rows sorted by group with one matrix per group: the node types of
+ * a heterogeneous graph, or the experts of a routed layer. Group g holds the rows
+ * [offsets[g], offsets[g + 1]) of the matrices with `rows` rows.
+ *   GCN_GEMM_NN  C[rows x N] : C_g = A_g B_g     A [rows x K], B_g [K x N]
+ *   GCN_GEMM_NT  C[rows x N] : C_g = A_g B_g^T   A [rows x K], B_g [N x K]
+ *   GCN_GEMM_TN  C_g [K x N] = A_g^T B_g         A [rows x K], B [rows x N]
+ * so that Y = X W_g, dX = dY W_g^T and dW_g = X_g^T dY_g take W as one layout.
+ *  offsets   int64 device array [n_groups + 1], not decreasing, in [0, rows]. It
+ *            is read when the kernels run, so a captured call follows it. Rows
+ *            before the first and behind the last offset belong to no group: NN
+ *            and NT leave those rows of C as they were, TN leaves them out.
+ *            Offsets outside [0, rows] are taken as 0 or rows and a group that
+ *            ends before it begins as an empty one; no error is reported.
+ *  A group without rows takes no part in NN and NT; in TN its C_g is zero.
+ *  dtype     GCN_DT_F32 or GCN_DT_BF16: the type of A and B. dtype_c: that of C,
+ *            GCN_DT_F32 or, for NN and NT, that of A and B (rounded once).
+ *            Products and sums as in gcn_gemm_f32 for fp32 operands; exact
+ *            products and fp32 sums for bf16 ones.
+ *  lda, ldb, ldc  row strides; stride_w: elements from one group's matrix to the
+ *            next one's, of B in NN and NT (>= 0; 0: one matrix for all), of C in
+ *            TN (at least (K - 1) ldc + N). C may not overlap A or B.
+ * 1 <= n_groups < 65536, 0 <= rows < 2^31, 1 <= K, N < 2^24. Results repeat bit for bit.
+ * TN takes temporaries (sums of parts of long groups). Asynchronous on `stream`. */
+gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* offsets, int64_t rows,
+                            int64_t N, int64_t K, const void* A, int64_t lda, const void* B,
+                            int64_t ldb, int dtype, void* C, int64_t ldc, int dtype_c,
+                            int64_t stride_w, void* stream);
+
+/* Which elements a dropout keeps: those whose 32-bit random word is at least
+ * floor(p 2^32). The word of element (i, f) is word f % 4 of the block that
+ * Philox4x32 (7 rounds; Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as
+ * easy as 1, 2, 3", 2011) makes of the counter (f / 4, row0 + i, call mod 2^32,
+ * call / 2^32) under the key (seed mod 2^32, seed / 2^32). So the mask is a function
+ * of these numbers alone: it is never stored, the backward pass forms it anew, it
+ * does not depend on strides, types or on how rows are spread over workers
+ * (row0: the first row's number in the whole matrix). */
+typedef struct {
+  double p;              /* share of elements dropped, 0 <= p < 1 */
+  uint64_t seed;         /* the generator's key */
+  uint64_t call;         /* which mask under this key: another one for every layer and step */
+  const uint64_t* step;  /* device, or NULL: a number added to `call` (modulo 2^64) when the
+                            kernel runs, so that replays of a captured call can differ */
+  int64_t row0;          /* >= 0, row0 + n <= 2^32 */
+} gcn_dropout_spec;
+
+/* Y[i, f] = X[i, f] / (1 - p) where the element is kept, else +0 (also of an
+ * infinity or NaN); computed in fp32 and rounded once to the type. The gradient is
+ * the same call on dY. X and Y [n x F] are of type dtype (GCN_DT_F32 or
+ * GCN_DT_BF16); Y may be X itself (same ld), and may not overlap it otherwise.
+ * `drop` is a host pointer, read before the call returns. Asynchronous. */
+gcn_status gcn_dropout(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
+                       const gcn_dropout_spec* drop, void* Y, int64_t ldy, void* stream);
+
+/* Row LayerNorm with weights, and optionally dropout behind it:
+ *   H = (X - mean) / sqrt(var + eps),  Y = dropout(H * gamma + beta)
+ * over the F features of each row, biased variance, sums of the statistics in
+ * double, the rest in fp32, rounded once to the type.
+ *  X, Y      [n x F] of type dtype (GCN_DT_F32 or GCN_DT_BF16); Y may be X itself
+ *            (same ld), and may not overlap it otherwise.
+ *  gamma, beta  fp32 [F], or NULL for 1 and 0.
+ *  drop      NULL: no dropout; else as for gcn_dropout.
+ * Asynchronous. Nothing is kept for the backward pass but X itself. */
+gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
+                                    const float* gamma, const float* beta, double eps,
+                                    const gcn_dropout_spec* drop, void* Y, int64_t ldy,
+                                    void* stream);
+
+/* Gradients of gcn_layernorm_affine_fwd, from the same X, gamma, eps and drop:
+ *   G = dropout(dY), dgamma = sum_i G * H, dbeta = sum_i G, T = G * gamma,
+ *   dX = (T - mean(T) - H * mean(T * H)) / sqrt(var + eps)
+ * (the mask is formed again, and the statistics are taken again of the rows, which
+ * the pass holds anyway). dX [n x F] of type dtype, may be dY or X itself (same
+ * ld), and may not overlap them otherwise; dgamma and dbeta fp32 [F]. Each may be
+ * NULL, not all three. With n = 0 dgamma and dbeta become zero. Rows are summed in
+ * an order that n, F and the type alone decide. Takes temporaries for dgamma and
+ * dbeta. Asynchronous. */
+gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
+                                    const float* gamma, double eps, const gcn_dropout_spec* drop,
+                                    const void* dY, int64_t lddy, void* dX, int64_t lddx,
+                                    float* dgamma, float* dbeta, void* stream);
 
 /* ---- hybrid pre/post-aggregation (Algorithm 1, Sections 5.2 and 5.3) ---- */
 

@@ -1,0 +1,179 @@
+// Products of rows sorted by group with one matrix per group (gcn_gemm_grouped).
+//
+// The groups' sizes are known on the device only. So a launch covers every tile
+// that any offsets could need, and a workgroup finds its own: with R rows per
+// tile, the tiles of group g take the slots from offsets[g] / R + g on. Its rows
+// need at most offsets[g + 1] / R - offsets[g] / R + 1 tiles, so the next group
+// begins behind them, all groups end before rows / R + n_groups, and the group of
+// a slot is found by comparing, without sums over the groups before it.
+
+#include <algorithm>
+
+#include "element.h"
+
+namespace gcn {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct GroupArgs {
+  int groups;
+  const int64_t* offsets;
+  int64_t rows;
+  int N, K;  // columns of C; of A
+  const void* A;
+  int64_t lda;
+  const void* B;
+  int64_t ldb;
+  void* C;
+  int64_t ldc;
+  int64_t stride_w;
+};
+
+// An offset, inside [0, rows] whatever the array holds.
+__device__ inline int64_t offset_at(const GroupArgs& a, int g) {
+  const int64_t o = a.offsets[g];
+  return o < 0 ? 0 : (o > a.rows ? a.rows : o);
+}
+
+// The last group whose slots begin at or before `slot` (0 if none does): every
+// lane of the wavefront compares one group of the range left.
+__device__ inline int group_of(const GroupArgs& a, int64_t slot, int R) {
+  int lo = 0, len = a.groups;
+  while (len > 1) {
+    const int step = (len + 63) / 64;
+    const int g = lo + (int)(threadIdx.x & 63) * step;
+    const bool at = g < lo + len && offset_at(a, g) / R + g <= slot;
+    const uint64_t hit = __ballot(at);
+    const int last = hit ? 63 - __clzll((long long)hit) : 0;
+    lo += last * step;
+    len = min(step, a.groups - lo);
+  }
+  return lo;
+}
+
+// The general kernel: one 64 x 64 tile of C per workgroup, fp32 products, any
+// type, size and alignment.
+constexpr int kTile = 64, kDepth = 16;
+
+template <class T, class TC, int OP>
+__global__ __launch_bounds__(kThreads) void k_grouped(GroupArgs a) {
+  __shared__ float as[kDepth][kTile + 4], bs[kDepth][kTile + 4];
+  const T* A = static_cast<const T*>(a.A);
+  const T* B = static_cast<const T*>(a.B);
+  TC* C = static_cast<TC*>(a.C);
+  const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
+  const int n0 = blockIdx.y * kTile;
+  int64_t i0 = 0;  // first row of C
+  int64_t m_end, k0 = 0, k1 = a.K;
+  if constexpr (OP == GCN_GEMM_TN) {
+    const int g = blockIdx.x;
+    k0 = offset_at(a, g);
+    k1 = offset_at(a, g + 1);
+    i0 = (int64_t)blockIdx.z * kTile;
+    m_end = a.K;
+    C += g * a.stride_w;
+  } else {
+    const int64_t slot = blockIdx.x;
+    const int g = group_of(a, slot, kTile);
+    const int64_t beg = offset_at(a, g);
+    m_end = offset_at(a, g + 1);
+    const int64_t tile = slot - (beg / kTile + g);
+    i0 = beg + tile * kTile;
+    if (tile < 0 || i0 >= m_end) return;
+    B += g * a.stride_w;
+  }
+  float acc[4][4] = {};
+  for (int64_t kk = k0; kk < k1; kk += kDepth) {
+    for (int e = t; e < kDepth * kTile; e += kThreads) {
+      // neighbouring threads read neighbouring elements of a row
+      const int kf = e % kDepth, rf = e / kDepth, kt = e / kTile, rt = e % kTile;
+      if constexpr (OP == GCN_GEMM_TN) {
+        const bool in = kk + kt < k1;
+        as[kt][rt] = in && i0 + rt < m_end ? to_float(A[(kk + kt) * a.lda + i0 + rt]) : 0.f;
+        bs[kt][rt] = in && n0 + rt < a.N ? to_float(B[(kk + kt) * a.ldb + n0 + rt]) : 0.f;
+      } else {
+        as[kf][rf] = kk + kf < k1 && i0 + rf < m_end ? to_float(A[(i0 + rf) * a.lda + kk + kf]) : 0.f;
+        if constexpr (OP == GCN_GEMM_NN)
+          bs[kt][rt] = kk + kt < k1 && n0 + rt < a.N ? to_float(B[(kk + kt) * a.ldb + n0 + rt]) : 0.f;
+        else
+          bs[kf][rf] = kk + kf < k1 && n0 + rf < a.N ? to_float(B[(n0 + rf) * a.ldb + kk + kf]) : 0.f;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = __builtin_fmaf(as[k][4 * ty + i], bs[k][4 * tx + j], acc[i][j]);
+    __syncthreads();
+  }
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = i0 + 4 * ty + i;
+      const int c = n0 + 4 * tx + j;
+      if (r < m_end && c < a.N) C[r * a.ldc + c] = from_float<TC>(acc[i][j]);
+    }
+}
+
+template <class T, class TC>
+gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
+  const unsigned cols = (unsigned)ceil_div((int64_t)a.N, (int64_t)kTile);
+  if (op == GCN_GEMM_TN) {
+    ProfScope ps("grouped_tn", s);
+    const dim3 grid((unsigned)a.groups, cols, (unsigned)ceil_div((int64_t)a.K, (int64_t)kTile));
+    hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_TN>), grid, dim3(kThreads), 0, s, a);
+  } else {
+    ProfScope ps(op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
+    const dim3 grid((unsigned)(a.rows / kTile + a.groups), cols);
+    if (op == GCN_GEMM_NN)
+      hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NN>), grid, dim3(kThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NT>), grid, dim3(kThreads), 0, s, a);
+  }
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
+}  // namespace
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* offsets,
+                                       int64_t rows, int64_t N, int64_t K, const void* A,
+                                       int64_t lda, const void* B, int64_t ldb, int dtype, void* C,
+                                       int64_t ldc, int dtype_c, int64_t stride_w, void* stream) {
+  clear_error();
+  CallScope scope(stream);
+  const bool tn = op == GCN_GEMM_TN;
+  if ((op != GCN_GEMM_NN && op != GCN_GEMM_NT && !tn) || n_groups < 1 || n_groups >= 65536 ||
+      rows < 0 || N < 1 || K < 1 || N >= (1 << 24) || K >= (1 << 24)) {
+    set_error("need a known op, n_groups in [1, 65536), rows >= 0 and N, K in [1, 2^24)");
+    return GCN_EINVAL;
+  }
+  if (rows >= (int64_t(1) << 31)) {
+    set_error("need rows < 2^31");
+    return GCN_ERANGE;
+  }
+  if ((dtype != GCN_DT_F32 && dtype != GCN_DT_BF16) ||
+      (dtype_c != GCN_DT_F32 && (tn || dtype_c != dtype))) {
+    set_error("need a known dtype, and dtype_c fp32 or (NN, NT) the operands'");
+    return GCN_EINVAL;
+  }
+  if (rows == 0 && !tn) return GCN_OK;
+  const int64_t big = int64_t(1) << 40;
+  if (!offsets || !C || (rows > 0 && (!A || !B)) || lda < K || ldc < N ||
+      ldb < (op == GCN_GEMM_NT ? K : N) || lda > big || ldb > big || ldc > big || stride_w < 0 ||
+      (tn && n_groups > 1 && stride_w < (K - 1) * ldc + N)) {
+    set_error("offsets, A, B, C must be non-NULL, row strides at least the rows' lengths, and "
+              "stride_w >= 0 (TN: at least a matrix of C)");
+    return GCN_EINVAL;
+  }
+  const GroupArgs a{(int)n_groups, offsets, rows, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, s);
+  return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, s) : grouped<bf16, bf16>(op, a, s);
+}

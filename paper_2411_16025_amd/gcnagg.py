@@ -35,7 +35,8 @@ EXPORTS = ("gcn_build_csr", "gcn_normalize", "gcn_normalize_rc", "gcn_normalize_
            "gcn_prepost_split",
            "gcn_add_rows", "gcn_add_rows_q", "gcn_aggregate_fwd", "gcn_aggregate_bwd", "gcn_aggregate_fwd_noalloc",
            "gcn_aggregate_fwd_q8halo", "gcn_quantize_rows_u8", "gcn_layernorm_quantize",
-           "gcn_gemm_f32", "gcn_relu",
+           "gcn_gemm_f32", "gcn_relu", "gcn_gemm_grouped", "gcn_dropout",
+           "gcn_layernorm_affine_fwd", "gcn_layernorm_affine_bwd",
            "gcn_relu_bwd", "gcn_softmax_xent", "gcn_gcn2_step", "gcn_graph_free",
            "gcn_graph_info", "gcn_graph_export", "gcn_graph_bins", "gcn_profile_enable",
            "gcn_profile_read", "gcn_last_error")
@@ -86,6 +87,13 @@ def lib():
                                      P, P, P]
         L.gcn_sage3_forward.argtypes = [P, P, i64, i64, i64, i64, P, P, P, P, ctypes.c_double, P,
                                         i64, P, i64, P, i64, P]
+        L.gcn_gemm_grouped.argtypes = [i32, i64, P, i64, i64, i64, P, i64, P, i64, i32, P, i64, i32,
+                                       i64, P]
+        L.gcn_dropout.argtypes = [i64, i64, P, i64, i32, P, P, i64, P]
+        L.gcn_layernorm_affine_fwd.argtypes = [i64, i64, P, i64, i32, P, P, ctypes.c_double, P, P,
+                                               i64, P]
+        L.gcn_layernorm_affine_bwd.argtypes = [i64, i64, P, i64, i32, P, ctypes.c_double, P, P, i64,
+                                               P, i64, P, P, P]
         L.gcn_graph_free.argtypes = [P]
         L.gcn_graph_free.restype = None
         L.gcn_graph_info.argtypes = [P, P, P, P]
@@ -597,6 +605,189 @@ def gcn_sage3_step(g: Graph, X: torch.Tensor, params, labels: torch.Tensor, lp_m
                                 dE.data_ptr() if dE is not None else None, loss.data_ptr(),
                                 _stream(stream)))
     return loss, grads, dE
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError("tensors must be on the current device (cuda:%d), got %s"
+                             % (dev, t.device))
+
+
+def _new(shape, dtype, device, stream):
+    """An output that work on `stream` writes: taken on that stream, so that its
+    memory is free there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _ld(t, name):
+    """Row stride of a 2-D row-major tensor, also of one with a single row."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("%s must be a 2-D row-major tensor (unit column stride)" % name)
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def gcn_gemm_grouped(op: int, offsets: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                     C: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                     stream=None):
+    """Products by group over the rows [offsets[g], offsets[g + 1]) (int64, on the GPU):
+    NN C_g = A_g B[g], NT C_g = A_g B[g]^T (B [groups, ., .], C [rows, N]) or TN
+    C[g] = A_g^T B_g (C [groups, K, N], fp32). Rows that belong to no group are not
+    written: a C that is made here holds nothing defined in them."""
+    _dev(offsets, torch.int64, "offsets")
+    code = _dtype_code(_dev(A, None, "A"))
+    _dev(B, A.dtype, "B")
+    if offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+        raise ValueError("offsets must be contiguous with groups + 1 entries")
+    G = offsets.numel() - 1
+    lda = _ld(A, "A")
+    rows, K = A.shape
+    if op == GCN_GEMM_TN:
+        ldb = _ld(B, "B")
+        if B.shape[0] != rows:
+            raise ValueError("A and B must have the same rows")
+        N = B.shape[1]
+        shape, dt = (G, K, N), torch.float32 if out_dtype is None else out_dtype
+    elif op in (GCN_GEMM_NN, GCN_GEMM_NT):
+        if B.dim() != 3 or B.shape[0] != G or (B.stride(2) != 1 and B.shape[2] > 1):
+            raise ValueError("B must be [groups, ., .] with unit column stride")
+        ldb = max(B.stride(1), B.shape[2]) if B.shape[1] <= 1 else B.stride(1)
+        N = B.shape[2 if op == GCN_GEMM_NN else 1]
+        if B.shape[1 if op == GCN_GEMM_NN else 2] != K:
+            raise ValueError("inner dimensions differ")
+        shape, dt = (rows, N), A.dtype if out_dtype is None else out_dtype
+    else:
+        raise ValueError("unknown op")
+    if C is None:
+        C = _new(shape, dt, A.device, stream)
+    _dev(C, dt if out_dtype is not None else None, "C")
+    if tuple(C.shape) != shape:
+        raise ValueError("C must be %s" % (shape,))
+    if op == GCN_GEMM_TN:
+        if C.stride(2) != 1 and N > 1:
+            raise ValueError("C must have unit column stride")
+        ldc = max(C.stride(1), N) if K <= 1 else C.stride(1)
+        stride_w = C.stride(0)
+    else:
+        ldc, stride_w = _ld(C, "C"), B.stride(0)
+    _on_current_device(offsets, A, B, C)
+    _check(lib().gcn_gemm_grouped(op, G, offsets.data_ptr(), rows, N, K, A.data_ptr(), lda,
+                                  B.data_ptr(), ldb, code, C.data_ptr(), ldc, _dtype_code(C),
+                                  stride_w, _stream(stream)))
+    return C
+
+
+class Dropout:
+    """Which elements a dropout keeps (gcn_dropout_spec): p, the generator's seed, and
+    the call and row0 that name the mask; `step` (an int64 tensor of one element on
+    the GPU, or None) is added to call when the kernel runs."""
+
+    class _Spec(ctypes.Structure):
+        _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("call", ctypes.c_uint64),
+                    ("step", ctypes.c_void_p), ("row0", ctypes.c_int64)]
+
+    def __init__(self, p: float, seed: int, call: int = 0, row0: int = 0,
+                 step: torch.Tensor | None = None):
+        if step is not None:
+            _dev(step, torch.int64, "step")
+            if step.numel() != 1:
+                raise ValueError("step must hold one value")
+        for v, nm in ((seed, "seed"), (call, "call")):
+            if not 0 <= v < 1 << 64:
+                raise ValueError("%s must be in [0, 2^64)" % nm)
+        self.p, self.seed, self.call, self.row0, self.step = p, seed, call, row0, step
+
+    def _ref(self):
+        return ctypes.byref(self._Spec(self.p, self.seed, self.call,
+                                       self.step.data_ptr() if self.step is not None else None,
+                                       self.row0))
+
+
+def _drop_ref(drop):
+    if drop is None:
+        return None
+    if not isinstance(drop, Dropout):
+        raise TypeError("drop must be a Dropout")
+    _on_current_device(drop.step)
+    return drop._ref()
+
+
+def _rows_out(X, Y, name, stream):
+    """Y, or a new one: rows like X's."""
+    if Y is None:
+        return _new(tuple(X.shape), X.dtype, X.device, stream)
+    _dev(Y, X.dtype, name)
+    if Y.shape != X.shape:
+        raise ValueError("%s must be %s" % (name, tuple(X.shape)))
+    return Y
+
+
+def gcn_dropout(X: torch.Tensor, drop: Dropout, Y: torch.Tensor | None = None, stream=None):
+    """Y = X / (1 - p) where drop keeps the element, else 0 (Y may be X); the gradient
+    is the same call on dY."""
+    code = _dtype_code(_dev(X, None, "X"))
+    if not isinstance(drop, Dropout):
+        raise TypeError("drop must be a Dropout")
+    ldx = _ld(X, "X")
+    Y = _rows_out(X, Y, "Y", stream)
+    _on_current_device(X, Y)
+    _check(lib().gcn_dropout(X.shape[0], X.shape[1], X.data_ptr(), ldx, code, _drop_ref(drop),
+                             Y.data_ptr(), _ld(Y, "Y"), _stream(stream)))
+    return Y
+
+
+def _weight(t, F, name):
+    if t is None:
+        return None
+    _dev(t, torch.float32, name)
+    if t.numel() != F or not t.is_contiguous():
+        raise ValueError("%s must hold F contiguous values" % name)
+    return t.data_ptr()
+
+
+def gcn_layernorm_affine_fwd(X: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5,
+                             drop: Dropout | None = None, Y: torch.Tensor | None = None,
+                             stream=None):
+    """Y = dropout((X - mean) / sqrt(var + eps) * gamma + beta) per row (Y may be X)."""
+    code = _dtype_code(_dev(X, None, "X"))
+    ldx = _ld(X, "X")
+    n, F = X.shape
+    Y = _rows_out(X, Y, "Y", stream)
+    _on_current_device(X, Y, gamma, beta)
+    _check(lib().gcn_layernorm_affine_fwd(n, F, X.data_ptr(), ldx, code, _weight(gamma, F, "gamma"),
+                                          _weight(beta, F, "beta"), eps, _drop_ref(drop),
+                                          Y.data_ptr(), _ld(Y, "Y"), _stream(stream)))
+    return Y
+
+
+def gcn_layernorm_affine_bwd(X: torch.Tensor, dY: torch.Tensor, gamma=None, eps: float = 1e-5,
+                             drop: Dropout | None = None, dX: torch.Tensor | None = None,
+                             input_grad: bool = True, weight_grad: bool = True, stream=None):
+    """(dX, dgamma, dbeta) of gcn_layernorm_affine_fwd; dX is None without input_grad (it
+    may be given, and be dY or X itself), dgamma and dbeta are without weight_grad."""
+    code = _dtype_code(_dev(X, None, "X"))
+    _dev(dY, X.dtype, "dY")
+    ldx, lddy = _ld(X, "X"), _ld(dY, "dY")
+    n, F = X.shape
+    if dY.shape != X.shape:
+        raise ValueError("dY must be %s" % (tuple(X.shape),))
+    dX = _rows_out(X, dX, "dX", stream) if input_grad else None
+    dgamma = _new((F,), torch.float32, X.device, stream) if weight_grad else None
+    dbeta = _new((F,), torch.float32, X.device, stream) if weight_grad else None
+    _on_current_device(X, dY, dX, gamma)
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    _check(lib().gcn_layernorm_affine_bwd(n, F, X.data_ptr(), ldx, code, _weight(gamma, F, "gamma"),
+                                          eps, _drop_ref(drop), dY.data_ptr(), lddy, ptr(dX),
+                                          _ld(dX, "dX") if dX is not None else 0, ptr(dgamma),
+                                          ptr(dbeta), _stream(stream)))
+    return dX, dgamma, dbeta
 
 
 def gcn_graph_info(g: Graph):

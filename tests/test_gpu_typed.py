@@ -1,0 +1,578 @@
+"""The typed layer's operators against 64-bit references: dropout from counters, LayerNorm
+with weights, products by group, and a layer made of them."""
+
+import numpy as np
+import pytest
+
+import synth
+import typed_ref as ref
+from gpu_util import bf16_round, dev, host, note
+
+pytestmark = pytest.mark.gpu
+
+KINDS = ("f32", "bf16")
+
+
+@pytest.fixture(scope="module")
+def G():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2411_16025_amd as pkg
+    pkg.lib()
+    return pkg
+
+
+def tdtype(kind):
+    import torch
+    return torch.float32 if kind == "f32" else torch.bfloat16
+
+
+def values(seed, n, F, kind, scale=1.0, shift=0.0):
+    """(n x F values of the type as fp32, on the host)."""
+    x = np.random.default_rng(seed).standard_normal((n, F)).astype(np.float32) * np.float32(scale) \
+        + np.float32(shift)
+    return bf16_round(x) if kind == "bf16" else x
+
+
+def rows(x, kind, pad=0, shift=0, fill=np.nan):
+    """x on the GPU with `pad` columns and `shift` elements in front, both holding `fill`."""
+    import torch
+    n, F = x.shape
+    flat = torch.full((shift + n * (F + pad) + 8,), float(fill), dtype=tdtype(kind), device="cuda:0")
+    t = flat[shift:shift + n * (F + pad)].view(n, F + pad)[:, :F] if n else \
+        torch.empty((0, F), dtype=tdtype(kind), device="cuda:0")
+    if n:
+        t.copy_(dev(x).to(tdtype(kind)))
+    return t
+
+
+def back(t):
+    return host(t.float()).astype(np.float64)
+
+
+def within(got, want, bound, what):
+    err = np.abs(got - want)
+    bad = ~(err <= bound + 1e-37)
+    if bad.any():
+        at = tuple(int(v) for v in np.argwhere(bad)[0])
+        raise AssertionError("%s: %d of %d outside, first at %s: got %r want %r bound %r" %
+                             (what, bad.sum(), bad.size, at, got[at], want[at],
+                              np.broadcast_to(bound, got.shape)[at]))
+
+
+# ---- dropout ---------------------------------------------------------------------
+
+SHAPES = [(1, 1), (1, 4), (3, 5), (7, 47), (64, 64), (5, 100), (1000, 33), (129, 256), (2, 4099),
+          (33, 1024)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,F", SHAPES)
+def test_dropout(G, n, F, kind):
+    import torch
+    for pad, shift, p in ((0, 0, 0.5), (8, 0, 0.25), (3, 1, 0.9)):
+        note("dropout n=%d F=%d %s pad=%d shift=%d" % (n, F, kind, pad, shift))
+        x = values(n * 31 + F, n, F, kind)
+        X = rows(x, kind, pad, shift)
+        drop = G.Dropout(p, seed=(5 << 40) + F, call=(3 << 33) + n, row0=17)
+        f = ref.factor(n, F, p, drop.seed, drop.call, 17)
+        Y = rows(np.full_like(x, 7.0), kind, pad + 1, 0, fill=9.0)
+        G.gcn_dropout(X, drop, Y)
+        got = back(Y)
+        # x scale: the scale and the product rounded once each, then the type's half step
+        half = ref.HALF[kind] if kind == "bf16" else 0.0
+        within(got, x * f, (2.01 * ref.U + half * 1.001) * np.abs(x * f), "dropout")
+        assert np.array_equal(got != 0, (x != 0) & (f != 0))
+        if n > 1:  # what lies between the rows is left
+            flat = torch.as_strided(Y, (n - 1, pad + 1), (Y.stride(0), 1), Y.storage_offset() + F)
+            assert bool((flat == 9.0).all())
+        G.gcn_dropout(X, drop, X)  # in place
+        assert np.array_equal(back(X), got)
+
+
+def test_dropout_special_values(G):
+    note("dropout special values")
+    x = np.array([[np.inf, np.nan, -np.inf, -0.0, 3.4e38, 1e-45, -1e-45, 0.0]] * 64, np.float32)
+    Y = host(G.gcn_dropout(dev(x), G.Dropout(0.5, 3)))
+    k = ref.kept(64, 8, 0.5, 3)
+    with np.errstate(over="ignore"):
+        want = np.where(k, x * np.float32(2), np.float32(0))
+    assert np.array_equal(Y.view(np.uint32)[~np.isnan(want)], want.view(np.uint32)[~np.isnan(want)])
+    assert np.array_equal(np.isnan(Y), np.isnan(want))
+    # nothing dropped: a copy, bit for bit
+    same = host(G.gcn_dropout(dev(x), G.Dropout(0.0, 3)))
+    assert np.array_equal(same.view(np.uint32)[~np.isnan(x)], x.view(np.uint32)[~np.isnan(x)])
+
+
+def test_dropout_rows_of_workers(G):
+    """Workers that hold parts of the rows get the parts of one mask."""
+    note("dropout parts")
+    import torch
+    X = dev(values(5, 100, 47, "f32"))
+    whole = G.gcn_dropout(X, G.Dropout(0.4, 11, 2))
+    parts = [G.gcn_dropout(X[a:b], G.Dropout(0.4, 11, 2, row0=a)) for a, b in ((0, 33), (33, 34), (34, 100))]
+    assert torch.equal(torch.cat(parts), whole)
+    assert not torch.equal(G.gcn_dropout(X, G.Dropout(0.4, 11, 3)), whole)
+    # the last row that a mask has
+    last = G.gcn_dropout(X[:2], G.Dropout(0.4, 11, 2, row0=(1 << 32) - 2))
+    f = ref.factor(2, 47, 0.4, 11, 2, (1 << 32) - 2)
+    assert np.array_equal(host(last) != 0, f != 0)
+
+
+def test_dropout_empty(G):
+    import torch
+    note("dropout empty")
+    assert G.gcn_dropout(torch.empty((0, 5), device="cuda:0"), G.Dropout(0.5, 1)).shape == (0, 5)
+
+
+# ---- LayerNorm with weights --------------------------------------------------------
+
+NORM_SHAPES = [(1, 1), (1, 2), (3, 7), (5, 32), (9, 47), (70, 64), (17, 100), (33, 128), (300, 256),
+               (11, 300), (19, 512), (6, 1000), (9, 1024), (5, 2048), (3, 2056), (4, 4096), (3, 4100),
+               (2, 8192), (2, 8200), (1, 20001), (2500, 20)]
+
+
+def weights(F, seed):
+    r = np.random.default_rng(seed)
+    return (1 + 0.3 * r.standard_normal(F)).astype(np.float32), \
+        (0.2 * r.standard_normal(F)).astype(np.float32)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,F", NORM_SHAPES)
+def test_layernorm_affine(G, n, F, kind):
+    for pad, shift, p, affine, mean in ((0, 0, 0.0, True, 0.0), (8, 0, 0.5, True, 3.0),
+                                        (5, 3, 0.1, False, 0.0)):
+        note("norm n=%d F=%d %s pad=%d shift=%d p=%g" % (n, F, kind, pad, shift, p))
+        x, dy = values(n + F, n, F, kind, 1.5, mean), values(n + F + 1, n, F, kind)
+        gamma, beta = weights(F, F) if affine else (np.ones(F, np.float32), np.zeros(F, np.float32))
+        wg, wb = (dev(gamma), dev(beta)) if affine else (None, None)
+        drop = G.Dropout(p, seed=F, call=n, row0=5) if p else None
+        f = ref.factor(n, F, p, F, n, 5) if p else 1.0
+        eps = 1e-5
+        X, dY = rows(x, kind, pad, shift), rows(dy, kind, pad + 2, shift)
+        Y = G.gcn_layernorm_affine_fwd(X, wg, wb, eps, drop)
+        within(back(Y), ref.norm_fwd(x, gamma, beta, eps, f),
+               ref.norm_fwd_bound(x, gamma, beta, eps, f, kind), "Y")
+        dx, dg, db = ref.norm_bwd(x, dy, gamma, eps, f)
+        bx, bg, bb = ref.norm_bwd_bound(x, dy, gamma, eps, f, kind)
+        dX, dgamma, dbeta = G.gcn_layernorm_affine_bwd(X, dY, wg, eps, drop)
+        within(back(dX), dx, bx, "dX")
+        within(back(dgamma), dg, bg, "dgamma")
+        within(back(dbeta), db, bb, "dbeta")
+        # parts of the outputs alone give the same bits, and so does a call in place
+        only, none, _ = G.gcn_layernorm_affine_bwd(X, dY, wg, eps, drop, weight_grad=False)
+        assert none is None and np.array_equal(back(only), back(dX))
+        none, dg2, db2 = G.gcn_layernorm_affine_bwd(X, dY, wg, eps, drop, input_grad=False)
+        assert none is None
+        assert np.array_equal(host(dg2), host(dgamma)) and np.array_equal(host(db2), host(dbeta))
+        G.gcn_layernorm_affine_bwd(X, dY, wg, eps, drop, dX=dY)
+        assert np.array_equal(back(dY), back(dX))
+        G.gcn_layernorm_affine_fwd(X, wg, wb, eps, drop, Y=X)
+        assert np.array_equal(back(X), back(Y))
+
+
+@pytest.mark.parametrize("F", [64, 100, 1024, 8193])
+def test_layernorm_affine_far_mean(G, F):
+    """Rows whose mean is 4000 times their deviation: the normalized values keep fp32's
+    precision (the bound has no term of the mean; the double sums' error is 2^-53 of
+    it per addition)."""
+    note("norm far mean F=%d" % F)
+    x = values(F, 5, F, "f32", 0.25, 1000.0)
+    gamma, beta = weights(F, 3)
+    Y = G.gcn_layernorm_affine_fwd(dev(x), dev(gamma), dev(beta), 1e-5)
+    within(back(Y), ref.norm_fwd(x, gamma, beta, 1e-5),
+           ref.norm_fwd_bound(x, gamma, beta, 1e-5, 1.0, "f32"), "Y")
+
+
+def test_layernorm_affine_large_and_constant(G):
+    note("norm large values and constant rows")
+    x = values(1, 4, 96, "f32")
+    x[0] *= np.float32(1e30)    # squares beyond fp32
+    x[1] = np.float32(2.5)      # no deviation
+    x[2] *= np.float32(1e-18)
+    dy = values(2, 4, 96, "f32")
+    gamma, beta = weights(96, 4)
+    Y = G.gcn_layernorm_affine_fwd(dev(x), dev(gamma), dev(beta), 1e-12)
+    within(back(Y), ref.norm_fwd(x, gamma, beta, 1e-12),
+           ref.norm_fwd_bound(x, gamma, beta, 1e-12, 1.0, "f32"), "Y")
+    dX, _, _ = G.gcn_layernorm_affine_bwd(dev(x), dev(dy), dev(gamma), 1e-12)
+    within(back(dX), ref.norm_bwd(x, dy, gamma, 1e-12)[0],
+           ref.norm_bwd_bound(x, dy, gamma, 1e-12, 1.0, "f32")[0], "dX")
+
+
+def test_layernorm_affine_nan_stays_in_its_row(G):
+    note("norm NaN row")
+    x, dy = values(8, 6, 64, "f32"), values(9, 6, 64, "f32")
+    x[2, 5] = np.nan
+    Y = host(G.gcn_layernorm_affine_fwd(dev(x)))
+    assert np.isnan(Y[2]).all() and np.isfinite(np.delete(Y, 2, 0)).all()
+    dX, _, db = G.gcn_layernorm_affine_bwd(dev(x), dev(dy))
+    assert np.isfinite(np.delete(host(dX), 2, 0)).all() and np.isfinite(host(db)).all()
+
+
+@pytest.mark.parametrize("n,F,kind", [(200000, 8, "f32"), (30011, 47, "bf16"), (70001, 256, "f32")])
+def test_layernorm_affine_weight_sums_of_many_rows(G, n, F, kind):
+    """Sums over many rows: worst-case bounds say little here, so the errors are held to
+    what independent roundings give: a sum of m terms in any tree has at most
+    about sqrt(m) U of the terms' root sum of squares times log2(m); 4e-6 relative
+    to the root sum of squares is 16 times that at 30 steps."""
+    note("norm sums n=%d F=%d" % (n, F))
+    x, dy = values(n, n, F, kind), values(n + 1, n, F, kind)
+    gamma, _ = weights(F, 1)
+    f = ref.factor(n, F, 0.5, 9)
+    _, dg, db = ref.norm_bwd(x, dy, gamma, 1e-5, f)
+    g = dy.astype(np.float64) * f
+    h, _ = ref.norm(x, 1e-5)
+    out = [G.gcn_layernorm_affine_bwd(rows(x, kind), rows(dy, kind), dev(gamma), 1e-5,
+                                      G.Dropout(0.5, 9)) for _ in range(2)]
+    within(back(out[0][1]), dg, 4e-6 * np.sqrt((g * h * g * h).sum(0)), "dgamma")
+    within(back(out[0][2]), db, 4e-6 * np.sqrt((g * g).sum(0)), "dbeta")
+    for a, b in zip(*out):  # bit for bit again
+        assert np.array_equal(back(a), back(b))
+
+
+def test_layernorm_affine_no_rows(G):
+    import torch
+    note("norm no rows")
+    X = torch.empty((0, 12), device="cuda:0")
+    assert G.gcn_layernorm_affine_fwd(X).shape == (0, 12)
+    dX, dg, db = G.gcn_layernorm_affine_bwd(X, X)
+    assert dX.shape == (0, 12) and not dg.any() and not db.any()
+
+
+def test_layernorm_affine_against_differences(G):
+    """d(sum(Y C)) along a direction, by the gradient and by central differences of the 64-bit
+    forward pass (step 1e-4: its own error is about 1e-8 of the value)."""
+    note("norm differences")
+    n, F, p = 9, 60, 0.3
+    r = np.random.default_rng(3)
+    x, c = values(1, n, F, "f32"), values(2, n, F, "f32")
+    gamma, beta = weights(F, 5)
+    f = ref.factor(n, F, p, 77)
+    dX, dg, db = G.gcn_layernorm_affine_bwd(dev(x), dev(c), dev(gamma), 1e-5, G.Dropout(p, 77))
+    vx, vg, vb = r.standard_normal((n, F)), r.standard_normal(F), r.standard_normal(F)
+    t = 1e-4
+
+    def loss(s):
+        return (ref.norm_fwd(x + s * vx, gamma + s * vg, beta + s * vb, 1e-5, f) * c).sum()
+    slope = (loss(t) - loss(-t)) / (2 * t)
+    got = (back(dX) * vx).sum() + (back(dg) * vg).sum() + (back(db) * vb).sum()
+    size = (np.abs(back(dX) * vx)).sum() + np.abs(back(dg) * vg).sum() + np.abs(back(db) * vb).sum()
+    assert abs(got - slope) < 1e-6 * size
+
+
+# ---- products by group ---------------------------------------------------------------
+
+# groups' sizes; rows before the first and behind the last group
+LAYOUTS = [([1], 0, 0), ([0], 0, 0), ([0, 0, 5, 0], 2, 3), ([64, 1, 0, 63, 65], 0, 0),
+           ([300, 17, 0, 129], 5, 7), ([3] * 70 + [0] * 5 + [40], 1, 0), ([700], 0, 1)]
+WIDTHS = [(1, 1), (8, 16), (47, 33), (100, 64), (64, 257), (129, 130)]
+
+
+def make_grouped(op, sizes, before, after, K, N, kind, seed):
+    ends = before + np.concatenate([[0], np.cumsum(sizes)])
+    n = int(ends[-1]) + after
+    r = np.random.default_rng(seed)
+    a = r.standard_normal((n, K)).astype(np.float32)
+    b = r.standard_normal((n, N) if op == 2 else
+                          (len(sizes), K, N) if op == 0 else (len(sizes), N, K)).astype(np.float32)
+    if kind == "bf16":
+        a, b = bf16_round(a), bf16_round(b)
+    return ends.astype(np.int64), n, a, b
+
+
+def on_gpu(b, kind, pad, shift):
+    """A [G, r, c] array with padded rows and matrices."""
+    import torch
+    g, r, c = b.shape
+    flat = torch.full((shift + g * (r * (c + pad) + pad) + 8,), float("nan"), dtype=tdtype(kind),
+                      device="cuda:0")
+    t = torch.as_strided(flat, (g, r, c), (r * (c + pad) + pad, c + pad, 1), shift)
+    t.copy_(dev(b).to(tdtype(kind)))
+    return t
+
+
+def run_grouped(G, op, sizes, before, after, K, N, kind, out, pad=0, shift=0, seed=0):
+    import torch
+    ends, n, a, b = make_grouped(op, sizes, before, after, K, N, kind, seed + K + N)
+    clean = [a.copy(), b.copy()]
+    outside = np.ones(n, bool)
+    outside[ends[0]:ends[-1]] = False
+    a[outside] = np.nan  # rows of no group do not take part
+    if op == 2:
+        b[outside] = np.nan
+    A = rows(a, kind, pad, shift)
+    B = rows(b, kind, pad, shift) if op == 2 else on_gpu(b, kind, pad, shift)
+    want, mag = ref.grouped(op, ends, *clean)
+    if op == 2:
+        C = on_gpu(np.full((len(sizes), K, N), 7.0, np.float32), out, pad, 0)
+    else:
+        C = rows(np.full((n, N), 7.0, np.float32), out, pad, shift)
+    G.gcn_gemm_grouped(op, dev(ends), A, B, C)
+    torch.cuda.synchronize()
+    got = back(C)
+    depth = max(sizes) if op == 2 else K
+    bound = ref.grouped_bound(want, mag, depth, out)
+    if op == 2:
+        within(got, want, bound, "C")
+    else:
+        within(got[~outside], want[~outside], bound[~outside], "C")
+        assert (got[outside] == 7.0).all()
+    again = C.clone()
+    G.gcn_gemm_grouped(op, dev(ends), A, B, again)
+    assert np.array_equal(back(again), got)
+
+
+@pytest.mark.parametrize("op,kind,out", [(op, kind, out) for op in (0, 1, 2) for kind, out in (
+    ("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")) if not (op == 2 and out == "bf16")])
+@pytest.mark.parametrize("layout", range(len(LAYOUTS)))
+def test_grouped(G, layout, op, kind, out):
+    for i, (K, N) in enumerate(WIDTHS):
+        pad, shift = ((0, 0), (8, 0), (3, 1))[i % 3]
+        note("grouped op=%d layout=%d K=%d N=%d %s->%s" % (op, layout, K, N, kind, out))
+        run_grouped(G, op, *LAYOUTS[layout], K, N, kind, out, pad, shift)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("op", [0, 1, 2])
+@pytest.mark.parametrize("sizes,K,N", [
+    ([1500, 0, 700], 256, 256), ([2100], 512, 96), ([1, 2, 0, 1, 3], 1024, 520),
+    ([5000, 3], 64, 128), ([257, 255, 256], 264, 512), ([40] * 33, 72, 80)])
+def test_grouped_larger(G, op, kind, sizes, K, N):
+    for pad, shift in ((0, 0), (1, 0)):
+        note("grouped op=%d %s sizes=%s K=%d N=%d pad=%d" % (op, kind, sizes[:4], K, N, pad))
+        run_grouped(G, op, sizes, 0, 2, K, N, kind, "f32", pad, shift, seed=1)
+
+
+@pytest.mark.parametrize("groups", [1, 64, 65, 4097, 20000])
+def test_grouped_many_groups(G, groups):
+    """Groups found among many, most of them empty."""
+    note("grouped many groups=%d" % groups)
+    r = np.random.default_rng(groups)
+    sizes = np.zeros(groups, np.int64)
+    at = r.integers(0, groups, 40)
+    sizes[at] = r.integers(1, 90, 40)
+    sizes[-1] = 3
+    for op in (0, 1, 2):
+        run_grouped(G, op, sizes.tolist(), 0, 0, 12, 20, "f32", "f32")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_grouped_shared_and_interleaved_weights(G, kind):
+    import torch
+    note("grouped weights' strides %s" % kind)
+    ends, n, a, b = make_grouped(0, [9, 0, 70], 0, 0, 40, 24, kind, 4)
+    A, t = rows(a, kind), tdtype(kind)
+    one = dev(b[0]).to(t)[None].expand(3, -1, -1)       # stride 0: one matrix for all groups
+    got = G.gcn_gemm_grouped(0, dev(ends), A, one, out_dtype=torch.float32)
+    want, mag = ref.grouped(0, ends, a, np.broadcast_to(b[:1], b.shape))
+    within(back(got), want, ref.grouped_bound(want, mag, 40, "f32"), "shared")
+    inter = dev(np.ascontiguousarray(b.transpose(1, 0, 2))).to(t).transpose(0, 1)  # [K][G][N] in memory
+    got = G.gcn_gemm_grouped(0, dev(ends), A, inter, out_dtype=torch.float32)
+    want, mag = ref.grouped(0, ends, a, b)
+    within(back(got), want, ref.grouped_bound(want, mag, 40, "f32"), "interleaved")
+
+
+def test_grouped_bad_offsets_stay_inside(G):
+    """Offsets out of range or order: groups are cut to the rows there are; what lies behind
+    C's rows is left."""
+    import torch
+    note("grouped bad offsets")
+    n, K, N = 50, 16, 24
+    a, b = values(1, n, K, "f32"), np.random.default_rng(2).standard_normal((3, K, N)).astype(np.float32)
+    A, B = rows(a, "f32"), dev(b)
+    flat = torch.full((n + 40, N), 7.0, device="cuda:0")
+    for ends in ([-5, 10, 20, 1 << 40], [0, 60, 70, 80], [30, 10, 40, 45], [1 << 50] * 4):
+        flat.fill_(7.0)
+        G.gcn_gemm_grouped(0, dev(np.array(ends, np.int64)), A, B, flat[20:20 + n])
+        assert bool((flat[:20] == 7.0).all()) and bool((flat[20 + n:] == 7.0).all()), ends
+        C = torch.full((5, K, N), 7.0, device="cuda:0")
+        G.gcn_gemm_grouped(2, dev(np.array(ends, np.int64)), A, A.repeat(1, 2)[:, :N], C[1:4])
+        assert bool((C[0] == 7.0).all()) and bool((C[4] == 7.0).all())
+    flat.fill_(7.0)
+    G.gcn_gemm_grouped(0, dev(np.array([-5, 10, 20, 1 << 40], np.int64)), A, B, flat[20:20 + n])
+    want, mag = ref.grouped(0, [0, 10, 20, 50], a, b)
+    within(back(flat[20:20 + n]), want, ref.grouped_bound(want, mag, K, "f32"), "cut offsets")
+
+
+def test_grouped_special_values(G):
+    """An infinity or NaN reaches the outputs of its own products and no others."""
+    note("grouped special values")
+    for kind in KINDS:
+        ends, n, a, b = make_grouped(0, [40, 0, 30], 0, 0, 64, 48, kind, 6)
+        a[3, 5], a[50, 60] = np.inf, np.nan
+        b[2, 7, 9] = -np.inf
+        got = back(G.gcn_gemm_grouped(0, dev(ends), rows(a, kind), dev(b).to(tdtype(kind))))
+        with np.errstate(invalid="ignore"):
+            want, _ = ref.grouped(0, ends, a, b)
+        assert np.array_equal(np.isfinite(got), np.isfinite(want)), kind
+        assert np.array_equal(np.isnan(got), np.isnan(want)), kind
+        dy = values(3, n, 48, kind)
+        dy[45, 2] = np.nan
+        b[2, 7, 9] = 1.0
+        a[3, 5], a[50, 60] = 1.0, 1.0
+        dw = back(G.gcn_gemm_grouped(2, dev(ends), rows(a, kind), rows(dy, kind)))
+        assert np.isnan(dw[2][:, 2]).all() and np.isfinite(np.delete(dw[2], 2, 1)).all()
+        assert np.isfinite(dw[0]).all() and not dw[1].any()
+
+
+def test_grouped_no_rows(G):
+    import torch
+    note("grouped no rows")
+    ends = dev(np.zeros(4, np.int64))
+    A = torch.empty((0, 16), device="cuda:0")
+    assert G.gcn_gemm_grouped(0, ends, A, torch.ones((3, 16, 8), device="cuda:0")).shape == (0, 8)
+    dw = torch.full((3, 16, 8), 7.0, device="cuda:0")
+    G.gcn_gemm_grouped(2, ends, A, torch.empty((0, 8), device="cuda:0"), dw)
+    assert not dw.any()
+
+
+def test_binding_refusals(G):
+    import torch
+    note("binding refusals")
+    X = torch.ones((4, 8), device="cuda:0")
+    with pytest.raises(TypeError):
+        G.gcn_dropout(X.double(), G.Dropout(0.5, 1))
+    with pytest.raises(TypeError):
+        G.gcn_dropout(X, 0.5)
+    with pytest.raises(ValueError):
+        G.gcn_dropout(X.t(), G.Dropout(0.5, 1))
+    with pytest.raises(ValueError):
+        G.Dropout(0.5, -1)
+    with pytest.raises(G.GcnError):
+        G.gcn_dropout(X, G.Dropout(1.0, 1))
+    with pytest.raises(TypeError):
+        G.gcn_layernorm_affine_bwd(X, X.bfloat16())
+    with pytest.raises(ValueError):
+        G.gcn_layernorm_affine_fwd(X, torch.ones(7, device="cuda:0"))
+    ends = torch.tensor([0, 4], device="cuda:0")
+    with pytest.raises(TypeError):
+        G.gcn_gemm_grouped(0, ends.int(), X, X[None])
+    with pytest.raises(ValueError):
+        G.gcn_gemm_grouped(0, ends, X, torch.ones((1, 4, 8), device="cuda:0"))
+    with pytest.raises(ValueError):
+        G.gcn_gemm_grouped(2, ends, X, X[:3])
+    with pytest.raises(G.GcnError):
+        G.gcn_gemm_grouped(0, ends, X, torch.ones((1, 8, 8), device="cuda:0"), out_dtype=torch.bfloat16)
+
+
+# ---- streams, captured graphs, a whole layer ---------------------------------------------
+
+
+class Layer:
+    """O = X W_type, Y = dropout(LayerNorm(O) gamma + beta), Z = A Y, and its gradients."""
+
+    def __init__(self, G, n=600, K=40, F=64, groups=5, seed=0):
+        r = np.random.default_rng(seed)
+        self.G, self.n, self.K, self.F, self.groups = G, n, K, F, groups
+        self.ends = np.sort(np.concatenate([[0, n], r.integers(0, n + 1, groups - 1)])).astype(np.int64)
+        self.W = (r.standard_normal((groups, K, F)) / np.sqrt(K)).astype(np.float32)
+        self.gamma, self.beta = weights(F, seed)
+        src, dst = synth.er_edges(seed + 50, n, 6 * n)
+        self.flags = synth.SYMMETRIZE | synth.ADD_SELF_LOOPS
+        self.edges = (src, dst)
+        self.g = G.gcn_build_csr(n, n, dev(src), dev(dst), self.flags)
+        G.gcn_normalize(self.g)
+
+    def step(self, X, dZ, w, drop, stream=None):
+        G, (offs, W, gamma, beta) = self.G, w
+        kw = dict(stream=stream)
+        O = G.gcn_gemm_grouped(G.GCN_GEMM_NN, offs, X, W, **kw)
+        Y = G.gcn_layernorm_affine_fwd(O, gamma, beta, 1e-5, drop, **kw)
+        Z = G.gcn_aggregate_fwd(self.g, Y, **kw)
+        dY = G.gcn_aggregate_bwd(self.g, dZ, **kw)
+        dO, dgamma, dbeta = G.gcn_layernorm_affine_bwd(O, dY, gamma, 1e-5, drop, **kw)
+        dX = G.gcn_gemm_grouped(G.GCN_GEMM_NT, offs, dO, W, **kw)
+        dW = G.gcn_gemm_grouped(G.GCN_GEMM_TN, offs, X, dO, **kw)
+        return Z, dX, dW, dgamma, dbeta
+
+    def weights(self):
+        return dev(self.ends), dev(self.W), dev(self.gamma), dev(self.beta)
+
+    def reference(self, x, dz, f):
+        import oracle
+        og = oracle.Graph(self.n, self.n, *self.edges, self.flags)
+        o, _ = ref.grouped(0, self.ends, x, self.W)
+        y = ref.norm_fwd(o, self.gamma, self.beta, 1e-5, f)
+        a = np.zeros((self.n, self.n))
+        for i in range(self.n):
+            s = slice(og.csr_ptr[i], og.csr_ptr[i + 1])
+            a[i, og.csr_idx[s]] = og.csr_val[s]
+        dy = a.T @ dz
+        do, dg, db = ref.norm_bwd(o, dy, self.gamma, 1e-5, f)
+        dx, _ = ref.grouped(1, self.ends, do, self.W)
+        dw, _ = ref.grouped(2, self.ends, x, do)
+        return a @ y, dx, dw, dg, db
+
+
+def near(got, want, what, rel=3e-6):
+    """Five operators in a row, each within a few U sqrt(K) of its sums: 3e-6 of the
+    result's norm is 50 U."""
+    got, want = back(got), np.asarray(want, np.float64)
+    err = np.linalg.norm(got - want) / max(np.linalg.norm(want), 1e-300)
+    assert err < rel, "%s: relative error %.2e" % (what, err)
+
+
+def test_layer_runs_together(G):
+    note("typed layer")
+    m = Layer(G)
+    x, dz = values(1, m.n, m.K, "f32"), values(2, m.n, m.F, "f32")
+    out = m.step(dev(x), dev(dz), m.weights(), G.Dropout(0.5, 21, 4))
+    want = m.reference(x, dz, ref.factor(m.n, m.F, 0.5, 21, 4))
+    for name, a, b in zip(("Z", "dX", "dW", "dgamma", "dbeta"), out, want):
+        near(a, b, name)
+    m.g.free()
+
+
+def test_layer_captured(G):
+    """The layer in a captured graph, replayed with new inputs, other group sizes and another
+    mask (the device's step counter), with eager runs of the same layer between the replays."""
+    import torch
+    note("typed layer captured")
+    m = Layer(G, seed=3)
+    X, dZ = dev(values(1, m.n, m.K, "f32")), dev(values(2, m.n, m.F, "f32"))
+    w = m.weights()
+    step = torch.zeros(1, dtype=torch.int64, device="cuda:0")
+    drop = G.Dropout(0.5, 33, call=10, step=step)
+    m.step(X, dZ, w, drop)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = m.step(X, dZ, w, drop)
+        step.add_(1)
+    r = np.random.default_rng(9)
+    for rep in range(4):
+        X.copy_(dev(values(10 + rep, m.n, m.K, "f32")))
+        ends = np.sort(np.concatenate([[0, m.n], r.integers(0, m.n + 1, m.groups - 1)]))
+        w[0].copy_(dev(ends.astype(np.int64)))
+        torch.cuda.synchronize()
+        eager = m.step(X, dZ, w, G.Dropout(0.5, 33, call=10 + rep))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(step) == rep + 1
+        for name, a, b in zip(("Z", "dX", "dW", "dgamma", "dbeta"), out, eager):
+            assert torch.equal(a, b), (rep, name)
+    del graph
+    m.g.free()
+
+
+def test_layer_on_two_streams(G):
+    """Two layers at once on streams of their own, each with its own temporaries."""
+    import torch
+    note("typed layer on two streams")
+    m = Layer(G, n=3000, seed=5)
+    w = m.weights()
+    ins = [(dev(values(20 + i, m.n, m.K, "f32")), dev(values(30 + i, m.n, m.F, "f32"))) for i in range(2)]
+    want = [m.step(x, dz, w, G.Dropout(0.5, 1, i)) for i, (x, dz) in enumerate(ins)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(3):
+        got = [m.step(*ins[i], w, G.Dropout(0.5, 1, i), stream=streams[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        for t, u in zip(a, b):
+            assert torch.equal(t, u)
+    m.g.free()
