@@ -49,7 +49,7 @@
 
 #include <algorithm>
 
-#include "common.h"
+#include "groups.h"
 
 namespace gcn {
 namespace {
@@ -159,6 +159,8 @@ struct TallArgs {
   const float* mask;
   int64_t ldm;
   bool relu;
+  Groups groups;     // products by group: B of group g at B + g stride_b
+  int64_t stride_b;
 };
 
 __device__ inline float finish(const TallArgs& a, float v, int64_t gm, int64_t gn) {
@@ -219,7 +221,8 @@ __device__ inline void mul_again(int64_t k0, int64_t k1, Load load, f16 (*acc)[N
 // meanwhile (two LDS buffers, one barrier a step). B is split by every
 // workgroup anew: laid out once by a kernel of its own it needed scratch, which a
 // captured call and one without free memory cannot have. BT: B is stored N x K.
-template <int WR, int WC, int RBW, int NBW, bool BT>
+// GROUPED: the rows of a tile are of one group, and so is B (groups.h).
+template <int WR, int WC, int RBW, int NBW, bool BT, bool GROUPED = false>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tall(TallArgs a) {
   constexpr int RB = WR * RBW, NB = WC * NBW;  // blocks of the workgroup's tile
   constexpr int ROWS = RB * 32;
@@ -237,8 +240,16 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tall(TallArgs a) {
   // the second finds its rows of A in that XCD's L2
   const int64_t xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;
   const int ct = (int)(idx % a.col_tiles);
-  const int64_t m0 = ((idx / a.col_tiles) * 8 + xcd) * ROWS;
+  int64_t m0 = (idx / a.col_tiles) * 8 + xcd;
   const int n0 = ct * NB * 32;
+  if constexpr (GROUPED) {
+    const GroupTile gt = group_tile(a.groups, m0, ROWS);
+    m0 = gt.beg;
+    a.M = gt.end;
+    a.B += gt.g * a.stride_b;
+  } else {
+    m0 *= ROWS;
+  }
   if (m0 >= a.M) return;  // the whole workgroup
 
   // a thread's pieces of A: row t / 4 + RP p, k = 4 (t % 4) .. + 3
@@ -455,6 +466,9 @@ struct TnArgs {
   int64_t ldb;
   float* part;  // [groups][M][N]
   int m_tiles, n_tiles;
+  Groups by;    // products by group: chunks of a group's rows (groups.h), the first one's sums
+  float* C;     // in C + g stride_c, those of the others in part
+  int64_t ldc, stride_c;
 };
 
 // The tile's columns of A and of B are loaded 8 rows per thread with 4-byte
@@ -464,7 +478,7 @@ struct TnArgs {
 // A is negated in every other chunk (see the head of this file). RUN: a workgroup
 // takes several chunks, one after the other, and adds their sums to its partial
 // C (without it the loop is gone, and with it the registers it costs).
-template <int WR, int WC, int RBW, int NBW, int PF, bool RUN>
+template <int WR, int WC, int RBW, int NBW, int PF, bool RUN, bool GROUPED = false>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
   constexpr int RB = WR * RBW, NB = WC * NBW, NT = 64 * WR * WC;
   constexpr int AU = (RB * 64 + NT - 1) / NT;  // (column, half step) units per thread
@@ -479,6 +493,15 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
   const int tile = (int)(idx % tiles);
   const int64_t group = idx / tiles * 8 + (blockIdx.x & 7);
   if (group >= a.groups) return;  // the whole workgroup
+  GroupTile gt;
+  if constexpr (GROUPED) {
+    gt = group_tile(a.by, group, (int)a.split);
+    if (gt.beg >= gt.end && (gt.beg != gt.first || gt.end < gt.first)) {
+      // no chunk; but the first one of an empty group is its zeros
+      if (gt.beg != gt.first) return;
+      gt.end = gt.beg;
+    }
+  }
   const int m0 = (tile / a.n_tiles) * RB * 32, n0 = (tile % a.n_tiles) * NB * 32;
 
   // unit u of a block of columns: column (u / 64) * 32 + u % 32, half u / 32 % 2;
@@ -498,8 +521,13 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
   const int h8 = 8 * ((t >> 5) & 1);  // the half is the same for all of a thread's units
 
   auto sum_chunk = [&](int64_t chunk, bool add) {
-    const int64_t kb = chunk * a.split;
-    const int64_t ke = kb + a.split < a.K ? kb + a.split : a.K;
+    int64_t kb = chunk * a.split;
+    int64_t ke = kb + a.split < a.K ? kb + a.split : a.K;
+    if constexpr (GROUPED) {
+      kb = gt.beg;
+      ke = kb + a.split < gt.end ? kb + a.split : gt.end;
+      chunk = (gt.beg - gt.first) / a.split;
+    }
     const float sign = chunk & 1 ? -kUp : kUp;
     float down = chunk & 1 ? -kDown : kDown;
     struct Pieces {
@@ -580,6 +608,15 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
 
     float* part = a.part + group * a.M * a.N;
     int wm = m0 + wr * RBW * 32, wn = n0 + wc * NBW * 32, N = a.N;
+    int64_t ldp = N;
+    if constexpr (GROUPED) {
+      if (chunk == 0) {
+        part = a.C + gt.g * a.stride_c;
+        ldp = a.ldc;
+      } else {
+        part = a.part + (group - gt.g - 1) * a.M * a.N;
+      }
+    }
     // (the addresses of the sums are formed here, not kept over the chunks)
     if (RUN) asm volatile("" : "+s"(wm), "+s"(wn), "+s"(N));
     if (not_finite<RBW, NBW>(acc)) {
@@ -611,7 +648,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
         for (int e = 0; e < 16; ++e) {
           const int m = wm + i * 32 + result_row(e, lane);
           if (m < a.M && n < N) {
-            float* q = part + (int64_t)m * N + n;
+            float* q = part + (int64_t)m * (GROUPED ? ldp : N) + n;
             const float v = acc[i][j][e] * down;
             *q = RUN && add ? *q + v : v;
           }
@@ -680,7 +717,8 @@ gcn_status gemm_split_tall(int op, int64_t M, int64_t N, int64_t K, const float*
   int per = (int)ceil_div(nb, col_tiles);
   per = per <= 2 ? per : (per + 1) / 2 * 2;
   ProfScope ps(op == GCN_GEMM_NN ? "gemm_nn" : "gemm_nt", stream);
-  const TallArgs a{M, (int)N, (int)K, A, lda, B, ldb, (int)col_tiles, C, ldc, mask, ldm, relu};
+  const TallArgs a{M, (int)N, (int)K, A, lda, B, ldb, (int)col_tiles, C, ldc, mask, ldm, relu,
+                   {}, 0};
   const hipError_t e = op == GCN_GEMM_NN ? launch_split_tall<false>(a, per, stream)
                                          : launch_split_tall<true>(a, per, stream);
   if (e != hipSuccess) return hip_fail(e, "k_split_tall", __FILE__, __LINE__);
@@ -726,7 +764,7 @@ gcn_status gemm_split_tn(int64_t M, int64_t N, int64_t K, const float* A, int64_
   float* part = nullptr;
   GCN_CHECK(talloc(&part, groups * M * N, stream, "GEMM partials"));
   const TnArgs a{(int)M, (int)N, K, split, chunks, run, groups, A, lda, B, ldb, part, (int)m_tiles,
-                 (int)n_tiles};
+                 (int)n_tiles, {}, nullptr, 0, 0};
   const dim3 grid((unsigned)(tiles * ceil_div(groups, (int64_t)8) * 8));
   hipError_t e;
   {
@@ -748,6 +786,89 @@ gcn_status gemm_split_tn(int64_t M, int64_t N, int64_t K, const float* A, int64_
                                   : hip_fail(e, "k_split_tn", __FILE__, __LINE__);
   tfree(part, stream);
   return st;
+}
+
+// ---- products by group -------------------------------------------------------------
+
+bool gemm_split_grouped_takes(int op, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc) {
+  if (op == GCN_GEMM_TN) return lda < (int64_t(1) << 26) && ldb < (int64_t(1) << 26);
+  return lda < (int64_t(1) << 22) && ldb < (int64_t(1) << (op == GCN_GEMM_NT ? 22 : 26)) &&
+         ldc < (int64_t(1) << 27);
+}
+
+namespace {
+
+template <bool BT>
+gcn_status launch_split_grouped(const TallArgs& a, int per, hipStream_t stream) {
+  auto go = [&](auto kern, int threads, int64_t rows) {
+    const int64_t blocks = ceil_div(group_slots(a.groups, rows), (int64_t)8) * 8 * a.col_tiles;
+    GCN_CHECK(launch_fits(blocks, threads));
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), 0, stream, a);
+    GCN_HIP(hipGetLastError());
+    return GCN_OK;
+  };
+  switch (per) {
+    case 1: return go(k_split_tall<4, 1, 1, 1, BT, true>, 256, 128);
+    case 2: return go(k_split_tall<4, 1, 1, 2, BT, true>, 256, 128);
+    case 4: return go(k_split_tall<2, 2, 2, 2, BT, true>, 256, 128);
+    case 6: return go(k_split_tall<2, 2, 2, 3, BT, true>, 256, 128);
+    default:
+      return a.groups.rows >= 32768 && a.groups.rows / a.groups.n >= 1024
+                 ? go(k_split_tall<4, 2, 2, 4, BT, true>, 512, 256)
+                 : go(k_split_tall<1, 4, 2, 2, BT, true>, 256, 64);
+  }
+}
+
+}  // namespace
+
+gcn_status gemm_split_grouped(int op, const Groups& g, int64_t N, int64_t K, const float* A,
+                              int64_t lda, const float* B, int64_t ldb, int64_t stride_w, float* C,
+                              int64_t ldc, hipStream_t stream) {
+  const int64_t nb = ceil_div(N, (int64_t)32);
+  const int64_t col_tiles = ceil_div(nb, (int64_t)8);
+  int per = (int)ceil_div(nb, col_tiles);
+  per = per <= 2 ? per : (per + 1) / 2 * 2;
+  const TallArgs a{g.rows, (int)N, (int)K, A, lda, B, ldb, (int)col_tiles, C, ldc, nullptr, 0,
+                   false, g, stride_w};
+  return op == GCN_GEMM_NN ? launch_split_grouped<false>(a, per, stream)
+                           : launch_split_grouped<true>(a, per, stream);
+}
+
+gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const float* A, int64_t lda,
+                                 const float* B, int64_t ldb, float* C, int64_t ldc,
+                                 int64_t stride_w, hipStream_t stream) {
+  // tiles and chunks as in gemm_split_tn; chunks of at most 2048 rows
+  const bool wide = K > 128 && N > 128 && g.rows / g.n >= 2048 && g.rows >= 131072;
+  const int64_t tm = wide ? 256 : 128;
+  const int64_t tn = wide ? 256 : (N <= 32 ? 32 : (N <= 64 ? 64 : 128));
+  const int64_t m_tiles = ceil_div(K, tm), n_tiles = ceil_div(N, tn), tiles = m_tiles * n_tiles;
+  const int64_t rounds = std::max<int64_t>(1, ceil_div(g.rows * tiles, (int64_t)512 * 2048));
+  const int64_t want = std::max<int64_t>(1, 512 * rounds / tiles);
+  const int64_t least = K * N <= 32768 ? 64 : 128;
+  const int64_t split = std::max<int64_t>(
+      least, std::min<int64_t>(2048, ceil_div(ceil_div(g.rows, want), (int64_t)kKs) * kKs));
+  const int64_t slots = group_slots(g, split);
+  const int64_t parts = g.rows / split;
+  const int64_t blocks = tiles * ceil_div(slots, (int64_t)8) * 8;
+  GCN_CHECK(launch_fits(blocks, 512));
+  TempScope temps(stream);
+  float* part = nullptr;
+  if (parts > 0) GCN_CHECK(temps.alloc(&part, parts * K * N, "grouped GEMM partials"));
+  const TnArgs a{(int)K, (int)N, 0, split, 0, 1, slots, A, lda, B, ldb, part, (int)m_tiles,
+                 (int)n_tiles, g, C, ldc, stride_w};
+  auto go = [&](auto kern, int threads) {
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), 0, stream, a);
+  };
+  if (wide)
+    go(k_split_tn<4, 2, 2, 4, 1, false, true>, 512);
+  else if (tn == 128)
+    go(k_split_tn<2, 2, 2, 2, 2, false, true>, 256);
+  else if (tn == 64)
+    go(k_split_tn<4, 1, 1, 2, 2, false, true>, 256);
+  else
+    go(k_split_tn<4, 1, 1, 1, 2, false, true>, 256);
+  GCN_HIP(hipGetLastError());
+  return parts > 0 ? sum_group_partials(g, split, K, N, part, C, ldc, stride_w, stream) : GCN_OK;
 }
 
 }  // namespace gcn

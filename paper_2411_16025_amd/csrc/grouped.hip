@@ -1,15 +1,9 @@
 // Products of rows sorted by group with one matrix per group (gcn_gemm_grouped).
-//
-// The groups' sizes are known on the device only. So a launch covers every tile
-// that any offsets could need, and a workgroup finds its own: with R rows per
-// tile, the tiles of group g take the slots from offsets[g] / R + g on. Its rows
-// need at most offsets[g + 1] / R - offsets[g] / R + 1 tiles, so the next group
-// begins behind them, all groups end before rows / R + n_groups, and the group of
-// a slot is found by comparing, without sums over the groups before it.
 
 #include <algorithm>
 
 #include "element.h"
+#include "groups.h"
 
 namespace gcn {
 namespace {
@@ -17,9 +11,7 @@ namespace {
 constexpr int kThreads = 256;
 
 struct GroupArgs {
-  int groups;
-  const int64_t* offsets;
-  int64_t rows;
+  Groups by;
   int N, K;  // columns of C; of A
   const void* A;
   int64_t lda;
@@ -29,28 +21,6 @@ struct GroupArgs {
   int64_t ldc;
   int64_t stride_w;
 };
-
-// An offset, inside [0, rows] whatever the array holds.
-__device__ inline int64_t offset_at(const GroupArgs& a, int g) {
-  const int64_t o = a.offsets[g];
-  return o < 0 ? 0 : (o > a.rows ? a.rows : o);
-}
-
-// The last group whose slots begin at or before `slot` (0 if none does): every
-// lane of the wavefront compares one group of the range left.
-__device__ inline int group_of(const GroupArgs& a, int64_t slot, int R) {
-  int lo = 0, len = a.groups;
-  while (len > 1) {
-    const int step = (len + 63) / 64;
-    const int g = lo + (int)(threadIdx.x & 63) * step;
-    const bool at = g < lo + len && offset_at(a, g) / R + g <= slot;
-    const uint64_t hit = __ballot(at);
-    const int last = hit ? 63 - __clzll((long long)hit) : 0;
-    lo += last * step;
-    len = min(step, a.groups - lo);
-  }
-  return lo;
-}
 
 // The general kernel: one 64 x 64 tile of C per workgroup, fp32 products, any
 // type, size and alignment.
@@ -68,20 +38,17 @@ __global__ __launch_bounds__(kThreads) void k_grouped(GroupArgs a) {
   int64_t m_end, k0 = 0, k1 = a.K;
   if constexpr (OP == GCN_GEMM_TN) {
     const int g = blockIdx.x;
-    k0 = offset_at(a, g);
-    k1 = offset_at(a, g + 1);
+    k0 = group_offset(a.by, g);
+    k1 = group_offset(a.by, g + 1);
     i0 = (int64_t)blockIdx.z * kTile;
     m_end = a.K;
     C += g * a.stride_w;
   } else {
-    const int64_t slot = blockIdx.x;
-    const int g = group_of(a, slot, kTile);
-    const int64_t beg = offset_at(a, g);
-    m_end = offset_at(a, g + 1);
-    const int64_t tile = slot - (beg / kTile + g);
-    i0 = beg + tile * kTile;
-    if (tile < 0 || i0 >= m_end) return;
-    B += g * a.stride_w;
+    const GroupTile gt = group_tile(a.by, blockIdx.x, kTile);
+    i0 = gt.beg;
+    m_end = gt.end;
+    if (i0 >= m_end) return;
+    B += gt.g * a.stride_w;
   }
   float acc[4][4] = {};
   for (int64_t kk = k0; kk < k1; kk += kDepth) {
@@ -123,11 +90,11 @@ gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
   const unsigned cols = (unsigned)ceil_div((int64_t)a.N, (int64_t)kTile);
   if (op == GCN_GEMM_TN) {
     ProfScope ps("grouped_tn", s);
-    const dim3 grid((unsigned)a.groups, cols, (unsigned)ceil_div((int64_t)a.K, (int64_t)kTile));
+    const dim3 grid((unsigned)a.by.n, cols, (unsigned)ceil_div((int64_t)a.K, (int64_t)kTile));
     hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_TN>), grid, dim3(kThreads), 0, s, a);
   } else {
     ProfScope ps(op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
-    const dim3 grid((unsigned)(a.rows / kTile + a.groups), cols);
+    const dim3 grid((unsigned)group_slots(a.by, kTile), cols);
     if (op == GCN_GEMM_NN)
       hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NN>), grid, dim3(kThreads), 0, s, a);
     else
@@ -137,7 +104,37 @@ gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
   return GCN_OK;
 }
 
+// One element per thread and step: the partial sums behind C's own in chunk order.
+__global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t split, int64_t K,
+                                                         int64_t N, const float* part, float* C,
+                                                         int64_t ldc, int64_t stride_w) {
+  const int g = blockIdx.y;
+  const int64_t beg = group_offset(by, g), rows = group_offset(by, g + 1) - beg;
+  const int64_t more = (rows + split - 1) / split - 1;
+  if (more <= 0) return;
+  part += beg / split * K * N;
+  C += g * stride_w;
+  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < K * N;
+       t += (int64_t)gridDim.x * kThreads) {
+    float* c = C + t / N * ldc + t % N;
+    float s = *c;
+    for (int64_t j = 0; j < more; ++j) s += part[j * K * N + t];
+    *c = s;
+  }
+}
+
 }  // namespace
+
+gcn_status sum_group_partials(const Groups& g, int64_t split, int64_t K, int64_t N,
+                              const float* part, float* C, int64_t ldc, int64_t stride_w,
+                              hipStream_t stream) {
+  const int64_t blocks = std::min<int64_t>(ceil_div(K * N, (int64_t)kThreads), 4096);
+  hipLaunchKernelGGL(k_group_sums, dim3((unsigned)blocks, (unsigned)g.n), dim3(kThreads), 0, stream,
+                     g, split, K, N, part, C, ldc, stride_w);
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
 }  // namespace gcn
 
 using namespace gcn;
@@ -172,8 +169,16 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
               "stride_w >= 0 (TN: at least a matrix of C)");
     return GCN_EINVAL;
   }
-  const GroupArgs a{(int)n_groups, offsets, rows, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
+  const Groups by{(int)n_groups, offsets, rows};
   hipStream_t s = (hipStream_t)stream;
+  if (dtype == GCN_DT_F32 && gemm_split_grouped_takes(op, N, K, lda, ldb, ldc)) {
+    ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
+    const float *fa = static_cast<const float*>(A), *fb = static_cast<const float*>(B);
+    float* fc = static_cast<float*>(C);
+    return tn ? gemm_split_tn_grouped(by, N, K, fa, lda, fb, ldb, fc, ldc, stride_w, s)
+              : gemm_split_grouped(op, by, N, K, fa, lda, fb, ldb, stride_w, fc, ldc, s);
+  }
+  const GroupArgs a{by, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
   if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, s);
   return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, s) : grouped<bf16, bf16>(op, a, s);
 }

@@ -1,0 +1,83 @@
+// Rows sorted by group, as kernels take them (gcn_gemm_grouped).
+//
+// The groups' sizes are known on the device only. So a launch covers every tile
+// that any offsets could need, and a workgroup finds its own: with R rows per
+// tile, the tiles of group g take the slots from offsets[g] / R + g on. Its rows
+// need at most offsets[g + 1] / R - offsets[g] / R + 1 tiles, so the next group
+// begins behind them, all groups end before rows / R + n_groups, and the group of
+// a slot is found by comparing, without sums over the groups before it.
+#pragma once
+
+#include "common.h"
+
+namespace gcn {
+
+struct Groups {
+  int n;
+  const int64_t* offsets;  // [n + 1]
+  int64_t rows;
+};
+
+inline int64_t group_slots(const Groups& g, int64_t R) { return g.rows / R + g.n; }
+
+// A launch has fewer than 2^32 threads along an axis.
+inline gcn_status launch_fits(int64_t blocks, int64_t threads) {
+  if (blocks < (int64_t(1) << 32) / threads) return GCN_OK;
+  set_error("more tiles than one launch takes");
+  return GCN_ERANGE;
+}
+
+// The grouped products on the bf16 matrix cores with three-part operands
+// (gemm_split.hip). C [rows x N] = A [rows x K] op(B_g), B_g of group g at
+// B + g stride_w; takes: whether sizes and strides fit the kernel.
+bool gemm_split_grouped_takes(int op, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc);
+gcn_status gemm_split_grouped(int op, const Groups& g, int64_t N, int64_t K, const float* A,
+                              int64_t lda, const float* B, int64_t ldb, int64_t stride_w, float* C,
+                              int64_t ldc, hipStream_t stream);
+// C_g [K x N] = A_g^T B_g, C_g at C + g stride_w.
+gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const float* A, int64_t lda,
+                                 const float* B, int64_t ldb, float* C, int64_t ldc,
+                                 int64_t stride_w, hipStream_t stream);
+// C_g += the partial sums of the chunks behind the first one of group g, in their
+// order; chunks of `split` rows, that of slot s at part + (s - g - 1) K N.
+gcn_status sum_group_partials(const Groups& g, int64_t split, int64_t K, int64_t N,
+                              const float* part, float* C, int64_t ldc, int64_t stride_w,
+                              hipStream_t stream);
+
+#ifdef __HIPCC__
+// An offset, inside [0, rows] whatever the array holds.
+__device__ inline int64_t group_offset(const Groups& a, int g) {
+  const int64_t o = a.offsets[g];
+  return o < 0 ? 0 : (o > a.rows ? a.rows : o);
+}
+
+// A tile's group and rows; beg >= end: nothing (first: the group's first tile).
+struct GroupTile {
+  int g;
+  int64_t beg, end, first;  // the tile's first row, the group's end, the group's first row
+};
+
+// The last group whose slots begin at or before `slot` (0 if none does): every
+// lane of the wavefront compares one group of the range left.
+__device__ inline GroupTile group_tile(const Groups& a, int64_t slot, int R) {
+  int lo = 0, len = a.n;
+  while (len > 1) {
+    const int step = (len + 63) / 64;
+    const int g = lo + (int)(threadIdx.x & 63) * step;
+    const bool at = g < lo + len && group_offset(a, g) / R + g <= slot;
+    const uint64_t hit = __ballot(at);
+    const int last = hit ? 63 - __clzll((long long)hit) : 0;
+    lo += last * step;
+    len = min(step, a.n - lo);
+  }
+  GroupTile t;
+  t.g = __builtin_amdgcn_readfirstlane(lo);
+  t.first = group_offset(a, t.g);
+  t.end = group_offset(a, t.g + 1);
+  const int64_t tile = slot - (t.first / R + t.g);
+  t.beg = tile < 0 ? t.end : t.first + tile * R;
+  return t;
+}
+#endif
+
+}  // namespace gcn
