@@ -178,6 +178,11 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     return tn ? gemm_split_tn_grouped(by, N, K, fa, lda, fb, ldb, fc, ldc, stride_w, s)
               : gemm_split_grouped(op, by, N, K, fa, lda, fb, ldb, stride_w, fc, ldc, s);
   }
+  if (dtype == GCN_DT_BF16 && gemm_grouped_bf16_takes(lda, ldb)) {
+    ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
+    return gemm_grouped_bf16(op, by, N, K, A, lda, B, ldb, C, ldc, dtype_c == GCN_DT_BF16, stride_w,
+                             s);
+  }
   const GroupArgs a{by, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
   if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, s);
   return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, s) : grouped<bf16, bf16>(op, a, s);
