@@ -1,6 +1,7 @@
 // bf16 products of rows sorted by group, on the matrix cores (gcn_gemm_grouped).
 
 #include <algorithm>
+#include <type_traits>
 
 #include "element.h"
 #include "groups.h"
@@ -12,6 +13,7 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef float f16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4u __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
 
@@ -28,7 +30,9 @@ struct MulArgs {
   void* C;
   int64_t ldc, stride_c;
   int col_tiles, row_tiles;  // tiles along N, and (TN) along M
-  int64_t slots, split;      // groups.h; TN: rows of a chunk
+  uint32_t slots;            // groups.h
+  int64_t split;             // TN: rows of a chunk
+  bool c_vec;                // bf16 C: rows of 8-byte aligned fours
   float* part;               // TN: sums of the chunks behind the first ones
 };
 
@@ -141,42 +145,66 @@ struct Loader {
   }
 };
 
+// The loads to LDS are done, for all wavefronts.
 __device__ inline void wait_loads() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vector memory, that is the loads to LDS
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vector memory
   __syncthreads();
+}
+
+// Lane l of 4 has four rows' values of column l; it gets the four columns of row l as bf16.
+__device__ inline u2 quad_rows(float r0, float r1, float r2, float r3) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+  const uint32_t p0 = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{r0, r1}), bf2));
+  const uint32_t p1 = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{r2, r3}), bf2));
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+  // with lane l ^ 1: rows 0, 2 (even lanes) or 1, 3 of two columns
+  const uint32_t q0 = __builtin_amdgcn_mov_dpp(p0, 0xB1, 0xF, 0xF, false);
+  const uint32_t q1 = __builtin_amdgcn_mov_dpp(p1, 0xB1, 0xF, 0xF, false);
+  const uint32_t sel = odd ? 0x03020706u : 0x05040100u;
+  const uint32_t w0 = __builtin_amdgcn_perm(q0, p0, sel), w1 = __builtin_amdgcn_perm(q1, p1, sel);
+  // with lane l ^ 2: row 0 or 1 (lower lanes) or 2 or 3 of four columns
+  const uint32_t t = __builtin_amdgcn_mov_dpp(high ? w0 : w1, 0x4E, 0xF, 0xF, false);
+  return high ? u2{t, w1} : u2{w0, t};
 }
 
 // A workgroup of WR x WC wavefronts, RB x CB blocks of 32 x 32 of C each.
 template <int OP, class TC, bool DIRECT, int BK, int WR, int WC, int RB, int CB>
-__global__ __launch_bounds__(64 * WR * WC, 2) void k_mul(MulArgs a) {
+__global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulArgs a) {
   constexpr bool AK = OP != GCN_GEMM_TN, BKC = OP == GCN_GEMM_NT;
   constexpr int NT = 64 * WR * WC, BM = 32 * WR * RB, BN = 32 * WC * CB;
   using TA = Tile<AK, BM, BK>;
   using TB = Tile<BKC, BN, BK>;
+  // an array per buffer: the compiler then knows that reads of one need not wait for the
+  // loads to another
   __shared__ __align__(16) char a0[TA::kBytes], a1[TA::kBytes], b0[TB::kBytes], b1[TB::kBytes];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = w / WC, wc = w % WC;
-  // Each XCD takes a run of row slots, four of them beside each other over the columns:
-  // the workgroups that run at a time share rows of A and columns of B in its L2.
-  const int64_t per_xcd = (a.slots + 7) / 8, idx = blockIdx.x >> 3;
-  int64_t slot;
+  // The tiles, chunk by chunk (TN) or in bands of four row tiles beside each other over the
+  // columns, divide evenly among the XCDs: the workgroups that run at a time on one share
+  // rows of A and columns of B in its L2.
+  constexpr int LEAST = OP == GCN_GEMM_TN ? 1 : 0;  // an empty group's C is zero
+  const int R = OP == GCN_GEMM_TN ? (int)a.split : BM;
+  const bool counted = a.by.n <= kCountedGroups;
+  int before = 0;
+  const uint32_t rows = counted ? group_tiles(a.by, R, LEAST, &before) : a.slots;
+  const uint32_t per_row = a.col_tiles * a.row_tiles, units = rows * per_row, xcd = blockIdx.x & 7;
+  const uint32_t u = (uint32_t)((uint64_t)units * xcd / 8) + (blockIdx.x >> 3);
+  if (u >= (uint32_t)((uint64_t)units * (xcd + 1) / 8)) return;
+  uint32_t slot;
   int ct, rt = 0;
   if constexpr (OP == GCN_GEMM_TN) {
-    const int tiles = a.col_tiles * a.row_tiles;
-    slot = (blockIdx.x & 7) * per_xcd + idx / tiles;
-    rt = (int)(idx % tiles) / a.col_tiles;
-    ct = (int)(idx % tiles) % a.col_tiles;
-    if (idx / tiles >= per_xcd) return;
+    slot = u / per_row;
+    rt = (int)(u % per_row) / a.col_tiles;
+    ct = (int)(u % per_row) % a.col_tiles;
   } else {
-    const int64_t band = idx / (4 * a.col_tiles), in = idx - band * 4 * a.col_tiles;
-    const int64_t of = std::min<int64_t>(4, per_xcd - 4 * band);  // slots of the band
-    if (of <= 0) return;
-    if (in >= of * a.col_tiles) return;
-    slot = (blockIdx.x & 7) * per_xcd + 4 * band + in % of;
+    const uint32_t band = u / (4 * per_row), in = u - band * 4 * per_row;
+    const uint32_t of = std::min(4u, rows - 4 * band);  // row tiles of the band
+    slot = 4 * band + in % of;
     ct = (int)(in / of);
   }
-  if (slot >= a.slots) return;
-  const GroupTile gt = group_tile(a.by, slot, OP == GCN_GEMM_TN ? (int)a.split : BM);
+  const GroupTile gt = counted ? counted_tile(a.by, (int)slot, R, LEAST, before)
+                               : group_tile(a.by, slot, R);
   int64_t k_beg = 0, k_end = a.K;
   Loader<AK, BM, BK, NT, DIRECT> la;
   Loader<BKC, BN, BK, NT, DIRECT> lb;
@@ -211,48 +239,86 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul(MulArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  auto stage = [&](int64_t k, const char* ca, const char* cb, char* na, char* nb) {
-    const bool more = k + BK < k_end;
-    if (more) {
-      la.load(na, k + BK, k_end - k - BK);
-      lb.load(nb, k + BK, k_end - k - BK);
-    }
+  // Fragments of a step are read while the step before it is multiplied; the first ones of
+  // the next stage too, so the one barrier of a stage stands before its last step: all
+  // have read the stage's last fragments then, and the next stage is in LDS.
+  constexpr int STEPS = BK / 16;
+  static_assert(STEPS % 2 == 0, "the fragments' buffers alternate over the stages");
+  bf8 fa[2][RB], fb[2][CB];
+  auto read = [&](int to, int step, const char* ca, const char* cb) {
 #pragma unroll
-    for (int st = 0; st < BK / 16; ++st) {
-      bf8 fa[RB], fb[CB];
+    for (int i = 0; i < RB; ++i) fa[to][i] = TA::read(ca, wr * RB + i, step, lane);
 #pragma unroll
-      for (int i = 0; i < RB; ++i) fa[i] = TA::read(ca, wr * RB + i, st, lane);
-#pragma unroll
-      for (int j = 0; j < CB; ++j) fb[j] = TB::read(cb, wc * CB + j, st, lane);
-#pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int j = 0; j < CB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-    }
-    if (more) {
-      la.store(na);
-      lb.store(nb);
-    }
-    wait_loads();
+    for (int j = 0; j < CB; ++j) fb[to][j] = TB::read(cb, wc * CB + j, step, lane);
   };
-  if (k_beg < k_end) {
-    la.load(a0, k_beg, k_end - k_beg);
-    lb.load(b0, k_beg, k_end - k_beg);
+  // One or two LDS reads between two products.
+  constexpr int READS = (AK ? 1 : 2) * RB + (BKC ? 1 : 2) * CB;
+  auto multiply = [&](int from) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+        acc[i][j] =
+            __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[from][i], fb[from][j], acc[i][j], 0, 0, 0);
+#pragma unroll
+    for (int p = 0; p < RB * CB; ++p) {
+      __builtin_amdgcn_sched_group_barrier(0x100, (READS + RB * CB - 1) / (RB * CB), 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    }
+  };
+  const int64_t stages = (k_end - k_beg + BK - 1) / BK;
+  auto load = [&](int64_t s, char* la_to, char* lb_to) {
+    const int64_t k = k_beg + s * BK;
+    la.load(la_to, k, k_end - k);
+    lb.load(lb_to, k, k_end - k);
+  };
+  // stage s has been read from (ca, cb): stage s + 1, in (na, nb) or on its way there, is waited
+  // for, and stage s + 2 goes to (ca, cb) (past the last one, zeros)
+  auto pass_on = [&](int64_t s, char* ca, char* cb, char* na, char* nb) {
+    la.store(na);
+    lb.store(nb);
+    wait_loads();
+    load(s + 2, ca, cb);
+  };
+  auto stage = [&](int64_t s, char* ca, char* cb, char* na, char* nb) {
+#pragma unroll
+    for (int st = 0; st + 1 < STEPS; ++st) {
+      read((st + 1) & 1, st + 1, ca, cb);
+      multiply(st & 1);
+    }
+    pass_on(s, ca, cb, na, nb);
+    read(0, 0, na, nb);
+    multiply((STEPS - 1) & 1);
+  };
+  if (stages > 0) {
+    load(0, a0, b0);
     la.store(a0);
     lb.store(b0);
     wait_loads();
-  }
-  for (int64_t k = k_beg; k < k_end; k += 2 * BK) {
-    stage(k, a0, b0, a1, b1);
-    if (k + BK < k_end) stage(k + BK, a1, b1, a0, b0);
+    load(1, a1, b1);
+    if (m0 + wr * RB * 32 >= m_end) {  // no rows for this wavefront: it brings its part only
+      for (int64_t s = 0; s < stages; s += 2) {
+        pass_on(s, a0, b0, a1, b1);
+        if (s + 1 < stages) pass_on(s + 1, a1, b1, a0, b0);
+      }
+      wait_loads();
+      return;
+    }
+    read(0, 0, a0, b0);
+    for (int64_t s = 0; s < stages; s += 2) {
+      stage(s, a0, b0, a1, b1);
+      if (s + 1 >= stages) break;
+      stage(s + 1, a1, b1, a0, b0);
+    }
+    wait_loads();  // those past the last stage
   }
 
   TC* C = static_cast<TC*>(a.C);
   int64_t ldc = a.ldc;
   if constexpr (OP == GCN_GEMM_TN) {
     if (gt.beg != gt.first) {
-      C = reinterpret_cast<TC*>(a.part) + (slot - gt.g - 1) * a.M * a.N;
+      C = reinterpret_cast<TC*>(a.part) +
+          (gt.first / a.split + (gt.beg - gt.first) / a.split - 1) * a.M * a.N;
       ldc = a.N;
     } else {
       C += gt.g * a.stride_c;
@@ -261,13 +327,34 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul(MulArgs a) {
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t r = m0 + (wr * RB + i) * 32 + (e & 3) + 8 * (e >> 2) + 4 * (lane >> 5);
-      TC* q = C + r * ldc;
+    for (int j = 0; j < CB; ++j) {
+      const int64_t r0 = m0 + (wr * RB + i) * 32 + 4 * (lane >> 5);
+      const int c0 = n0 + (wc * CB + j) * 32;
+      if constexpr (sizeof(TC) == 4) {
+        const int c = c0 + (lane & 31);
 #pragma unroll
-      for (int j = 0; j < CB; ++j) {
-        const int c = n0 + (wc * CB + j) * 32 + (lane & 31);
-        if (r < m_end && c < a.N) q[c] = from_float<TC>(acc[i][j][e]);
+        for (int e = 0; e < 16; ++e) {
+          const int64_t r = r0 + (e & 3) + 8 * (e >> 2);
+          if (r < m_end && c < a.N) C[r * ldc + c] = acc[i][j][e];
+        }
+      } else {
+        // 4 x 4 values of 4 lanes change places, so that a lane has 4 columns of a row (one
+        // 8-byte store instead of 4 of 2 bytes)
+        const int c = c0 + (lane & 28);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const int64_t r = r0 + (lane & 3) + 2 * e;
+          const u2 v = quad_rows(acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]);
+          if (r >= m_end) continue;
+          uint16_t* q = reinterpret_cast<uint16_t*>(C) + r * ldc + c;
+          if (c + 4 <= a.N && a.c_vec) {
+            *reinterpret_cast<u2*>(q) = v;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (c + k < a.N) q[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+          }
+        }
       }
     }
 }
@@ -277,9 +364,10 @@ gcn_status launch(MulArgs a, hipStream_t s) {
   constexpr int BM = 32 * WR * RB, BN = 32 * WC * CB;
   a.col_tiles = (int)ceil_div((int64_t)a.N, (int64_t)BN);
   a.row_tiles = OP == GCN_GEMM_TN ? (int)ceil_div((int64_t)a.M, (int64_t)BM) : 1;
-  a.slots = group_slots(a.by, OP == GCN_GEMM_TN ? a.split : BM);
-  const int64_t blocks = ceil_div(a.slots, (int64_t)8) * 8 * a.col_tiles * a.row_tiles;
+  const int64_t slots = group_slots(a.by, OP == GCN_GEMM_TN ? a.split : BM);
+  const int64_t blocks = ceil_div(slots * a.col_tiles * a.row_tiles, (int64_t)8) * 8;
   GCN_CHECK(launch_fits(blocks, 64 * WR * WC));
+  a.slots = (uint32_t)slots;
   hipLaunchKernelGGL((k_mul<OP, TC, DIRECT, BK, WR, WC, RB, CB>), dim3((unsigned)blocks),
                      dim3(64 * WR * WC), 0, s, a);
   GCN_HIP(hipGetLastError());
@@ -288,8 +376,8 @@ gcn_status launch(MulArgs a, hipStream_t s) {
 
 template <int OP, class TC, bool DIRECT>
 gcn_status mul(const MulArgs& a, hipStream_t s) {
-  if (a.N > 128 && a.by.rows / a.by.n >= 192)
-    return launch<OP, TC, DIRECT, 64, 2, 4, 4, 2>(a, s);
+  if constexpr (DIRECT)
+    if (a.N > 128 && a.by.rows / a.by.n >= 192) return launch<OP, TC, true, 64, 4, 2, 2, 4>(a, s);
   return launch<OP, TC, DIRECT, 64, 2, 2, 2, 2>(a, s);
 }
 
@@ -315,6 +403,7 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
   a.C = C;
   a.ldc = ldc;
   a.N = (int)N;
+  a.c_vec = c_bf16 && reinterpret_cast<uintptr_t>(C) % 8 == 0 && ldc % 4 == 0;
   const bool rows_ok = aligned16(A, lda) && aligned16(B, ldb);
   if (op == GCN_GEMM_TN) {
     a.M = (int)K;

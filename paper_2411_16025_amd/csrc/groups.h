@@ -56,6 +56,28 @@ __device__ inline int64_t group_offset(const Groups& a, int g) {
   return o < 0 ? 0 : (o > a.rows ? a.rows : o);
 }
 
+// Tiles of R rows of all groups, counted (each group at least `least` tiles). The whole wavefront.
+__device__ inline int group_tiles_of(const Groups& a, int g, int R, int least) {
+  const int64_t rows = group_offset(a, g + 1) - group_offset(a, g);
+  const int tiles = rows > 0 ? (int)((rows + R - 1) / R) : 0;
+  return tiles > least ? tiles : least;
+}
+
+// With up to this many groups a workgroup counts the tiles before its own, so that no
+// slots are empty and the tiles divide evenly among the XCDs (32,768 x 4096 x 2048, one
+// group: 129 slots for 128 tiles, 537 us in runs of slots, 496 so); of more groups the
+// slots' search reads less.
+constexpr int kCountedGroups = 1024;
+
+__device__ inline int wave_inclusive(int v) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int u = __shfl_up(v, off, 64);
+    if ((int)(threadIdx.x & 63) >= off) v += u;
+  }
+  return v;
+}
+
 // A tile's group and rows; beg >= end: nothing (first: the group's first tile).
 struct GroupTile {
   int g;
@@ -82,6 +104,41 @@ __device__ inline GroupTile group_tile(const Groups& a, int64_t slot, int R) {
   const int64_t tile = slot - (t.first / R + t.g);
   t.beg = tile < 0 ? t.end : t.first + tile * R;
   return t;
+}
+
+// The number of tiles; before: of the groups before this lane's (a.n / 64 of them, rounded up).
+__device__ inline int group_tiles(const Groups& a, int R, int least, int* before) {
+  const int per = (a.n + 63) / 64, lane = threadIdx.x & 63;
+  int mine = 0;
+  for (int i = 0; i < per; ++i)
+    if (lane * per + i < a.n) mine += group_tiles_of(a, lane * per + i, R, least);
+  const int upto = wave_inclusive(mine);
+  *before = upto - mine;
+  return __builtin_amdgcn_readlane(upto, 63);
+}
+
+// Tile t of the counted ones.
+__device__ inline GroupTile counted_tile(const Groups& a, int t, int R, int least, int before) {
+  const int per = (a.n + 63) / 64, lane = threadIdx.x & 63;
+  // the last lane whose groups begin at or before t (those of the lanes behind it begin later)
+  const uint64_t at = __ballot(lane * per < a.n && before <= t);
+  const int l = 63 - __clzll((long long)at);
+  t -= __builtin_amdgcn_readlane(before, l);
+  int g = l * per;
+  if (per > 1) {
+    const int mine = lane < per && g + lane < a.n ? group_tiles_of(a, g + lane, R, least) : 0;
+    const int first = wave_inclusive(mine) - mine;
+    const uint64_t in = __ballot(mine > 0 && first <= t);
+    const int j = in ? 63 - __clzll((long long)in) : 0;
+    t -= __builtin_amdgcn_readlane(first, j);
+    g += j;
+  }
+  GroupTile r;
+  r.g = __builtin_amdgcn_readfirstlane(g);
+  r.first = group_offset(a, r.g);
+  r.end = group_offset(a, r.g + 1);
+  r.beg = r.first + (int64_t)t * R;
+  return r;
 }
 #endif
 
