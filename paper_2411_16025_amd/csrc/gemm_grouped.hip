@@ -408,7 +408,12 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
   if (op == GCN_GEMM_TN) {
     a.M = (int)K;
     a.stride_c = stride_w;
-    a.split = 2048;
+    // Chunks of 256 to 2048 rows: about 512 workgroups of 256 x 256 of C where there are few
+    // groups; with many groups a chunk is a bound on the work of one.
+    const int64_t tiles = ceil_div(K, (int64_t)256) * ceil_div(N, (int64_t)256);
+    a.split = std::min<int64_t>(
+        2048, std::max<int64_t>(256, ceil_div(ceil_div(g.rows * tiles, (int64_t)512), (int64_t)64) * 64));
+    if (g.n * tiles >= 512) a.split = 2048;
     TempScope temps(s);
     const int64_t parts = g.rows / a.split;
     if (parts > 0) GCN_CHECK(temps.alloc(&a.part, parts * K * N, "grouped GEMM partials"));

@@ -104,18 +104,21 @@ gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
   return GCN_OK;
 }
 
-// One element per thread and step: the partial sums behind C's own in chunk order.
+// Partial sum p (blockIdx.y) belongs to the last group that begins in chunk p of all rows or
+// before it, if that has so many: a group of several chunks reaches the next multiple of
+// `split`. The workgroups of a group's partial sums share its elements, each element
+// the sum of all of them in chunk order.
 __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t split, int64_t K,
-                                                         int64_t N, const float* part, float* C,
+                                                         int64_t N, int64_t p, const float* part, float* C,
                                                          int64_t ldc, int64_t stride_w) {
-  const int g = blockIdx.y;
-  const int64_t beg = group_offset(by, g), rows = group_offset(by, g + 1) - beg;
-  const int64_t more = (rows + split - 1) / split - 1;
-  if (more <= 0) return;
-  part += beg / split * K * N;
-  C += g * stride_w;
-  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < K * N;
-       t += (int64_t)gridDim.x * kThreads) {
+  p += blockIdx.y;
+  const GroupTile gt = group_tile_from(by, [&](int g) { return group_offset(by, g) / split <= p; });
+  const int64_t p0 = gt.first / split, more = (gt.end - gt.first + split - 1) / split - 1;
+  if (p < p0 || p >= p0 + more) return;
+  part += p0 * K * N;
+  C += gt.g * stride_w;
+  for (int64_t t = ((p - p0) * gridDim.x + blockIdx.x) * kThreads + threadIdx.x; t < K * N;
+       t += more * gridDim.x * kThreads) {
     float* c = C + t / N * ldc + t % N;
     float s = *c;
     for (int64_t j = 0; j < more; ++j) s += part[j * K * N + t];
@@ -128,10 +131,14 @@ __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t spli
 gcn_status sum_group_partials(const Groups& g, int64_t split, int64_t K, int64_t N,
                               const float* part, float* C, int64_t ldc, int64_t stride_w,
                               hipStream_t stream) {
-  const int64_t blocks = std::min<int64_t>(ceil_div(K * N, (int64_t)kThreads), 4096);
-  hipLaunchKernelGGL(k_group_sums, dim3((unsigned)blocks, (unsigned)g.n), dim3(kThreads), 0, stream,
-                     g, split, K, N, part, C, ldc, stride_w);
-  GCN_HIP(hipGetLastError());
+  const int64_t parts = g.rows / split;
+  const int64_t blocks = std::min(ceil_div(K * N, (int64_t)kThreads),
+                                  std::max<int64_t>(16, ceil_div(4096, parts)));
+  for (int64_t p = 0; p < parts; p += 65535) {  // (a grid's second axis)
+    hipLaunchKernelGGL(k_group_sums, dim3((unsigned)blocks, (unsigned)std::min<int64_t>(parts - p, 65535)),
+                       dim3(kThreads), 0, stream, g, split, K, N, p, part, C, ldc, stride_w);
+    GCN_HIP(hipGetLastError());
+  }
   return GCN_OK;
 }
 

@@ -84,23 +84,29 @@ struct GroupTile {
   int64_t beg, end, first;  // the tile's first row, the group's end, the group's first row
 };
 
-// The last group whose slots begin at or before `slot` (0 if none does): every
-// lane of the wavefront compares one group of the range left.
-__device__ inline GroupTile group_tile(const Groups& a, int64_t slot, int R) {
+// The last group that begins (begins(g), true up to some group) and its rows, beg = first:
+// every lane of the wavefront asks for one group of the range left.
+template <class Begins>
+__device__ inline GroupTile group_tile_from(const Groups& a, Begins begins) {
   int lo = 0, len = a.n;
   while (len > 1) {
     const int step = (len + 63) / 64;
     const int g = lo + (int)(threadIdx.x & 63) * step;
-    const bool at = g < lo + len && group_offset(a, g) / R + g <= slot;
-    const uint64_t hit = __ballot(at);
+    const uint64_t hit = __ballot(g < lo + len && begins(g));
     const int last = hit ? 63 - __clzll((long long)hit) : 0;
+    len = min(step, len - last * step);
     lo += last * step;
-    len = min(step, a.n - lo);
   }
   GroupTile t;
   t.g = __builtin_amdgcn_readfirstlane(lo);
-  t.first = group_offset(a, t.g);
+  t.beg = t.first = group_offset(a, t.g);
   t.end = group_offset(a, t.g + 1);
+  return t;
+}
+
+// The tile of a slot.
+__device__ inline GroupTile group_tile(const Groups& a, int64_t slot, int R) {
+  GroupTile t = group_tile_from(a, [&](int g) { return group_offset(a, g) / R + g <= slot; });
   const int64_t tile = slot - (t.first / R + t.g);
   t.beg = tile < 0 ? t.end : t.first + tile * R;
   return t;
