@@ -45,6 +45,18 @@ __device__ inline void drop_words(const Drop& d, uint64_t call, uint32_t row, ui
   w[3] = c3;
 }
 
+// Columns f .. f + N - 1 of a row (f and N multiples of 4).
+template <int N>
+__device__ inline void drop_piece(const Drop& d, uint64_t call, uint32_t row, int f, float (&v)[N]) {
+#pragma unroll
+  for (int b = 0; b < N; b += 4) {
+    uint32_t w[4];
+    drop_words(d, call, row, (uint32_t)(f + b) / 4, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[b + e] = w[e] >= d.least ? v[b + e] * d.scale : 0.f;
+  }
+}
+
 __device__ inline uint64_t drop_call(const Drop& d) { return d.call + (d.step ? *d.step : 0); }
 #endif
 

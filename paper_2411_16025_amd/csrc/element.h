@@ -18,6 +18,75 @@ __device__ inline T from_float(float v) {
   return (T)v;
 }
 
+// Pieces of 16 bytes, at any element.
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+template <class T>
+constexpr int kPiece = 16 / (int)sizeof(T);
+
+template <class T>
+struct Unaligned {
+  typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Unaligned<bf16> {
+  typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
+};
+
+// The piece at column f of a row of F; zeros behind its end.
+template <class T>
+__device__ inline u4 load_piece(const T* row, int f, int F) {
+  if (f + kPiece<T> <= F) return *reinterpret_cast<const typename Unaligned<T>::type*>(row + f);
+  u4 r = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < kPiece<T> - 1; ++e)
+    if (f + e < F) {
+      if constexpr (sizeof(T) == 4)
+        r[e] = reinterpret_cast<const uint32_t*>(row)[f + e];
+      else
+        r[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[f + e] << (16 * (e & 1));
+    }
+  return r;
+}
+
+template <class T>
+__device__ inline void unpack(u4 r, float (&v)[kPiece<T>]) {
+#pragma unroll
+  for (int e = 0; e < kPiece<T>; ++e) {
+    if constexpr (sizeof(T) == 4)
+      v[e] = __uint_as_float(r[e]);
+    else
+      v[e] = __uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16);
+  }
+}
+
+// The part inside the row; each value rounded to nearest even.
+template <class T>
+__device__ inline void store_piece(T* row, int f, int F, const float (&v)[kPiece<T>]) {
+  u4 r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 4) {
+      r[e] = __float_as_uint(v[e]);
+    } else {
+      typedef float f2 __attribute__((ext_vector_type(2)));
+      typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+      r[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{v[2 * e], v[2 * e + 1]}), bf2));
+    }
+  }
+  if (f + kPiece<T> <= F) {
+    *reinterpret_cast<typename Unaligned<T>::type*>(row + f) = r;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < kPiece<T> - 1; ++e)
+    if (f + e < F) {
+      if constexpr (sizeof(T) == 4)
+        reinterpret_cast<uint32_t*>(row)[f + e] = r[e];
+      else
+        reinterpret_cast<uint16_t*>(row)[f + e] = (uint16_t)(r[e / 2] >> (16 * (e & 1)));
+    }
+}
+
 // n rows of F columns of a known type.
 inline gcn_status check_rows(int64_t n, int64_t F, int dtype) {
   if (n < 0 || F <= 0 || F >= (int64_t(1) << 31) ||

@@ -14,7 +14,6 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef float f16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4u __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
 
 #define GCN_GLOBAL __attribute__((address_space(1)))

@@ -1,15 +1,14 @@
 // Row LayerNorm with weights and the dropout behind it, forward and backward.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dropout.h"
 #include "element.h"
+#include "lanes.h"
 
 namespace gcn {
 namespace {
-
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 
 struct NormArgs {
   int64_t n;
@@ -23,45 +22,274 @@ struct NormArgs {
   int64_t lddy;
   void* out;  // Y or dX
   int64_t ldo;
+  float *dgamma, *dbeta;  // of a single workgroup; else part [workgroups][2][F]
+  float* part;
 };
 
-// Sum over the workgroup (every thread gets it).
+// The mean as the sum of two floats: d = (x - hi) - lo loses nothing where the mean is far from 0.
+struct Mean {
+  float hi, lo;
+  __device__ inline explicit Mean(double mean)
+      : hi((float)mean), lo((float)(mean - (double)(float)mean)) {}
+  __device__ inline float from(float x) const { return (x - hi) - lo; }
+};
+
+// ---- rows in registers -----------------------------------------------------------
+//
+// G lanes hold a row (a part of a wavefront, or a workgroup of G threads), each NV
+// pieces of 16 bytes, piece j of lane l at column (l + j G) V, V elements to a piece;
+// memory is read once and written once. A workgroup walks its rows, the next one's
+// pieces in flight while it works on one, and keeps the weights (and, backward, its
+// sums of their gradients) in registers meanwhile. Sums of the statistics in double:
+// they cost two operations per element more than fp32 and have the whole range of x^2.
+
+constexpr int threads_of(int G) { return G > 256 ? G : 256; }  // of a workgroup
+
+template <class T, int G, int NV>
+struct Rows {
+  static constexpr int V = kPiece<T>, NT = threads_of(G), kSlots = NT / G;
+  static constexpr int kWaves = NT / 64;
+
+  // Sum over the row's lanes (every lane gets it; `red`: NT / 64 values of LDS).
+  template <class S>
+  __device__ static inline S sum(S v, S* red) {
+    if constexpr (G <= 64) {
+      return slot_sum<G>(v);
+    } else {
+      v = slot_sum<64>(v);
+      __syncthreads();  // the sums before have been read
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = red[0];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v += red[w];
+      return v;
+    }
+  }
+  __device__ static inline int column(int j) { return ((int)(threadIdx.x % G) + j * G) * V; }
+  __device__ static inline void load(u4 (&r)[NV], const void* x, int64_t ld, int64_t i, int64_t n,
+                                     int F) {
+    const T* row = static_cast<const T*>(x) + i * ld;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) r[j] = load_piece(row, column(j), i < n ? F : 0);
+  }
+  __device__ static inline void weights(float (&w)[NV][V], const float* from, float none, int F) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        w[j][e] = from && column(j) + e < F ? from[column(j) + e] : none;
+  }
+  // x becomes x - mean (0 behind the row); 1 / sqrt(var + eps).
+  __device__ static inline float center(float (&x)[NV][V], int F, double eps, double* red) {
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s += (double)x[j][e];  // 0 behind the row
+    const Mean mean(sum(s, red) / (double)F);
+    double q = 0.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x[j][e] = column(j) + e < F ? mean.from(x[j][e]) : 0.f;
+        q = __builtin_fma((double)x[j][e], (double)x[j][e], q);
+      }
+    return (float)inv_sqrt(sum(q, red) / (double)F + eps);
+  }
+};
+
+template <class T, int G, int NV, bool DROP>
+__global__ __launch_bounds__(threads_of(G)) void k_norm_fwd(NormArgs a) {
+  using R = Rows<T, G, NV>;
+  constexpr int V = R::V;
+  __shared__ double red[R::kWaves];
+  const uint64_t call = DROP ? drop_call(a.drop) : 0;
+  float gamma[NV][V], beta[NV][V];
+  R::weights(gamma, a.gamma, 1.f, a.F);
+  R::weights(beta, a.beta, 0.f, a.F);
+  const int64_t step = (int64_t)gridDim.x * R::kSlots;
+  int64_t i = (int64_t)blockIdx.x * R::kSlots + threadIdx.x / G;
+  u4 raw[NV];
+  R::load(raw, a.x, a.ldx, i, a.n, a.F);
+  // rows [i - threadIdx.x / G, + kSlots) of the workgroup: all its threads stay while one has a row
+  for (int64_t first = (int64_t)blockIdx.x * R::kSlots; first < a.n; first += step, i += step) {
+    float x[NV][V];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) unpack<T>(raw[j], x[j]);
+    R::load(raw, a.x, a.ldx, i + step, a.n, a.F);
+    const float rstd = R::center(x, a.F, a.eps, red);
+    if (i >= a.n) continue;
+    T* y = static_cast<T*>(a.out) + i * a.ldo;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        x[j][e] = __builtin_fmaf(x[j][e] * rstd, gamma[j][e], beta[j][e]);
+      if (DROP) drop_piece<V>(a.drop, call, (uint32_t)i, R::column(j), x[j]);
+      store_piece<T>(y, R::column(j), a.F, x[j]);
+    }
+  }
+}
+
+// WANT_X: dX; WANT_W: dgamma and dbeta.
+template <class T, int G, int NV, bool DROP, bool WANT_X, bool WANT_W>
+__global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
+  using R = Rows<T, G, NV>;
+  constexpr int V = R::V;
+  __shared__ double red[R::kWaves];
+  __shared__ float2 red2[R::kWaves];
+  const uint64_t call = DROP ? drop_call(a.drop) : 0;
+  float gamma[NV][V], sg[NV][V] = {}, sb[NV][V] = {};
+  R::weights(gamma, a.gamma, 1.f, a.F);
+  const int64_t step = (int64_t)gridDim.x * R::kSlots;
+  int64_t i = (int64_t)blockIdx.x * R::kSlots + threadIdx.x / G;
+  u4 rx[NV], rg[NV];
+  R::load(rx, a.x, a.ldx, i, a.n, a.F);
+  R::load(rg, a.dy, a.lddy, i, a.n, a.F);
+  for (int64_t first = (int64_t)blockIdx.x * R::kSlots; first < a.n; first += step, i += step) {
+    float x[NV][V], g[NV][V];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      unpack<T>(rx[j], x[j]);
+      unpack<T>(rg[j], g[j]);
+    }
+    R::load(rx, a.x, a.ldx, i + step, a.n, a.F);
+    R::load(rg, a.dy, a.lddy, i + step, a.n, a.F);
+    const float rstd = R::center(x, a.F, a.eps, red);
+    float s1 = 0.f, s2 = 0.f;
+    const bool live = i < a.n;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (DROP) drop_piece<V>(a.drop, call, (uint32_t)i, R::column(j), g[j]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x[j][e] *= rstd;  // H
+        if (WANT_W) {
+          sg[j][e] = __builtin_fmaf(g[j][e], x[j][e], sg[j][e]);
+          sb[j][e] += g[j][e];
+        }
+        if (WANT_X) {
+          g[j][e] *= gamma[j][e];  // T
+          s1 += g[j][e];
+          s2 = __builtin_fmaf(g[j][e], x[j][e], s2);
+        }
+      }
+    }
+    if constexpr (WANT_X) {
+      float m1, m2;
+      if constexpr (G <= 64) {
+        m1 = slot_sum<G>(s1) / (float)a.F;
+        m2 = slot_sum<G>(s2) / (float)a.F;
+      } else {
+        s1 = slot_sum<64>(s1);
+        s2 = slot_sum<64>(s2);
+        if ((threadIdx.x & 63) == 0) red2[threadIdx.x >> 6] = make_float2(s1, s2);
+        __syncthreads();  // (read before the next row's sums, which have barriers of their own)
+        s1 = s2 = 0.f;
+#pragma unroll
+        for (int w = 0; w < R::kWaves; ++w) {
+          s1 += red2[w].x;
+          s2 += red2[w].y;
+        }
+        m1 = s1 / (float)a.F;
+        m2 = s2 / (float)a.F;
+      }
+      if (live) {
+        T* dx = static_cast<T*>(a.out) + i * a.ldo;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            g[j][e] = rstd * (g[j][e] - m1 - x[j][e] * m2);
+          store_piece<T>(dx, R::column(j), a.F, g[j]);
+        }
+      }
+    }
+  }
+  if constexpr (WANT_W) {
+    // the workgroup's sums: over the slots of a wavefront, then over the wavefronts
+    constexpr int W = G < 64 ? R::kWaves : R::kWaves * 64 / (G < 64 ? 64 : G);  // to add in LDS
+    __shared__ float sums[W > 1 ? W - 1 : 1][G * NV * V];
+    float* out_g = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.F : a.dgamma;
+    float* out_b = a.part ? out_g + a.F : a.dbeta;
+    auto finish = [&](float (&s)[NV][V], float* out) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+#pragma unroll
+          for (int off = G; off < 64; off *= 2) s[j][e] += __shfl_xor(s[j][e], off, 64);
+        }
+      const int w = (int)threadIdx.x / (G < 64 ? 64 : G);
+      const bool mine = (int)threadIdx.x % (G < 64 ? 64 : G) < G;
+      if constexpr (W > 1) {
+        __syncthreads();
+        if (w > 0 && mine)
+#pragma unroll
+          for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sums[w - 1][R::column(j) + e] = s[j][e];
+        __syncthreads();
+      }
+      if (w > 0 || !mine || !out) return;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int f = R::column(j) + e;
+          float v = s[j][e];
+          if constexpr (W > 1)
+#pragma unroll
+            for (int k = 0; k < W - 1; ++k) v += sums[k][f];
+          if (f < a.F) out[f] = v;
+        }
+    };
+    finish(sg, out_g);
+    finish(sb, out_b);
+  }
+}
+
+// ---- rows of any length ------------------------------------------------------------
+//
+// A workgroup walks the row, three times forward (the second and third time from the
+// caches) and four times backward.
+
+constexpr int kThreads = 256;
+
 template <class V>
 __device__ inline V block_sum(V v) {
-  __shared__ V part[kWaves];
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) v += __shfl_xor(v, off, 64);
+  __shared__ V part[kThreads / 64];
+  v = slot_sum<64>(v);
   __syncthreads();  // the values of the sum before have been read
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
   __syncthreads();
   v = part[0];
-  for (int w = 1; w < kWaves; ++w) v += part[w];
+  for (int w = 1; w < kThreads / 64; ++w) v += part[w];
   return v;
 }
 
-// mean as the sum of two floats (h = ((x - hi) - lo) rstd loses nothing where the
-// mean is far from 0), and 1 / sqrt(var + eps).
+// The row's mean and 1 / sqrt(var + eps).
 struct Stats {
-  float hi, lo, rstd;
-  __device__ inline float norm(float x) const { return ((x - hi) - lo) * rstd; }
+  Mean mean;
+  float rstd;
+  __device__ inline float norm(float x) const { return mean.from(x) * rstd; }
 };
 
 template <class T>
 __device__ inline Stats row_stats(const T* x, int F, double eps) {
   double s = 0.0;
   for (int f = threadIdx.x; f < F; f += kThreads) s += (double)to_float(x[f]);
-  const double mean = block_sum(s) / (double)F;
+  const Mean mean(block_sum(s) / (double)F);
   double q = 0.0;
   for (int f = threadIdx.x; f < F; f += kThreads) {
-    const double d = (double)to_float(x[f]) - mean;
-    q += d * d;
+    const double d = (double)mean.from(to_float(x[f]));
+    q = __builtin_fma(d, d, q);
   }
-  const double var = block_sum(q) / (double)F;
-  const float hi = (float)mean;
-  return Stats{hi, (float)(mean - (double)hi), (float)(1.0 / sqrt(var + eps))};
+  return Stats{mean, (float)inv_sqrt(block_sum(q) / (double)F + eps)};
 }
 
-// The factor of element (i, f): scale where it is kept, else 0.
 __device__ inline bool kept(const Drop& d, uint64_t call, int64_t i, int f) {
   uint32_t w[4];
   drop_words(d, call, (uint32_t)i, (uint32_t)f >> 2, w);
@@ -69,7 +297,7 @@ __device__ inline bool kept(const Drop& d, uint64_t call, int64_t i, int f) {
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_norm_fwd(NormArgs a) {
+__global__ __launch_bounds__(kThreads) void k_norm_fwd_long(NormArgs a) {
   const uint64_t call = drop_call(a.drop);
   for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + i * a.ldx;
@@ -83,14 +311,12 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(NormArgs a) {
   }
 }
 
-// A workgroup's rows: i = blockIdx.x, + gridDim.x, ...; part [gridDim.x][2][F]
-// gets its sums of G H and G.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a, float* part) {
+__global__ __launch_bounds__(kThreads) void k_norm_bwd_long(NormArgs a) {
   const uint64_t call = drop_call(a.drop);
-  float* pg = part + (int64_t)blockIdx.x * 2 * a.F;
+  float* pg = a.part + (int64_t)blockIdx.x * 2 * a.F;
   float* pb = pg + a.F;
-  if (part)
+  if (a.part)
     for (int f = threadIdx.x; f < a.F; f += kThreads) pg[f] = pb[f] = 0.f;
   for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + i * a.ldx;
@@ -104,9 +330,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a, float* part) 
     for (int f = threadIdx.x; f < a.F; f += kThreads) {
       const float g = g_at(f), h = st.norm(to_float(x[f])), t = a.gamma ? g * a.gamma[f] : g;
       s1 += t;
-      s2 += t * h;
-      if (part) {
-        pg[f] += g * h;
+      s2 = __builtin_fmaf(t, h, s2);
+      if (a.part) {
+        pg[f] = __builtin_fmaf(g, h, pg[f]);
         pb[f] += g;
       }
     }
@@ -119,47 +345,120 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a, float* part) 
   }
 }
 
-// dgamma and dbeta: the sums of the workgroups' partial rows, in their order.
-__global__ __launch_bounds__(kThreads) void k_norm_sums(int64_t blocks, int F, const float* part,
-                                                        float* dgamma, float* dbeta) {
-  const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (c >= 2 * (int64_t)F) return;
-  float* out = c < F ? dgamma : dbeta;
-  if (!out) return;
+// dgamma and dbeta from the workgroups' rows of sums: 64 columns by 16 wavefronts, each of which
+// adds every sixteenth row in double, then the sixteen sums in turn.
+__global__ __launch_bounds__(1024) void k_norm_sums(int64_t blocks, int F, const float* part,
+                                                    float* dgamma, float* dbeta) {
+  __shared__ double sums[16][64];
+  const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int w = threadIdx.x >> 6;
   double s = 0.0;
-  for (int64_t b = 0; b < blocks; ++b) s += (double)part[b * 2 * F + c];
-  out[c < F ? c : c - F] = (float)s;
+  if (c < 2 * (int64_t)F)
+#pragma unroll 8
+    for (int64_t b = w; b < blocks; b += 16) s += (double)part[b * 2 * F + c];
+  sums[w][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (w > 0 || c >= 2 * (int64_t)F) return;
+  for (int k = 1; k < 16; ++k) s += sums[k][threadIdx.x & 63];
+  float* out = c < F ? dgamma : dbeta;
+  if (out) out[c < F ? c : c - F] = (float)s;
 }
 
-constexpr int64_t kRowBlocks = 2048;
+// ---- launch ----------------------------------------------------------------------
+
+// Longer rows do not fit the registers of 1024 threads (backward, with the sums, 512).
+constexpr int kLongestFwd = 16384, kLongestBwd = 8192;
+
+// The shape for rows of F elements: lanes that hold a row in 4 to 16 elements of each.
+template <class T, class Do>
+gcn_status with_shape(int F, Do go) {
+  constexpr int P = 16 / kPiece<T>;  // pieces of 16 elements
+  using std::integral_constant;
+  if (F <= 8 * kPiece<T>) return go(integral_constant<int, 8>(), integral_constant<int, 1>());
+  if (F <= 64) return go(integral_constant<int, 8>(), integral_constant<int, P / 2>());
+  if (F <= 128) return go(integral_constant<int, 8>(), integral_constant<int, P>());
+  if (F <= 256) return go(integral_constant<int, 16>(), integral_constant<int, P>());
+  if (F <= 512) return go(integral_constant<int, 32>(), integral_constant<int, P>());
+  if (F <= 1024) return go(integral_constant<int, 64>(), integral_constant<int, P>());
+  if (F <= 2048) return go(integral_constant<int, 256>(), integral_constant<int, P / 2>());
+  if (F <= 4096) return go(integral_constant<int, 256>(), integral_constant<int, P>());
+  return go(integral_constant<int, 512>(), integral_constant<int, P>());
+}
 
 template <class T>
-gcn_status norm_fwd(const NormArgs& a, hipStream_t s) {
+gcn_status norm_fwd(const NormArgs& a, bool drop, hipStream_t s) {
   ProfScope ps("layernorm_affine_fwd", s);
-  hipLaunchKernelGGL(k_norm_fwd<T>, dim3((unsigned)std::min(a.n, 8 * kRowBlocks)), dim3(kThreads),
-                     0, s, a);
+  if (a.F > kLongestFwd) {
+    hipLaunchKernelGGL(k_norm_fwd_long<T>, dim3((unsigned)std::min<int64_t>(a.n, 4096)),
+                       dim3(kThreads), 0, s, a);
+    GCN_HIP(hipGetLastError());
+    return GCN_OK;
+  }
+  auto run = [&](auto g, auto nv) {
+    constexpr int G = decltype(g)::value, NV = decltype(nv)::value;
+    using R = Rows<T, G, NV>;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.n, (int64_t)R::kSlots), 2048));
+    if (drop)
+      hipLaunchKernelGGL((k_norm_fwd<T, G, NV, true>), grid, dim3(R::NT), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_norm_fwd<T, G, NV, false>), grid, dim3(R::NT), 0, s, a);
+    GCN_HIP(hipGetLastError());
+    return GCN_OK;
+  };
+  if (a.F > 8192)
+    return run(std::integral_constant<int, 1024>(), std::integral_constant<int, 16 / kPiece<T>>());
+  return with_shape<T>(a.F, run);
+}
+
+gcn_status norm_sums(const NormArgs& a, int64_t blocks, hipStream_t s) {
+  hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)ceil_div(2 * (int64_t)a.F, (int64_t)64)),
+                     dim3(1024), 0, s, blocks, a.F, (const float*)a.part, a.dgamma, a.dbeta);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }
 
 template <class T>
-gcn_status norm_bwd(const NormArgs& a, float* dgamma, float* dbeta, hipStream_t s) {
+gcn_status norm_bwd(NormArgs a, bool drop, hipStream_t s) {
   ProfScope ps("layernorm_affine_bwd", s);
   TempScope temps(s);
-  const int64_t blocks = std::min(a.n, kRowBlocks);
-  float* part = nullptr;
-  if ((dgamma || dbeta) && blocks > 0)
-    GCN_CHECK(temps.alloc(&part, blocks * 2 * a.F, "sums of the weights' gradients"));
-  if (blocks > 0) {
-    hipLaunchKernelGGL(k_norm_bwd<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, part);
+  const bool want_w = a.dgamma || a.dbeta;
+  if (a.n == 0) return want_w ? norm_sums(a, 0, s) : GCN_OK;
+  // workgroups: rows of sums of at most 16 MiB in all
+  const int64_t most =
+      std::min<int64_t>(2048, std::max<int64_t>(512, (int64_t(1) << 21) / a.F));
+  if (a.F > kLongestBwd) {
+    const int64_t blocks = std::min(a.n, most);
+    if (want_w) GCN_CHECK(temps.alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients"));
+    hipLaunchKernelGGL(k_norm_bwd_long<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
     GCN_HIP(hipGetLastError());
+    return want_w ? norm_sums(a, blocks, s) : GCN_OK;
   }
-  if (dgamma || dbeta) {
-    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)ceil_div(2 * (int64_t)a.F, (int64_t)kThreads)),
-                       dim3(kThreads), 0, s, blocks, a.F, (const float*)part, dgamma, dbeta);
+  return with_shape<T>(a.F, [&](auto g, auto nv) {
+    constexpr int G = decltype(g)::value, NV = decltype(nv)::value;
+    using R = Rows<T, G, NV>;
+    // four rows and more to a slot: with one workgroup the sums are the results
+    const int64_t blocks =
+        want_w ? std::min(ceil_div(a.n, (int64_t)4 * R::kSlots), most)
+               : std::min<int64_t>(ceil_div(a.n, (int64_t)R::kSlots), 2048);
+    if (want_w && blocks > 1)
+      GCN_CHECK(temps.alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients"));
+    auto run = [&](auto d) {
+      constexpr bool D = decltype(d)::value;
+      const dim3 grid((unsigned)blocks), threads(R::NT);
+      if (!want_w)
+        hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, true, false>), grid, threads, 0, s, a);
+      else if (a.out)
+        hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, true, true>), grid, threads, 0, s, a);
+      else
+        hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, false, true>), grid, threads, 0, s, a);
+    };
+    if (drop)
+      run(std::true_type());
+    else
+      run(std::false_type());
     GCN_HIP(hipGetLastError());
-  }
-  return GCN_OK;
+    return want_w && blocks > 1 ? norm_sums(a, blocks, s) : GCN_OK;
+  });
 }
 
 gcn_status check_eps(double eps) {
@@ -180,7 +479,7 @@ extern "C" gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void*
   clear_error();
   GCN_CHECK(check_rows(n, F, dtype));
   GCN_CHECK(check_eps(eps));
-  NormArgs a{n, (int)F, X, ldx, gamma, beta, eps, {}, nullptr, 0, Y, ldy};
+  NormArgs a{n, (int)F, X, ldx, gamma, beta, eps, {}, nullptr, 0, Y, ldy, nullptr, nullptr, nullptr};
   GCN_CHECK(make_drop(drop, n, &a.drop));
   if (n == 0) return GCN_OK;
   if (!X || !Y || ldx < F || ldy < F || (X == Y && ldx != ldy)) {
@@ -188,7 +487,8 @@ extern "C" gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void*
     return GCN_EINVAL;
   }
   hipStream_t s = (hipStream_t)stream;
-  return dtype == GCN_DT_F32 ? norm_fwd<float>(a, s) : norm_fwd<bf16>(a, s);
+  const bool on = a.drop.least > 0;
+  return dtype == GCN_DT_F32 ? norm_fwd<float>(a, on, s) : norm_fwd<bf16>(a, on, s);
 }
 
 extern "C" gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t ldx,
@@ -200,7 +500,7 @@ extern "C" gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void*
   CallScope scope(stream);
   GCN_CHECK(check_rows(n, F, dtype));
   GCN_CHECK(check_eps(eps));
-  NormArgs a{n, (int)F, X, ldx, gamma, nullptr, eps, {}, dY, lddy, dX, lddx};
+  NormArgs a{n, (int)F, X, ldx, gamma, nullptr, eps, {}, dY, lddy, dX, lddx, dgamma, dbeta, nullptr};
   GCN_CHECK(make_drop(drop, n, &a.drop));
   if (n > 0 && (!X || !dY || ldx < F || lddy < F || (dX && lddx < F) ||
                 (dX == X && lddx != ldx) || (dX == dY && lddx != lddy))) {
@@ -213,6 +513,6 @@ extern "C" gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void*
     return GCN_EINVAL;
   }
   hipStream_t s = (hipStream_t)stream;
-  return dtype == GCN_DT_F32 ? norm_bwd<float>(a, dgamma, dbeta, s)
-                             : norm_bwd<bf16>(a, dgamma, dbeta, s);
+  const bool on = a.drop.least > 0;
+  return dtype == GCN_DT_F32 ? norm_bwd<float>(a, on, s) : norm_bwd<bf16>(a, on, s);
 }
