@@ -50,14 +50,14 @@ struct Rows {
   static constexpr int V = kPiece<T>, NT = threads_of(G), kSlots = NT / G;
   static constexpr int kWaves = NT / 64;
 
-  // Sum over the row's lanes (every lane gets it; `red`: NT / 64 values of LDS).
+  // Sum over the row's lanes (every lane gets it). `red`: LDS that the sum two before this one
+  // used, so that one barrier is enough.
   template <class S>
   __device__ static inline S sum(S v, S* red) {
     if constexpr (G <= 64) {
       return slot_sum<G>(v);
     } else {
       v = slot_sum<64>(v);
-      __syncthreads();  // the sums before have been read
       if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
       __syncthreads();
       v = red[0];
@@ -77,17 +77,21 @@ struct Rows {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        w[j][e] = from && column(j) + e < F ? from[column(j) + e] : none;
+      for (int e = 0; e < V; e += 4) {
+        const u4 r = from ? load_piece(from, column(j) + e, F) : u4(__float_as_uint(none));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[j][e + k] = __uint_as_float(r[k]);
+      }
   }
   // x becomes x - mean (0 behind the row); 1 / sqrt(var + eps).
-  __device__ static inline float center(float (&x)[NV][V], int F, double eps, double* red) {
+  __device__ static inline float center(float (&x)[NV][V], int F, double eps,
+                                         double (&red)[2][kWaves]) {
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int e = 0; e < V; ++e) s += (double)x[j][e];  // 0 behind the row
-    const Mean mean(sum(s, red) / (double)F);
+    const Mean mean(sum(s, red[0]) / (double)F);
     double q = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -96,7 +100,7 @@ struct Rows {
         x[j][e] = column(j) + e < F ? mean.from(x[j][e]) : 0.f;
         q = __builtin_fma((double)x[j][e], (double)x[j][e], q);
       }
-    return (float)inv_sqrt(sum(q, red) / (double)F + eps);
+    return (float)inv_sqrt(sum(q, red[1]) / (double)F + eps);
   }
 };
 
@@ -104,7 +108,7 @@ template <class T, int G, int NV, bool DROP>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_fwd(NormArgs a) {
   using R = Rows<T, G, NV>;
   constexpr int V = R::V;
-  __shared__ double red[R::kWaves];
+  __shared__ double red[2][R::kWaves];
   const uint64_t call = DROP ? drop_call(a.drop) : 0;
   float gamma[NV][V], beta[NV][V];
   R::weights(gamma, a.gamma, 1.f, a.F);
@@ -138,26 +142,32 @@ template <class T, int G, int NV, bool DROP, bool WANT_X, bool WANT_W>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
   using R = Rows<T, G, NV>;
   constexpr int V = R::V;
-  __shared__ double red[R::kWaves];
+  // 1024 threads have no registers for the weights over the rows and the next row's pieces
+  constexpr bool KEEP = G < 1024;
+  __shared__ double red[2][R::kWaves];
   __shared__ float2 red2[R::kWaves];
   const uint64_t call = DROP ? drop_call(a.drop) : 0;
   float gamma[NV][V], sg[NV][V] = {}, sb[NV][V] = {};
-  R::weights(gamma, a.gamma, 1.f, a.F);
+  if (KEEP) R::weights(gamma, a.gamma, 1.f, a.F);
   const int64_t step = (int64_t)gridDim.x * R::kSlots;
   int64_t i = (int64_t)blockIdx.x * R::kSlots + threadIdx.x / G;
   u4 rx[NV], rg[NV];
-  R::load(rx, a.x, a.ldx, i, a.n, a.F);
-  R::load(rg, a.dy, a.lddy, i, a.n, a.F);
+  auto load = [&](int64_t row) {
+    R::load(rx, a.x, a.ldx, row, a.n, a.F);
+    R::load(rg, a.dy, a.lddy, row, a.n, a.F);
+  };
+  if (KEEP) load(i);
   for (int64_t first = (int64_t)blockIdx.x * R::kSlots; first < a.n; first += step, i += step) {
     float x[NV][V], g[NV][V];
+    if (!KEEP) load(i);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       unpack<T>(rx[j], x[j]);
       unpack<T>(rg[j], g[j]);
     }
-    R::load(rx, a.x, a.ldx, i + step, a.n, a.F);
-    R::load(rg, a.dy, a.lddy, i + step, a.n, a.F);
+    if (KEEP) load(i + step);
     const float rstd = R::center(x, a.F, a.eps, red);
+    if (!KEEP && WANT_X) R::weights(gamma, a.gamma, 1.f, a.F);
     float s1 = 0.f, s2 = 0.f;
     const bool live = i < a.n;
 #pragma unroll
@@ -186,7 +196,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
         s1 = slot_sum<64>(s1);
         s2 = slot_sum<64>(s2);
         if ((threadIdx.x & 63) == 0) red2[threadIdx.x >> 6] = make_float2(s1, s2);
-        __syncthreads();  // (read before the next row's sums, which have barriers of their own)
+        __syncthreads();  // (the next row's sums have barriers before red2 is written again)
         s1 = s2 = 0.f;
 #pragma unroll
         for (int w = 0; w < R::kWaves; ++w) {
@@ -345,29 +355,29 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd_long(NormArgs a) {
   }
 }
 
-// dgamma and dbeta from the workgroups' rows of sums: 64 columns by 16 wavefronts, each of which
-// adds every sixteenth row in double, then the sixteen sums in turn.
+// dgamma and dbeta from the workgroups' rows of sums: 16 columns by 64 lines of threads, each
+// of which adds every 64th row in double, then the 64 sums in turn.
 __global__ __launch_bounds__(1024) void k_norm_sums(int64_t blocks, int F, const float* part,
                                                     float* dgamma, float* dbeta) {
-  __shared__ double sums[16][64];
-  const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-  const int w = threadIdx.x >> 6;
+  __shared__ double sums[64][16];
+  const int l = threadIdx.x & 15, w = threadIdx.x >> 4;
+  const int64_t c = (int64_t)blockIdx.x * 16 + l;
   double s = 0.0;
   if (c < 2 * (int64_t)F)
 #pragma unroll 8
-    for (int64_t b = w; b < blocks; b += 16) s += (double)part[b * 2 * F + c];
-  sums[w][threadIdx.x & 63] = s;
+    for (int64_t b = w; b < blocks; b += 64) s += (double)part[b * 2 * F + c];
+  sums[w][l] = s;
   __syncthreads();
   if (w > 0 || c >= 2 * (int64_t)F) return;
-  for (int k = 1; k < 16; ++k) s += sums[k][threadIdx.x & 63];
+#pragma unroll 8
+  for (int k = 1; k < 64; ++k) s += sums[k][l];
   float* out = c < F ? dgamma : dbeta;
   if (out) out[c < F ? c : c - F] = (float)s;
 }
 
 // ---- launch ----------------------------------------------------------------------
 
-// Longer rows do not fit the registers of 1024 threads (backward, with the sums, 512).
-constexpr int kLongestFwd = 16384, kLongestBwd = 8192;
+constexpr int kLongest = 16384;  // longer rows do not fit the registers of 1024 threads
 
 // The shape for rows of F elements: lanes that hold a row in 4 to 16 elements of each.
 template <class T, class Do>
@@ -376,19 +386,20 @@ gcn_status with_shape(int F, Do go) {
   using std::integral_constant;
   if (F <= 8 * kPiece<T>) return go(integral_constant<int, 8>(), integral_constant<int, 1>());
   if (F <= 64) return go(integral_constant<int, 8>(), integral_constant<int, P / 2>());
-  if (F <= 128) return go(integral_constant<int, 8>(), integral_constant<int, P>());
+  if (F <= 128) return go(integral_constant<int, 16>(), integral_constant<int, P / 2>());
   if (F <= 256) return go(integral_constant<int, 16>(), integral_constant<int, P>());
   if (F <= 512) return go(integral_constant<int, 32>(), integral_constant<int, P>());
   if (F <= 1024) return go(integral_constant<int, 64>(), integral_constant<int, P>());
   if (F <= 2048) return go(integral_constant<int, 256>(), integral_constant<int, P / 2>());
   if (F <= 4096) return go(integral_constant<int, 256>(), integral_constant<int, P>());
-  return go(integral_constant<int, 512>(), integral_constant<int, P>());
+  if (F <= 8192) return go(integral_constant<int, 512>(), integral_constant<int, P>());
+  return go(integral_constant<int, 1024>(), integral_constant<int, P>());
 }
 
 template <class T>
 gcn_status norm_fwd(const NormArgs& a, bool drop, hipStream_t s) {
   ProfScope ps("layernorm_affine_fwd", s);
-  if (a.F > kLongestFwd) {
+  if (a.F > kLongest) {
     hipLaunchKernelGGL(k_norm_fwd_long<T>, dim3((unsigned)std::min<int64_t>(a.n, 4096)),
                        dim3(kThreads), 0, s, a);
     GCN_HIP(hipGetLastError());
@@ -405,13 +416,11 @@ gcn_status norm_fwd(const NormArgs& a, bool drop, hipStream_t s) {
     GCN_HIP(hipGetLastError());
     return GCN_OK;
   };
-  if (a.F > 8192)
-    return run(std::integral_constant<int, 1024>(), std::integral_constant<int, 16 / kPiece<T>>());
   return with_shape<T>(a.F, run);
 }
 
 gcn_status norm_sums(const NormArgs& a, int64_t blocks, hipStream_t s) {
-  hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)ceil_div(2 * (int64_t)a.F, (int64_t)64)),
+  hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)ceil_div(2 * (int64_t)a.F, (int64_t)16)),
                      dim3(1024), 0, s, blocks, a.F, (const float*)a.part, a.dgamma, a.dbeta);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
@@ -426,7 +435,7 @@ gcn_status norm_bwd(NormArgs a, bool drop, hipStream_t s) {
   // workgroups: rows of sums of at most 16 MiB in all
   const int64_t most =
       std::min<int64_t>(2048, std::max<int64_t>(512, (int64_t(1) << 21) / a.F));
-  if (a.F > kLongestBwd) {
+  if (a.F > kLongest) {
     const int64_t blocks = std::min(a.n, most);
     if (want_w) GCN_CHECK(temps.alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients"));
     hipLaunchKernelGGL(k_norm_bwd_long<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
