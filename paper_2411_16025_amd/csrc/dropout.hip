@@ -31,23 +31,48 @@ gcn_status make_drop(const gcn_dropout_spec* spec, int64_t n, Drop* out) {
 
 namespace {
 
-constexpr int kThreads = 256;
+// Pieces of 16 bytes, eight to a thread, so that a thread's loads are all on their way
+// before its first mask; a workgroup has a run of whole rows (or a part of a long one), and a
+// thread finds its piece's row by a multiplication. Reading and writing bound it, also at
+// 2 bytes an element: seven rounds are 14 wide multiplications for 4 elements.
+constexpr int kThreads = 256, kPer = 8, kTile = kThreads * kPer;
 
-// One thread per block of four columns.
+struct DropArgs {
+  uint32_t n, F, pieces;   // pieces of a row
+  uint32_t rows, parts;    // rows of a workgroup, workgroups of a row
+  uint32_t magic;          // ceil(2^32 / pieces): t magic / 2^32 = t / pieces for pieces > 1, t < 2^16
+  const void* x;
+  int64_t ldx;
+  void* y;
+  int64_t ldy;
+  Drop drop;
+};
+
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_dropout(int64_t n, int64_t F, const T* x, int64_t ldx,
-                                                      T* y, int64_t ldy, Drop d) {
-  const int64_t per = (F + 3) / 4;
-  const uint64_t call = drop_call(d);
-  for (int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x; t < n * per;
-       t += (int64_t)gridDim.x * kThreads) {
-    const int64_t i = t / per, b = t % per;
-    uint32_t w[4];
-    drop_words(d, call, (uint32_t)i, (uint32_t)b, w);
-    for (int e = 0; e < 4 && 4 * b + e < F; ++e) {
-      const float v = to_float(x[i * ldx + 4 * b + e]);
-      y[i * ldy + 4 * b + e] = from_float<T>(w[e] >= d.least ? v * d.scale : 0.f);
-    }
+__global__ __launch_bounds__(kThreads) void k_dropout(DropArgs a) {
+  const uint32_t row0 = blockIdx.x / a.parts * a.rows, piece0 = blockIdx.x % a.parts * kTile;
+  const uint64_t call = drop_call(a.drop);
+  uint32_t row[kPer], f[kPer];
+  u4 raw[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const uint32_t t = threadIdx.x + k * kThreads;
+    const uint32_t r =
+        a.pieces == 1 ? t : (a.rows > 1 ? (uint32_t)((uint64_t)t * a.magic >> 32) : 0);
+    const uint32_t piece = piece0 + t - r * a.pieces;
+    row[k] = row0 + r;
+    f[k] = piece * kPiece<T>;
+    if (r >= a.rows || row[k] >= a.n || piece >= a.pieces) f[k] = a.F;
+    raw[k] = load_piece(static_cast<const T*>(a.x) + row[k] * a.ldx, (int)f[k],
+                        f[k] < a.F ? (int)a.F : 0);
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (f[k] >= a.F) continue;
+    float v[kPiece<T>];
+    unpack<T>(raw[k], v);
+    drop_piece<kPiece<T>>(a.drop, call, row[k], (int)f[k], v);
+    store_piece<T>(static_cast<T*>(a.y) + row[k] * a.ldy, (int)f[k], (int)a.F, v);
   }
 }
 
@@ -55,10 +80,14 @@ template <class T>
 gcn_status dropout(int64_t n, int64_t F, const void* X, int64_t ldx, const Drop& d, void* Y,
                    int64_t ldy, hipStream_t s) {
   ProfScope ps("dropout", s);
-  const int64_t blocks = ceil_div(n * ((F + 3) / 4), (int64_t)kThreads);
-  hipLaunchKernelGGL(k_dropout<T>, dim3((unsigned)std::min<int64_t>(blocks, 16384)),
-                     dim3(kThreads), 0, s, n, F, static_cast<const T*>(X), ldx,
-                     static_cast<T*>(Y), ldy, d);
+  const int64_t pieces = ceil_div(F, (int64_t)kPiece<T>);
+  const int64_t rows = std::max<int64_t>(1, kTile / pieces), parts = ceil_div(pieces, (int64_t)kTile);
+  DropArgs a{(uint32_t)n, (uint32_t)F, (uint32_t)pieces, (uint32_t)rows, (uint32_t)parts,
+             (uint32_t)std::min<int64_t>(ceil_div(int64_t(1) << 32, pieces), 0xFFFFFFFF),
+             X, ldx, Y, ldy, d};
+  const int64_t blocks = ceil_div(n, rows) * parts;
+  GCN_CHECK(launch_fits(blocks, kThreads));
+  hipLaunchKernelGGL(k_dropout<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }

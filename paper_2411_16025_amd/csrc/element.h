@@ -87,6 +87,13 @@ __device__ inline void store_piece(T* row, int f, int F, const float (&v)[kPiece
     }
 }
 
+// A launch has fewer than 2^32 threads along an axis.
+inline gcn_status launch_fits(int64_t blocks, int64_t threads) {
+  if (blocks < (int64_t(1) << 32) / threads) return GCN_OK;
+  set_error("more tiles than one launch takes");
+  return GCN_ERANGE;
+}
+
 // n rows of F columns of a known type.
 inline gcn_status check_rows(int64_t n, int64_t F, int dtype) {
   if (n < 0 || F <= 0 || F >= (int64_t(1) << 31) ||

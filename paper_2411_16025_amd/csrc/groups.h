@@ -8,7 +8,7 @@
 // a slot is found by comparing, without sums over the groups before it.
 #pragma once
 
-#include "common.h"
+#include "element.h"
 
 namespace gcn {
 
@@ -19,13 +19,6 @@ struct Groups {
 };
 
 inline int64_t group_slots(const Groups& g, int64_t R) { return g.rows / R + g.n; }
-
-// A launch has fewer than 2^32 threads along an axis.
-inline gcn_status launch_fits(int64_t blocks, int64_t threads) {
-  if (blocks < (int64_t(1) << 32) / threads) return GCN_OK;
-  set_error("more tiles than one launch takes");
-  return GCN_ERANGE;
-}
 
 // The grouped products on the bf16 matrix cores with three-part operands
 // (gemm_split.hip). C [rows x N] = A [rows x K] op(B_g), B_g of group g at
