@@ -85,6 +85,200 @@ __global__ __launch_bounds__(kThreads) void k_grouped(GroupArgs a) {
     }
 }
 
+// ---- few rows per group ----------------------------------------------------------
+//
+// With a few rows to a group the matrices' bytes bound the product (24 rows over 13 of
+// 16 groups, 2048 x 1024 bf16: 54.5 MB). So a workgroup has 16 or 32 rows and 64 columns of C, its
+// eight wavefronts share the inner size in units of 64 (bf16) or 32 (fp32), and B comes from
+// memory straight into the registers of the matrix instruction, the next unit's on its way while
+// one is multiplied; the wavefronts' sums meet in LDS. bf16: v_mfma_f32_16x16x32_bf16, lane l holds
+// row (column) l % 16 and 8 of the inner size from 8 (l / 16); fp32: v_mfma_f32_16x16x4_f32,
+// one of the inner size, at 4 (l / 16) + s in step s. Both sides may take the inner size in any
+// order as long as it is the same one.
+constexpr int kFewThreads = 512, kFewCols = 64;
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u2a __attribute__((ext_vector_type(2), aligned(2)));
+
+// 4 values at column f of a row of N; zeros behind its end.
+__device__ inline u2 load4(const bf16* row, int f, int N) {
+  if (f + 4 <= N) return *reinterpret_cast<const u2a*>(row + f);
+  u2 r = {0, 0};
+  const uint16_t* h = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (f + e < N) r[e / 2] |= (uint32_t)h[f + e] << (16 * (e & 1));
+  return r;
+}
+
+// What a wavefront holds of B for a unit, and the product with R blocks of 16 rows of A.
+// acc[r][j]: rows 4 (l / 16) + e of block r; column: see few_column.
+template <class T, int OP, int R>
+struct Unit;
+
+template <int OP, int R>
+struct Unit<bf16, OP, R> {
+  static constexpr int K = 64;
+  u4 a[2][R], b[2][4];  // NN: b[h][j] = lines 8 (l / 16) + 2 j, + 1 of columns 4 (l % 16) ..
+  __device__ inline void load(const bf16* A, int64_t lda, const int (&row)[R], const bf16* B,
+                              int64_t ldb, int n0, int N, int k0, int K) {
+    const int l = threadIdx.x & 63, c = l & 15;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = k0 + 32 * h + 8 * (l >> 4);
+#pragma unroll
+      for (int r = 0; r < R; ++r) a[h][r] = load_piece(A + row[r] * lda, k, K);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (OP == GCN_GEMM_NT) {
+          const int n = n0 + 16 * j + c;
+          b[h][j] = load_piece(B + (int64_t)n * ldb, k, n < N ? K : 0);
+        } else {
+          const int f = n0 + 4 * c;
+          const u2 p = load4(B + (k + 2 * j) * ldb, f, k + 2 * j < K ? N : 0);
+          const u2 q = load4(B + (k + 2 * j + 1) * ldb, f, k + 2 * j + 1 < K ? N : 0);
+          b[h][j] = u4{p[0], p[1], q[0], q[1]};
+        }
+      }
+    }
+  }
+  __device__ inline void multiply(f4 (&acc)[R][4]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        u4 v = b[h][j];
+        if constexpr (OP == GCN_GEMM_NN)  // column 4 (l % 16) + j of the 8 lines
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[i] = __builtin_amdgcn_perm(b[h][i][2 + j / 2], b[h][i][j / 2],
+                                         j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf8, a[h][r]), __builtin_bit_cast(bf8, v), acc[r][j], 0, 0, 0);
+      }
+  }
+};
+
+template <int OP, int R>
+struct Unit<float, OP, R> {
+  static constexpr int K = 32;
+  u4 a[2][R], b[2][4];  // NN: b[h][s] = line 4 (l / 16) + s, columns 4 (l % 16) ..; NT: b[h][j] = 4 lines
+  __device__ inline void load(const float* A, int64_t lda, const int (&row)[R], const float* B,
+                              int64_t ldb, int n0, int N, int k0, int K) {
+    const int l = threadIdx.x & 63, c = l & 15;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = k0 + 16 * h + 4 * (l >> 4);
+#pragma unroll
+      for (int r = 0; r < R; ++r) a[h][r] = load_piece(A + row[r] * lda, k, K);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (OP == GCN_GEMM_NT) {
+          const int n = n0 + 16 * j + c;
+          b[h][j] = load_piece(B + (int64_t)n * ldb, k, n < N ? K : 0);
+        } else {
+          b[h][j] = load_piece(B + (k + j) * ldb, n0 + 4 * c, k + j < K ? N : 0);
+        }
+      }
+    }
+  }
+  __device__ inline void multiply(f4 (&acc)[R][4]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                __uint_as_float(a[h][r][s]),
+                __uint_as_float(OP == GCN_GEMM_NN ? b[h][s][j] : b[h][j][s]), acc[r][j], 0, 0, 0);
+  }
+};
+
+template <class T, class TC, int OP, int R>
+__global__ __launch_bounds__(kFewThreads) void k_few(GroupArgs a) {
+  constexpr int kWaves = kFewThreads / 64, kRows = 16 * R;
+  __shared__ float sums[kWaves][kRows][kFewCols];
+  const int col_tiles = (a.N + kFewCols - 1) / kFewCols;
+  const uint32_t tile = blockIdx.x / col_tiles;
+  const int n0 = (int)(blockIdx.x % col_tiles) * kFewCols;
+  GroupTile gt;
+  if (a.by.n <= kCountedGroups) {
+    int before;
+    if (tile >= (uint32_t)group_tiles(a.by, kRows, 0, &before)) return;
+    gt = counted_tile(a.by, (int)tile, kRows, 0, before);
+  } else {
+    gt = group_tile(a.by, tile, kRows);
+  }
+  if (gt.beg >= gt.end) return;
+  const int rows = (int)std::min<int64_t>(gt.end - gt.beg, kRows);
+  const T* A = static_cast<const T*>(a.A) + gt.beg * a.lda;
+  const T* B = static_cast<const T*>(a.B) + gt.g * a.stride_w;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int row[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) row[r] = std::min(16 * r + (l & 15), rows - 1);
+  f4 acc[R][4] = {};
+  using U = Unit<T, OP, R>;
+  U u[2];
+  const int step = kWaves * U::K;
+  int k = w * U::K;
+  if (k < a.K) u[0].load(A, a.lda, row, B, a.ldb, n0, a.N, k, a.K);
+  for (; k < a.K; k += 2 * step) {
+    if (k + step < a.K) u[1].load(A, a.lda, row, B, a.ldb, n0, a.N, k + step, a.K);
+    u[0].multiply(acc);
+    if (k + step >= a.K) break;
+    if (k + 2 * step < a.K) u[0].load(A, a.lda, row, B, a.ldb, n0, a.N, k + 2 * step, a.K);
+    u[1].multiply(acc);
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sums[w][16 * r + 4 * (l >> 4) + e][OP == GCN_GEMM_NN ? 4 * (l & 15) + j
+                                                             : 16 * j + (l & 15)] = acc[r][j][e];
+  __syncthreads();
+  TC* C = static_cast<TC*>(a.C) + gt.beg * a.ldc;
+  for (int t = threadIdx.x; t < rows * kFewCols; t += kFewThreads) {
+    const int i = t / kFewCols, c = t % kFewCols;
+    float s = 0.f;
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) s += sums[q][i][c];
+    if (n0 + c < a.N) C[i * a.ldc + n0 + c] = from_float<TC>(s);
+  }
+}
+
+// At most this many rows per group on average.
+constexpr int64_t kFewRows = 32;
+
+template <class T, class TC, int R>
+gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
+  const int64_t blocks = group_slots(a.by, 16 * R) * ceil_div((int64_t)a.N, (int64_t)kFewCols);
+  GCN_CHECK(launch_fits(blocks, kFewThreads));
+  if (op == GCN_GEMM_NN)
+    hipLaunchKernelGGL((k_few<T, TC, GCN_GEMM_NN, R>), dim3((unsigned)blocks), dim3(kFewThreads), 0,
+                       s, a);
+  else
+    hipLaunchKernelGGL((k_few<T, TC, GCN_GEMM_NT, R>), dim3((unsigned)blocks), dim3(kFewThreads), 0,
+                       s, a);
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
+template <class T, class TC>
+gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
+  ProfScope ps(op == GCN_GEMM_NN ? "grouped_nn_few" : "grouped_nt_few", s);
+  return a.by.rows <= 16 * a.by.n ? few<T, TC, 1>(op, a, s) : few<T, TC, 2>(op, a, s);
+}
+
 template <class T, class TC>
 gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
   const unsigned cols = (unsigned)ceil_div((int64_t)a.N, (int64_t)kTile);
@@ -178,6 +372,11 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
   }
   const Groups by{(int)n_groups, offsets, rows};
   hipStream_t s = (hipStream_t)stream;
+  const GroupArgs a{by, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
+  if (!tn && rows <= kFewRows * n_groups) {
+    if (dtype == GCN_DT_F32) return few<float, float>(op, a, s);
+    return dtype_c == GCN_DT_F32 ? few<bf16, float>(op, a, s) : few<bf16, bf16>(op, a, s);
+  }
   if (dtype == GCN_DT_F32 && gemm_split_grouped_takes(op, N, K, lda, ldb, ldc)) {
     ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
     const float *fa = static_cast<const float*>(A), *fb = static_cast<const float*>(B);
@@ -190,7 +389,6 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     return gemm_grouped_bf16(op, by, N, K, A, lda, B, ldb, C, ldc, dtype_c == GCN_DT_BF16, stride_w,
                              s);
   }
-  const GroupArgs a{by, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
   if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, s);
   return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, s) : grouped<bf16, bf16>(op, a, s);
 }
