@@ -812,10 +812,7 @@ gcn_status launch_split_grouped(const TallArgs& a, int per, hipStream_t stream) 
     case 2: return go(k_split_tall<4, 1, 1, 2, BT, true>, 256, 128);
     case 4: return go(k_split_tall<2, 2, 2, 2, BT, true>, 256, 128);
     case 6: return go(k_split_tall<2, 2, 2, 3, BT, true>, 256, 128);
-    default:
-      return a.groups.rows >= 32768 && a.groups.rows / a.groups.n >= 1024
-                 ? go(k_split_tall<4, 2, 2, 4, BT, true>, 512, 256)
-                 : go(k_split_tall<1, 4, 2, 2, BT, true>, 256, 64);
+    default: return go(k_split_tall<4, 2, 2, 4, BT, true>, 512, 256);
   }
 }
 
@@ -825,7 +822,11 @@ gcn_status gemm_split_grouped(int op, const Groups& g, int64_t N, int64_t K, con
                               int64_t lda, const float* B, int64_t ldb, int64_t stride_w, float* C,
                               int64_t ldc, hipStream_t stream) {
   const int64_t nb = ceil_div(N, (int64_t)32);
-  const int64_t col_tiles = ceil_div(nb, (int64_t)8);
+  // 256 x 256 tiles once there are many rows, also to a group (100,000 rows of 4 groups, 256 x 256:
+  // 86 us, 91 in tiles of 128 x 128; 16,384 rows of 16 groups, 2048 x 1024, in 64 x 256
+  // tiles, which would follow as in gemm_split_tall: 518 us, 433 in 128 x 128)
+  const bool big = g.rows >= 32768 && g.rows / g.n >= 1024;
+  const int64_t col_tiles = ceil_div(nb, (int64_t)(big ? 8 : 4));
   int per = (int)ceil_div(nb, col_tiles);
   per = per <= 2 ? per : (per + 1) / 2 * 2;
   const TallArgs a{g.rows, (int)N, (int)K, A, lda, B, ldb, (int)col_tiles, C, ldc, nullptr, 0,
