@@ -14,7 +14,8 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef float f16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u4u __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
+typedef uint32_t u2a __attribute__((ext_vector_type(2), aligned(2)));  // 8 bytes at any element
+typedef Unaligned<bf16>::type u4u;  // 16 bytes at any element
 
 #define GCN_GLOBAL __attribute__((address_space(1)))
 #define GCN_LDS __attribute__((address_space(3)))
@@ -31,7 +32,6 @@ struct MulArgs {
   int col_tiles, row_tiles;  // tiles along N, and (TN) along M
   uint32_t slots;            // groups.h
   int64_t split;             // TN: rows of a chunk
-  bool c_vec;                // bf16 C: rows of 8-byte aligned fours
   float* part;               // TN: sums of the chunks behind the first ones
 };
 
@@ -73,10 +73,21 @@ struct Tile {
   }
 };
 
+// A piece's elements moved down by n (of 2 bytes), zeros behind them.
+__device__ inline u4 move_down(u4 v, int n) {
+  const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+  const int bits = 16 * (n & 3);
+  const uint64_t a = n & 4 ? hi : lo, b = n & 4 ? 0 : hi;
+  uint64_t x = a >> bits | (bits ? b << (64 - bits) : 0), y = b >> bits;
+  if (n >= 8) x = y = 0;
+  return u4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)};
+}
+
 // The pieces of an operand that a thread brings to LDS: their offsets in memory from the
-// operand's first element of a stage, and whether the stage's inner range has them.
-// DIRECT: rows start on 16 bytes and hold whole pieces, and the loads go to LDS
-// themselves; else through registers, element by element where a piece is not whole.
+// operand's first element of a stage. DIRECT: rows start on 16 bytes and hold whole
+// pieces, and the loads go to LDS themselves. Else through registers, without a branch between
+// the loads: a piece that reaches over a row's end is read from 8 elements before the end
+// on (rows have 8) and moved down when it is stored.
 template <bool KC, int X, int BK, int NT, bool DIRECT>
 struct Loader {
   using T = Tile<KC, X, BK>;
@@ -84,11 +95,16 @@ struct Loader {
   const bf16* base;   // the operand's element (first of X, inner 0)
   int64_t ld;
   int have;           // of X inside the matrix
+  int64_t had;        // of the inner size, in the stage whose pieces are in v
   uint32_t off[kCount];
   u4 v[DIRECT ? 1 : kCount];
 
   __device__ static inline bool mine(int p) {
     return T::kPieces % NT == 0 || (int)threadIdx.x + p * NT < T::kPieces;
+  }
+  __device__ static inline int line_of(int p) { return (int)(threadIdx.x + p * NT) / T::kPerLine; }
+  __device__ static inline int element_of(int p) {  // of its line, a multiple of 8
+    return 8 * (((int)(threadIdx.x + p * NT) % T::kPerLine) ^ T::swz(line_of(p)));
   }
   __device__ inline void init(const bf16* b, int64_t ld_, int have_) {
     base = b;
@@ -96,50 +112,62 @@ struct Loader {
     have = have_;
 #pragma unroll
     for (int p = 0; p < kCount; ++p) {
-      const int s = threadIdx.x + p * NT, line = s / T::kPerLine;
-      const int e = 8 * ((s % T::kPerLine) ^ T::swz(line));
+      const int line = line_of(p), e = element_of(p);
       if constexpr (KC)
-        off[p] = 2 * (uint32_t)((line < have ? line : have - 1) * (uint32_t)ld + e);
-      else
-        off[p] = 2 * (uint32_t)(line * (uint32_t)ld + (e < have || !DIRECT ? e : 0));
+        off[p] = 2 * ((line < have ? line : have - 1) * (uint32_t)ld + e);
+      else if constexpr (DIRECT)
+        off[p] = 2 * (line * (uint32_t)ld + (e < have ? e : 0));
+      else  // (from the first of X - 8, which may lie before the tile)
+        off[p] = 2 * (line * (uint32_t)ld + (uint32_t)(std::min(e, have - 8) + 8));
     }
   }
   // Pieces of the stage whose inner range begins at k0 and has `left` elements.
   __device__ inline void load(char* lds, int64_t k0, int64_t left) {
     const char* at = reinterpret_cast<const char*>(KC ? base + k0 : base + k0 * ld);
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (DIRECT) {
+      const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int p = 0; p < kCount; ++p) {
-      if (!mine(p)) continue;
-      const int s = threadIdx.x + p * NT, line = s / T::kPerLine;
-      const int e = 8 * ((s % T::kPerLine) ^ T::swz(line));
-      if constexpr (DIRECT) {
+      for (int p = 0; p < kCount; ++p) {
+        if (!mine(p)) continue;
         const char* q = at + off[p];
-        if (left < BK && (KC ? e : line) >= left) q = reinterpret_cast<const char*>(&g_zeros);
+        if (left < BK && (KC ? element_of(p) : line_of(p)) >= left)
+          q = reinterpret_cast<const char*>(&g_zeros);
         __builtin_amdgcn_global_load_lds((const GCN_GLOBAL void*)q,
                                          (GCN_LDS void*)(lds + (w * 64 + p * NT) * 16), 16, 0, 0);
-      } else {
-        const bf16* q = reinterpret_cast<const bf16*>(at + off[p]);
-        const int in = KC ? (int)std::min<int64_t>(left - e, 8)
-                          : (line < left ? std::min(have - e, 8) : 0);
-        u4 x = {0, 0, 0, 0};
-        if (in >= 8) {
-          x = *reinterpret_cast<const u4u*>(q);
-        } else {
-          const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+      }
+    } else {
+      had = left;
+      if (left <= 0) return;  // past the last stage
+      if (!KC) at -= 16;
+      if (left >= BK) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < in) x[j / 2] |= (uint32_t)h[j] << (16 * (j & 1));
+        for (int p = 0; p < kCount; ++p)
+          if (mine(p)) v[p] = *reinterpret_cast<const u4u*>(at + off[p]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < kCount; ++p) {
+          const int over = KC ? element_of(p) - (int)left + 8 : line_of(p) - (int)left + 1;
+          const char* q = at + off[p];
+          if (over > 0) q -= KC ? 2 * (int64_t)over : 2 * over * ld;
+          if (mine(p)) v[p] = *reinterpret_cast<const u4u*>(q);
         }
-        v[p] = x;
       }
     }
   }
   __device__ inline void store(char* lds) {
     if constexpr (!DIRECT) {
+      const bool whole = had >= BK && (KC || have >= X);
 #pragma unroll
-      for (int p = 0; p < kCount; ++p)
-        if (mine(p)) *reinterpret_cast<u4*>(lds + (threadIdx.x + p * NT) * 16) = v[p];
+      for (int p = 0; p < kCount; ++p) {
+        if (!mine(p)) continue;
+        u4 x = v[p];
+        if (!whole) {
+          const int64_t over = (KC ? element_of(p) - had : (int64_t)element_of(p) - have) + 8;
+          x = move_down(x, (int)std::min<int64_t>(8, std::max<int64_t>(0, over)));
+          if (!KC && line_of(p) >= had) x = u4{0, 0, 0, 0};
+        }
+        *reinterpret_cast<u4*>(lds + (threadIdx.x + p * NT) * 16) = x;
+      }
     }
   }
 };
@@ -346,8 +374,8 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
           const u2 v = quad_rows(acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]);
           if (r >= m_end) continue;
           uint16_t* q = reinterpret_cast<uint16_t*>(C) + r * ldc + c;
-          if (c + 4 <= a.N && a.c_vec) {
-            *reinterpret_cast<u2*>(q) = v;
+          if (c + 4 <= a.N) {
+            *reinterpret_cast<u2a*>(q) = v;
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -373,59 +401,122 @@ gcn_status launch(MulArgs a, hipStream_t s) {
   return GCN_OK;
 }
 
+// The shape of a workgroup's tile. Columns for more than one 128-wide tile, and rows to a
+// group that fill it mostly: 256 x 256, and 128 x 256 with two workgroups to a CU, whose
+// stores the other one's products hide, where the inner size is short (100,000 rows of 4
+// groups, 512 x 1024: 167 us and 180; 32,768 rows of 16 groups, 2048 x 4096: 616 us
+// and 593). Operands that are brought through registers have none left for 256 x 256.
 template <int OP, class TC, bool DIRECT>
 gcn_status mul(const MulArgs& a, hipStream_t s) {
+  const bool wide = a.N > 128 && a.by.rows / a.by.n >= 192;
+  if constexpr (OP != GCN_GEMM_TN)
+    if (wide && a.K < 1024) return launch<OP, TC, DIRECT, 32, 2, 2, 2, 4>(a, s);
   if constexpr (DIRECT)
-    if (a.N > 128 && a.by.rows / a.by.n >= 192) return launch<OP, TC, true, 64, 4, 2, 2, 4>(a, s);
+    if (wide) return launch<OP, TC, true, 64, 4, 2, 2, 4>(a, s);
   return launch<OP, TC, DIRECT, 64, 2, 2, 2, 2>(a, s);
 }
 
-bool aligned16(const void* p, int64_t ld) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0;
+// Rows of 8-element pieces that start on 16 bytes.
+struct Operand {
+  const bf16* p;
+  int64_t ld, stride;   // of rows, of the groups' matrices
+  int64_t groups, rows, cols;
+  bool direct() const {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 &&
+           (groups == 1 || stride % 8 == 0);
+  }
+  int64_t pieces() const { return groups * rows * ((cols + 7) / 8); }
+};
+
+__global__ __launch_bounds__(256) void k_pad(Operand o, u4* out) {
+  const uint32_t per = (uint32_t)((o.cols + 7) / 8);
+  const uint32_t t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= o.groups * o.rows * per) return;
+  const uint32_t line = t / per, f = 8 * (t % per), g = line / (uint32_t)o.rows;
+  out[t] = load_piece(o.p + g * o.stride + (line - g * o.rows) * o.ld, (int)f, (int)o.cols);
+}
+
+// A copy with rows padded with zeros to whole pieces.
+gcn_status pad(Operand* o, TempScope* temps, hipStream_t s) {
+  u4* to = nullptr;
+  GCN_CHECK(temps->alloc(&to, o->pieces(), "padded operand"));
+  hipLaunchKernelGGL(k_pad, dim3((unsigned)ceil_div(o->pieces(), (int64_t)256)), dim3(256), 0, s, *o,
+                     to);
+  GCN_HIP(hipGetLastError());
+  o->p = reinterpret_cast<const bf16*>(to);
+  o->ld = (o->cols + 7) / 8 * 8;
+  o->stride = o->rows * o->ld;
+  return GCN_OK;
+}
+
+// Whether both operands can be loaded directly, after copies of those that cannot where the
+// product is large against them: of odd sizes a product runs at about 430 TFLOP/s through
+// registers and 900 directly, and a copy moves 32 bytes a piece (32,768 rows of 16 groups,
+// 2047 x 4093: 766 us, 1290 without). Without memory for the copies it stays with the registers.
+bool make_direct(Operand* a, Operand* b, double work, TempScope* temps, hipStream_t s) {
+  int64_t pieces = 0;
+  for (Operand* o : {a, b})
+    if (!o->direct()) pieces += o->pieces();
+  if (pieces == 0) return true;
+  if (work < 0x1p34 || work / 2048 < (double)pieces || pieces >= (int64_t(1) << 31)) return false;
+  for (Operand* o : {a, b})
+    if (!o->direct() && pad(o, temps, s) != GCN_OK) {
+      clear_error();
+      return false;
+    }
+  return true;
 }
 
 }  // namespace
 
-bool gemm_grouped_bf16_takes(int64_t lda, int64_t ldb) {
-  return lda < (int64_t(1) << 22) && ldb < (int64_t(1) << 22);
+bool gemm_grouped_bf16_takes(int64_t N, int64_t K, int64_t lda, int64_t ldb) {
+  return N >= 8 && K >= 8 && lda < (int64_t(1) << 22) && ldb < (int64_t(1) << 22);
 }
 
 gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, const void* A,
                              int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
                              bool c_bf16, int64_t stride_w, hipStream_t s) {
+  const bool tn = op == GCN_GEMM_TN;
+  TempScope temps(s);
+  Operand oa{static_cast<const bf16*>(A), lda, 0, 1, g.rows, K}, ob = oa;
+  ob.p = static_cast<const bf16*>(B);
+  ob.ld = ldb;
+  ob.cols = op == GCN_GEMM_NT ? K : N;
+  if (!tn) {
+    ob.stride = stride_w;
+    ob.groups = stride_w == 0 ? 1 : g.n;
+    ob.rows = op == GCN_GEMM_NT ? N : K;
+  }
+  const bool direct = make_direct(&oa, &ob, (double)g.rows * (double)N * (double)K, &temps, s);
   MulArgs a{};
   a.by = g;
-  a.A = static_cast<const bf16*>(A);
-  a.lda = lda;
-  a.B = static_cast<const bf16*>(B);
-  a.ldb = ldb;
+  a.A = oa.p;
+  a.lda = oa.ld;
+  a.B = ob.p;
+  a.ldb = ob.ld;
+  a.stride_b = stride_w == 0 ? 0 : ob.stride;
   a.C = C;
   a.ldc = ldc;
   a.N = (int)N;
-  a.c_vec = c_bf16 && reinterpret_cast<uintptr_t>(C) % 8 == 0 && ldc % 4 == 0;
-  const bool rows_ok = aligned16(A, lda) && aligned16(B, ldb);
-  if (op == GCN_GEMM_TN) {
+  if (tn) {
     a.M = (int)K;
     a.stride_c = stride_w;
-    // Chunks of 256 to 2048 rows: about 512 workgroups of 256 x 256 of C where there are few
-    // groups; with many groups a chunk is a bound on the work of one.
+    // Chunks of 256 to 4096 rows: one workgroup of 256 x 256 of C to a CU where there are few
+    // groups (500,000 rows of 4 groups, 256 x 256: 131 us, with two to a CU and twice the partial
+    // sums 172); with many groups a chunk is a bound on the work of one.
     const int64_t tiles = ceil_div(K, (int64_t)256) * ceil_div(N, (int64_t)256);
     a.split = std::min<int64_t>(
-        2048, std::max<int64_t>(256, ceil_div(ceil_div(g.rows * tiles, (int64_t)512), (int64_t)64) * 64));
-    if (g.n * tiles >= 512) a.split = 2048;
-    TempScope temps(s);
+        4096, std::max<int64_t>(256, ceil_div(ceil_div(g.rows * tiles, (int64_t)240), (int64_t)64) * 64));
+    if (g.n * tiles >= 512) a.split = 4096;
     const int64_t parts = g.rows / a.split;
     if (parts > 0) GCN_CHECK(temps.alloc(&a.part, parts * K * N, "grouped GEMM partials"));
-    GCN_CHECK(rows_ok && K % 8 == 0 && N % 8 == 0 ? (mul<GCN_GEMM_TN, float, true>(a, s))
-                                                  : (mul<GCN_GEMM_TN, float, false>(a, s)));
+    GCN_CHECK(direct ? (mul<GCN_GEMM_TN, float, true>(a, s))
+                     : (mul<GCN_GEMM_TN, float, false>(a, s)));
     return parts > 0 ? sum_group_partials(g, a.split, K, N, a.part, static_cast<float*>(C), ldc,
                                           stride_w, s)
                      : GCN_OK;
   }
   a.K = (int)K;
-  a.stride_b = stride_w;
-  const bool direct = rows_ok && K % 8 == 0 && stride_w % 8 == 0 &&
-                      (op == GCN_GEMM_NT || N % 8 == 0);
   auto go = [&](auto kernel_nn, auto kernel_nt) {
     return op == GCN_GEMM_NN ? kernel_nn(a, s) : kernel_nt(a, s);
   };

@@ -303,6 +303,8 @@ gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
 // before it, if that has so many: a group of several chunks reaches the next multiple of
 // `split`. The workgroups of a group's partial sums share its elements, each element
 // the sum of all of them in chunk order.
+constexpr int kAhead = 16;  // loads on their way at a time
+
 __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t split, int64_t K,
                                                          int64_t N, int64_t p, const float* part, float* C,
                                                          int64_t ldc, int64_t stride_w) {
@@ -316,7 +318,16 @@ __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t spli
        t += more * gridDim.x * kThreads) {
     float* c = C + t / N * ldc + t % N;
     float s = *c;
-    for (int64_t j = 0; j < more; ++j) s += part[j * K * N + t];
+    const float* q = part + t;
+    int64_t j = 0;
+    for (; j + kAhead <= more; j += kAhead, q += kAhead * K * N) {
+      float v[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) v[i] = q[i * K * N];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) s += v[i];
+    }
+    for (; j < more; ++j, q += K * N) s += *q;
     *c = s;
   }
 }
@@ -385,7 +396,7 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     return tn ? gemm_split_tn_grouped(by, N, K, fa, lda, fb, ldb, fc, ldc, stride_w, s)
               : gemm_split_grouped(op, by, N, K, fa, lda, fb, ldb, stride_w, fc, ldc, s);
   }
-  if (dtype == GCN_DT_BF16 && gemm_grouped_bf16_takes(lda, ldb)) {
+  if (dtype == GCN_DT_BF16 && gemm_grouped_bf16_takes(N, K, lda, ldb)) {
     ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
     return gemm_grouped_bf16(op, by, N, K, A, lda, B, ldb, C, ldc, dtype_c == GCN_DT_BF16, stride_w,
                              s);

@@ -32,7 +32,7 @@ gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const fl
                                  const float* B, int64_t ldb, float* C, int64_t ldc,
                                  int64_t stride_w, hipStream_t stream);
 // bf16 products (gemm_grouped.hip): C = A op(B_g), or C_g = A_g^T B_g, C bf16 or fp32.
-bool gemm_grouped_bf16_takes(int64_t lda, int64_t ldb);
+bool gemm_grouped_bf16_takes(int64_t N, int64_t K, int64_t lda, int64_t ldb);
 gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, const void* A,
                              int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
                              bool c_bf16, int64_t stride_w, hipStream_t stream);

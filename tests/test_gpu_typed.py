@@ -345,6 +345,14 @@ def test_grouped_larger(G, op, kind, sizes, K, N):
         run_grouped(G, op, sizes, 0, 2, K, N, kind, "f32", pad, shift, seed=1)
 
 
+@pytest.mark.parametrize("op", [0, 1, 2])
+def test_grouped_large_odd(G, op):
+    """Large bf16 products of odd widths, whose operands are copied to aligned rows first; what
+    lies beside the rows is NaN."""
+    note("grouped large odd op=%d" % op)
+    run_grouped(G, op, [1400, 0, 1000], 3, 2, 2049, 4001, "bf16", "f32", pad=1, shift=1)
+
+
 @pytest.mark.parametrize("groups", [1, 64, 65, 4097, 20000])
 def test_grouped_many_groups(G, groups):
     """Groups found among many, most of them empty."""
