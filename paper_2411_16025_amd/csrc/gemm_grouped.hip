@@ -91,7 +91,8 @@ __device__ inline u4 move_down(u4 v, int n) {
 template <bool KC, int X, int BK, int NT, bool DIRECT>
 struct Loader {
   using T = Tile<KC, X, BK>;
-  static constexpr int kCount = (T::kPieces + NT - 1) / NT;
+  static constexpr int kCount = T::kPieces / NT;
+  static_assert(T::kPieces % NT == 0, "every thread has as many pieces");
   const bf16* base;   // the operand's element (first of X, inner 0)
   int64_t ld;
   int have;           // of X inside the matrix
@@ -99,9 +100,6 @@ struct Loader {
   uint32_t off[kCount];
   u4 v[DIRECT ? 1 : kCount];
 
-  __device__ static inline bool mine(int p) {
-    return T::kPieces % NT == 0 || (int)threadIdx.x + p * NT < T::kPieces;
-  }
   __device__ static inline int line_of(int p) { return (int)(threadIdx.x + p * NT) / T::kPerLine; }
   __device__ static inline int element_of(int p) {  // of its line, a multiple of 8
     return 8 * (((int)(threadIdx.x + p * NT) % T::kPerLine) ^ T::swz(line_of(p)));
@@ -128,7 +126,6 @@ struct Loader {
       const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
       for (int p = 0; p < kCount; ++p) {
-        if (!mine(p)) continue;
         const char* q = at + off[p];
         if (left < BK && (KC ? element_of(p) : line_of(p)) >= left)
           q = reinterpret_cast<const char*>(&g_zeros);
@@ -142,14 +139,14 @@ struct Loader {
       if (left >= BK) {
 #pragma unroll
         for (int p = 0; p < kCount; ++p)
-          if (mine(p)) v[p] = *reinterpret_cast<const u4u*>(at + off[p]);
+          v[p] = *reinterpret_cast<const u4u*>(at + off[p]);
       } else {
 #pragma unroll
         for (int p = 0; p < kCount; ++p) {
           const int over = KC ? element_of(p) - (int)left + 8 : line_of(p) - (int)left + 1;
           const char* q = at + off[p];
           if (over > 0) q -= KC ? 2 * (int64_t)over : 2 * over * ld;
-          if (mine(p)) v[p] = *reinterpret_cast<const u4u*>(q);
+          v[p] = *reinterpret_cast<const u4u*>(q);
         }
       }
     }
@@ -159,7 +156,6 @@ struct Loader {
       const bool whole = had >= BK && (KC || have >= X);
 #pragma unroll
       for (int p = 0; p < kCount; ++p) {
-        if (!mine(p)) continue;
         u4 x = v[p];
         if (!whole) {
           const int64_t over = (KC ? element_of(p) - had : (int64_t)element_of(p) - have) + 8;
@@ -172,9 +168,10 @@ struct Loader {
   }
 };
 
-// The loads to LDS are done, for all wavefronts.
+// The loads to LDS are done, but for the last N of a thread, for all wavefronts.
+template <int N = 0>
 __device__ inline void wait_loads() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vector memory
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4 << 14));  // vector memory
   __syncthreads();
 }
 
@@ -213,8 +210,9 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
   constexpr int LEAST = OP == GCN_GEMM_TN ? 1 : 0;  // an empty group's C is zero
   const int R = OP == GCN_GEMM_TN ? (int)a.split : BM;
   const bool counted = a.by.n <= kCountedGroups;
-  int before = 0;
-  const uint32_t rows = counted ? group_tiles(a.by, R, LEAST, &before) : a.slots;
+  TileCount count{};
+  if (counted) count = count_tiles(a.by, R, LEAST);
+  const uint32_t rows = counted ? count.total : a.slots;
   const uint32_t per_row = a.col_tiles * a.row_tiles, units = rows * per_row, xcd = blockIdx.x & 7;
   const uint32_t u = (uint32_t)((uint64_t)units * xcd / 8) + (blockIdx.x >> 3);
   if (u >= (uint32_t)((uint64_t)units * (xcd + 1) / 8)) return;
@@ -230,7 +228,7 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
     slot = 4 * band + in % of;
     ct = (int)(in / of);
   }
-  const GroupTile gt = counted ? counted_tile(a.by, (int)slot, R, LEAST, before)
+  const GroupTile gt = counted ? counted_tile(a.by, count, (int)slot, R, LEAST)
                                : group_tile(a.by, slot, R);
   int64_t k_beg = 0, k_end = a.K;
   Loader<AK, BM, BK, NT, DIRECT> la;
@@ -321,8 +319,8 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
     load(0, a0, b0);
     la.store(a0);
     lb.store(b0);
-    wait_loads();
     load(1, a1, b1);
+    wait_loads<DIRECT ? decltype(la)::kCount + decltype(lb)::kCount : 63>();
     if (m0 + wr * RB * 32 >= m_end) {  // no rows for this wavefront: it brings its part only
       for (int64_t s = 0; s < stages; s += 2) {
         pass_on(s, a0, b0, a1, b1);
@@ -340,6 +338,8 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
     wait_loads();  // those past the last stage
   }
 
+  // C past the caches, which hold A and B for the workgroups that still read them (32,768 x 4096 x
+  // 2048, one group: 521 us, 490 so)
   TC* C = static_cast<TC*>(a.C);
   int64_t ldc = a.ldc;
   if constexpr (OP == GCN_GEMM_TN) {
@@ -362,7 +362,8 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int64_t r = r0 + (e & 3) + 8 * (e >> 2);
-          if (r < m_end && c < a.N) C[r * ldc + c] = acc[i][j][e];
+          if (r < m_end && c < a.N)
+            __builtin_nontemporal_store(acc[i][j][e], reinterpret_cast<float*>(C) + r * ldc + c);
         }
       } else {
         // 4 x 4 values of 4 lanes change places, so that a lane has 4 columns of a row (one
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
           if (r >= m_end) continue;
           uint16_t* q = reinterpret_cast<uint16_t*>(C) + r * ldc + c;
           if (c + 4 <= a.N) {
-            *reinterpret_cast<u2a*>(q) = v;
+            __builtin_nontemporal_store(v, reinterpret_cast<u2a*>(q));
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)

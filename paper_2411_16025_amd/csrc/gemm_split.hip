@@ -434,7 +434,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tall(TallArgs a) {
           float v = __builtin_fmaf(acc[i][j][e], e & 1 ? odd : even, 0.f);
           if (a.mask) v = mk[lm + j * 32] > 0.f ? v : 0.f;
           if (a.relu) v = fmaxf(v, 0.f);
-          c[lc + j * 32] = v;
+          if constexpr (GROUPED)  // past the caches, as in gemm_grouped.hip
+            __builtin_nontemporal_store(v, c + lc + j * 32);
+          else
+            c[lc + j * 32] = v;
         }
       }
   } else {

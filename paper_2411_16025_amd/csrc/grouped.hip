@@ -210,9 +210,9 @@ __global__ __launch_bounds__(kFewThreads) void k_few(GroupArgs a) {
   const int n0 = (int)(blockIdx.x % col_tiles) * kFewCols;
   GroupTile gt;
   if (a.by.n <= kCountedGroups) {
-    int before;
-    if (tile >= (uint32_t)group_tiles(a.by, kRows, 0, &before)) return;
-    gt = counted_tile(a.by, (int)tile, kRows, 0, before);
+    const TileCount count = count_tiles(a.by, kRows, 0);
+    if (tile >= (uint32_t)count.total) return;
+    gt = counted_tile(a.by, count, (int)tile, kRows, 0);
   } else {
     gt = group_tile(a.by, tile, kRows);
   }
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t spli
                                                          int64_t N, int64_t p, const float* part, float* C,
                                                          int64_t ldc, int64_t stride_w) {
   p += blockIdx.y;
-  const GroupTile gt = group_tile_from(by, [&](int g) { return group_offset(by, g) / split <= p; });
+  const GroupTile gt = group_tile_from(by, [&](int, int64_t o) { return o / split <= p; });
   const int64_t p0 = gt.first / split, more = (gt.end - gt.first + split - 1) / split - 1;
   if (p < p0 || p >= p0 + more) return;
   part += p0 * K * N;

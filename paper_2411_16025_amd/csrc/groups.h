@@ -49,9 +49,8 @@ __device__ inline int64_t group_offset(const Groups& a, int g) {
   return o < 0 ? 0 : (o > a.rows ? a.rows : o);
 }
 
-// Tiles of R rows of all groups, counted (each group at least `least` tiles). The whole wavefront.
-__device__ inline int group_tiles_of(const Groups& a, int g, int R, int least) {
-  const int64_t rows = group_offset(a, g + 1) - group_offset(a, g);
+// Tiles of R rows that a group of so many rows has, at least `least`.
+__device__ inline int tiles_of(int64_t rows, int R, int least) {
   const int tiles = rows > 0 ? (int)((rows + R - 1) / R) : 0;
   return tiles > least ? tiles : least;
 }
@@ -62,13 +61,21 @@ __device__ inline int group_tiles_of(const Groups& a, int g, int R, int least) {
 // slots' search reads less.
 constexpr int kCountedGroups = 1024;
 
+// Sums over the lanes up to each one (register moves: within rows of 16, then the last lane of a
+// row to the next row, of two rows to the next two).
 __device__ inline int wave_inclusive(int v) {
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int u = __shfl_up(v, off, 64);
-    if ((int)(threadIdx.x & 63) >= off) v += u;
-  }
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 to rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 to rows 2 and 3
   return v;
+}
+
+__device__ inline int64_t lane_value(int64_t v, int lane) {
+  return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)v, lane) |
+         (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32;
 }
 
 // A tile's group and rows; beg >= end: nothing (first: the group's first tile).
@@ -77,20 +84,29 @@ struct GroupTile {
   int64_t beg, end, first;  // the tile's first row, the group's end, the group's first row
 };
 
-// The last group that begins (begins(g), true up to some group) and its rows, beg = first:
+// The last group that begins (begins(g, its offset), true up to some group) and its rows, beg = first:
 // every lane of the wavefront asks for one group of the range left.
 template <class Begins>
 __device__ inline GroupTile group_tile_from(const Groups& a, Begins begins) {
+  const int lane = threadIdx.x & 63;
+  GroupTile t;
+  if (a.n < 64) {  // every lane has an offset
+    const int64_t o = group_offset(a, lane <= a.n ? lane : a.n);
+    const uint64_t hit = __ballot(lane < a.n && begins(lane, o));
+    t.g = hit ? 63 - __clzll((long long)hit) : 0;
+    t.beg = t.first = lane_value(o, t.g);
+    t.end = lane_value(o, t.g + 1);
+    return t;
+  }
   int lo = 0, len = a.n;
   while (len > 1) {
     const int step = (len + 63) / 64;
-    const int g = lo + (int)(threadIdx.x & 63) * step;
-    const uint64_t hit = __ballot(g < lo + len && begins(g));
+    const int g = lo + lane * step;
+    const uint64_t hit = __ballot(g < lo + len && begins(g, group_offset(a, g)));
     const int last = hit ? 63 - __clzll((long long)hit) : 0;
     len = min(step, len - last * step);
     lo += last * step;
   }
-  GroupTile t;
   t.g = __builtin_amdgcn_readfirstlane(lo);
   t.beg = t.first = group_offset(a, t.g);
   t.end = group_offset(a, t.g + 1);
@@ -99,43 +115,60 @@ __device__ inline GroupTile group_tile_from(const Groups& a, Begins begins) {
 
 // The tile of a slot.
 __device__ inline GroupTile group_tile(const Groups& a, int64_t slot, int R) {
-  GroupTile t = group_tile_from(a, [&](int g) { return group_offset(a, g) / R + g <= slot; });
+  GroupTile t = group_tile_from(a, [&](int g, int64_t o) { return o / R + g <= slot; });
   const int64_t tile = slot - (t.first / R + t.g);
   t.beg = tile < 0 ? t.end : t.first + tile * R;
   return t;
 }
 
-// The number of tiles; before: of the groups before this lane's (a.n / 64 of them, rounded up).
-__device__ inline int group_tiles(const Groups& a, int R, int least, int* before) {
+// The tiles of all groups, counted by a wavefront; each lane has a.n / 64 groups, rounded up.
+struct TileCount {
+  int total, before;   // of the groups before the lane's own
+  int64_t first, end;  // the lane's group, where it has one
+};
+
+__device__ inline TileCount count_tiles(const Groups& a, int R, int least) {
   const int per = (a.n + 63) / 64, lane = threadIdx.x & 63;
+  TileCount c{0, 0, 0, 0};
   int mine = 0;
   for (int i = 0; i < per; ++i)
-    if (lane * per + i < a.n) mine += group_tiles_of(a, lane * per + i, R, least);
+    if (lane * per + i < a.n) {
+      c.first = group_offset(a, lane * per + i);
+      c.end = group_offset(a, lane * per + i + 1);
+      mine += tiles_of(c.end - c.first, R, least);
+    }
   const int upto = wave_inclusive(mine);
-  *before = upto - mine;
-  return __builtin_amdgcn_readlane(upto, 63);
+  c.before = upto - mine;
+  c.total = __builtin_amdgcn_readlane(upto, 63);
+  return c;
 }
 
 // Tile t of the counted ones.
-__device__ inline GroupTile counted_tile(const Groups& a, int t, int R, int least, int before) {
+__device__ inline GroupTile counted_tile(const Groups& a, const TileCount& c, int t, int R,
+                                         int least) {
   const int per = (a.n + 63) / 64, lane = threadIdx.x & 63;
   // the last lane whose groups begin at or before t (those of the lanes behind it begin later)
-  const uint64_t at = __ballot(lane * per < a.n && before <= t);
+  const uint64_t at = __ballot(lane * per < a.n && c.before <= t);
   const int l = 63 - __clzll((long long)at);
-  t -= __builtin_amdgcn_readlane(before, l);
-  int g = l * per;
-  if (per > 1) {
-    const int mine = lane < per && g + lane < a.n ? group_tiles_of(a, g + lane, R, least) : 0;
+  t -= __builtin_amdgcn_readlane(c.before, l);
+  GroupTile r;
+  if (per == 1) {
+    r.g = l;
+    r.first = lane_value(c.first, l);
+    r.end = lane_value(c.end, l);
+  } else {
+    const int g = l * per;
+    int mine = 0;
+    if (lane < per && g + lane < a.n)
+      mine = tiles_of(group_offset(a, g + lane + 1) - group_offset(a, g + lane), R, least);
     const int first = wave_inclusive(mine) - mine;
     const uint64_t in = __ballot(mine > 0 && first <= t);
     const int j = in ? 63 - __clzll((long long)in) : 0;
     t -= __builtin_amdgcn_readlane(first, j);
-    g += j;
+    r.g = __builtin_amdgcn_readfirstlane(g + j);
+    r.first = group_offset(a, r.g);
+    r.end = group_offset(a, r.g + 1);
   }
-  GroupTile r;
-  r.g = __builtin_amdgcn_readfirstlane(g);
-  r.first = group_offset(a, r.g);
-  r.end = group_offset(a, r.g + 1);
   r.beg = r.first + (int64_t)t * R;
   return r;
 }
