@@ -45,7 +45,10 @@ struct Mean {
 
 constexpr int threads_of(int G) { return G > 256 ? G : 256; }  // of a workgroup
 
-template <class T, int G, int NV>
+// FULL: the row's length is that of its lanes' registers, so nothing is guarded (at 16,384 x 4096
+// bf16 the guards were 184 branches of a row's backward pass). Otherwise what lies behind
+// the row is 0 in the registers.
+template <class T, int G, int NV, bool FULL>
 struct Rows {
   static constexpr int V = kPiece<T>, NT = threads_of(G), kSlots = NT / G;
   static constexpr int kWaves = NT / 64;
@@ -67,46 +70,73 @@ struct Rows {
     }
   }
   __device__ static inline int column(int j) { return ((int)(threadIdx.x % G) + j * G) * V; }
+  // Row i; zeros from row n on.
   __device__ static inline void load(u4 (&r)[NV], const void* x, int64_t ld, int64_t i, int64_t n,
                                      int F) {
-    const T* row = static_cast<const T*>(x) + i * ld;
+    if (i >= n) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) r[j] = load_piece(row, column(j), i < n ? F : 0);
+      for (int j = 0; j < NV; ++j) r[j] = u4{0, 0, 0, 0};
+      return;
+    }
+    const T* row = static_cast<const T*>(x) + i * ld;
+    typedef typename Unaligned<T>::type piece;
+    if (FULL || F % V == 0) {  // whole pieces: those behind the row read its first one
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        r[j] = *reinterpret_cast<const piece*>(row + (FULL || column(j) < F ? column(j) : 0));
+      if (!FULL)
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r[j][e] = column(j) < F ? r[j][e] : 0;
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) r[j] = load_piece(row, column(j), F);
+    }
+  }
+  __device__ static inline void store(T* row, int j, int F, const float (&v)[V]) {
+    store_piece<T>(row, column(j), FULL ? column(j) + V : F, v);
   }
   __device__ static inline void weights(float (&w)[NV][V], const float* from, float none, int F) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int e = 0; e < V; e += 4) {
-        const u4 r = from ? load_piece(from, column(j) + e, F) : u4(__float_as_uint(none));
+        const int f = column(j) + e;
+        const u4 r = from ? load_piece(from, f, FULL ? f + 4 : F) : u4(__float_as_uint(none));
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[j][e + k] = __uint_as_float(r[k]);
       }
   }
   // x becomes x - mean (0 behind the row); 1 / sqrt(var + eps).
   __device__ static inline float center(float (&x)[NV][V], int F, double eps,
-                                         double (&red)[2][kWaves]) {
+                                        double (&red)[2][kWaves]) {
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < V; ++e) s += (double)x[j][e];  // 0 behind the row
+      for (int e = 0; e < V; ++e) s += (double)x[j][e];
     const Mean mean(sum(s, red[0]) / (double)F);
     double q = 0.0;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[j][e] = column(j) + e < F ? mean.from(x[j][e]) : 0.f;
-        q = __builtin_fma((double)x[j][e], (double)x[j][e], q);
+        float d = mean.from(x[j][e]);
+        if (!FULL) {
+          asm volatile("" : "+v"(d));  // (chosen, not branched over)
+          d = column(j) + e < F ? d : 0.f;
+        }
+        x[j][e] = d;
+        q = __builtin_fma((double)d, (double)d, q);
       }
     return (float)inv_sqrt(sum(q, red[1]) / (double)F + eps);
   }
 };
 
-template <class T, int G, int NV, bool DROP>
+template <class T, int G, int NV, bool DROP, bool FULL>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_fwd(NormArgs a) {
-  using R = Rows<T, G, NV>;
+  using R = Rows<T, G, NV, FULL>;
   constexpr int V = R::V;
   __shared__ double red[2][R::kWaves];
   const uint64_t call = DROP ? drop_call(a.drop) : 0;
@@ -117,7 +147,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_fwd(NormArgs a) {
   int64_t i = (int64_t)blockIdx.x * R::kSlots + threadIdx.x / G;
   u4 raw[NV];
   R::load(raw, a.x, a.ldx, i, a.n, a.F);
-  // rows [i - threadIdx.x / G, + kSlots) of the workgroup: all its threads stay while one has a row
+  // rows [first, + kSlots) of the workgroup: all its threads stay while one has a row
   for (int64_t first = (int64_t)blockIdx.x * R::kSlots; first < a.n; first += step, i += step) {
     float x[NV][V];
 #pragma unroll
@@ -132,15 +162,15 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_fwd(NormArgs a) {
       for (int e = 0; e < V; ++e)
         x[j][e] = __builtin_fmaf(x[j][e] * rstd, gamma[j][e], beta[j][e]);
       if (DROP) drop_piece<V>(a.drop, call, (uint32_t)i, R::column(j), x[j]);
-      store_piece<T>(y, R::column(j), a.F, x[j]);
+      R::store(y, j, a.F, x[j]);
     }
   }
 }
 
-// WANT_X: dX; WANT_W: dgamma and dbeta.
-template <class T, int G, int NV, bool DROP, bool WANT_X, bool WANT_W>
+// dX where a.out is given, and the sums for dgamma and dbeta where a place for them is.
+template <class T, int G, int NV, bool DROP, bool FULL>
 __global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
-  using R = Rows<T, G, NV>;
+  using R = Rows<T, G, NV, FULL>;
   constexpr int V = R::V;
   // 1024 threads have no registers for the weights over the rows and the next row's pieces
   constexpr bool KEEP = G < 1024;
@@ -167,98 +197,89 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
     }
     if (KEEP) load(i + step);
     const float rstd = R::center(x, a.F, a.eps, red);
-    if (!KEEP && WANT_X) R::weights(gamma, a.gamma, 1.f, a.F);
+    if (!KEEP) R::weights(gamma, a.gamma, 1.f, a.F);
     float s1 = 0.f, s2 = 0.f;
-    const bool live = i < a.n;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if (DROP) drop_piece<V>(a.drop, call, (uint32_t)i, R::column(j), g[j]);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[j][e] *= rstd;  // H
-        if (WANT_W) {
-          sg[j][e] = __builtin_fmaf(g[j][e], x[j][e], sg[j][e]);
-          sb[j][e] += g[j][e];
-        }
-        if (WANT_X) {
-          g[j][e] *= gamma[j][e];  // T
-          s1 += g[j][e];
-          s2 = __builtin_fmaf(g[j][e], x[j][e], s2);
-        }
+        x[j][e] *= rstd;  // H; G is 0 behind the rows and the row
+        sg[j][e] = __builtin_fmaf(g[j][e], x[j][e], sg[j][e]);
+        sb[j][e] += g[j][e];
+        g[j][e] *= gamma[j][e];  // T
+        s1 += g[j][e];
+        s2 = __builtin_fmaf(g[j][e], x[j][e], s2);
       }
     }
-    if constexpr (WANT_X) {
-      float m1, m2;
-      if constexpr (G <= 64) {
-        m1 = slot_sum<G>(s1) / (float)a.F;
-        m2 = slot_sum<G>(s2) / (float)a.F;
-      } else {
-        s1 = slot_sum<64>(s1);
-        s2 = slot_sum<64>(s2);
-        if ((threadIdx.x & 63) == 0) red2[threadIdx.x >> 6] = make_float2(s1, s2);
-        __syncthreads();  // (the next row's sums have barriers before red2 is written again)
-        s1 = s2 = 0.f;
+    if (!a.out) continue;
+    float m1, m2;
+    if constexpr (G <= 64) {
+      m1 = slot_sum<G>(s1) / (float)a.F;
+      m2 = slot_sum<G>(s2) / (float)a.F;
+    } else {
+      s1 = slot_sum<64>(s1);
+      s2 = slot_sum<64>(s2);
+      if ((threadIdx.x & 63) == 0) red2[threadIdx.x >> 6] = make_float2(s1, s2);
+      __syncthreads();  // (the next row's sums have barriers before red2 is written again)
+      s1 = s2 = 0.f;
 #pragma unroll
-        for (int w = 0; w < R::kWaves; ++w) {
-          s1 += red2[w].x;
-          s2 += red2[w].y;
-        }
-        m1 = s1 / (float)a.F;
-        m2 = s2 / (float)a.F;
+      for (int w = 0; w < R::kWaves; ++w) {
+        s1 += red2[w].x;
+        s2 += red2[w].y;
       }
-      if (live) {
-        T* dx = static_cast<T*>(a.out) + i * a.ldo;
+      m1 = s1 / (float)a.F;
+      m2 = s2 / (float)a.F;
+    }
+    if (i >= a.n) continue;
+    T* dx = static_cast<T*>(a.out) + i * a.ldo;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
+    for (int j = 0; j < NV; ++j) {
 #pragma unroll
-          for (int e = 0; e < V; ++e)
-            g[j][e] = rstd * (g[j][e] - m1 - x[j][e] * m2);
-          store_piece<T>(dx, R::column(j), a.F, g[j]);
-        }
-      }
+      for (int e = 0; e < V; ++e) g[j][e] = rstd * (g[j][e] - m1 - x[j][e] * m2);
+      R::store(dx, j, a.F, g[j]);
     }
   }
-  if constexpr (WANT_W) {
-    // the workgroup's sums: over the slots of a wavefront, then over the wavefronts
-    constexpr int W = G < 64 ? R::kWaves : R::kWaves * 64 / (G < 64 ? 64 : G);  // to add in LDS
-    __shared__ float sums[W > 1 ? W - 1 : 1][G * NV * V];
-    float* out_g = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.F : a.dgamma;
-    float* out_b = a.part ? out_g + a.F : a.dbeta;
-    auto finish = [&](float (&s)[NV][V], float* out) {
+  // the workgroup's sums: over the slots of a wavefront, then over the wavefronts
+  float* out_g = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.F : a.dgamma;
+  float* out_b = a.part ? out_g + a.F : a.dbeta;
+  if (!out_g && !out_b) return;
+  constexpr int L = G < 64 ? 64 : G, W = R::NT / L;  // lanes that hold a sum each, lines of them
+  __shared__ float sums[W > 1 ? W - 1 : 1][G * NV * V];
+  auto finish = [&](float (&s)[NV][V], float* out) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
+      for (int e = 0; e < V; ++e) {
 #pragma unroll
-          for (int off = G; off < 64; off *= 2) s[j][e] += __shfl_xor(s[j][e], off, 64);
-        }
-      const int w = (int)threadIdx.x / (G < 64 ? 64 : G);
-      const bool mine = (int)threadIdx.x % (G < 64 ? 64 : G) < G;
-      if constexpr (W > 1) {
-        __syncthreads();
-        if (w > 0 && mine)
-#pragma unroll
-          for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) sums[w - 1][R::column(j) + e] = s[j][e];
-        __syncthreads();
+        for (int off = G; off < 64; off *= 2) s[j][e] += __shfl_xor(s[j][e], off, 64);
       }
-      if (w > 0 || !mine || !out) return;
+    const int w = (int)threadIdx.x / L;
+    const bool mine = (int)threadIdx.x % L < G;
+    if constexpr (W > 1) {
+      __syncthreads();
+      if (w > 0 && mine)
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int f = R::column(j) + e;
-          float v = s[j][e];
-          if constexpr (W > 1)
+          for (int e = 0; e < V; ++e) sums[w - 1][R::column(j) + e] = s[j][e];
+      __syncthreads();
+    }
+    if (w > 0 || !mine || !out) return;
 #pragma unroll
-            for (int k = 0; k < W - 1; ++k) v += sums[k][f];
-          if (f < a.F) out[f] = v;
-        }
-    };
-    finish(sg, out_g);
-    finish(sb, out_b);
-  }
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int f = R::column(j) + e;
+        float v = s[j][e];
+        if constexpr (W > 1)
+#pragma unroll
+          for (int k = 0; k < W - 1; ++k) v += sums[k][f];
+        if (f < a.F) out[f] = v;
+      }
+  };
+  finish(sg, out_g);
+  finish(sb, out_b);
 }
 
 // ---- rows of any length ------------------------------------------------------------
@@ -396,6 +417,14 @@ gcn_status with_shape(int F, Do go) {
   return go(integral_constant<int, 1024>(), integral_constant<int, P>());
 }
 
+template <class Do>
+void with_flags(bool first, bool second, Do go) {
+  if (first)
+    second ? go(std::true_type(), std::true_type()) : go(std::true_type(), std::false_type());
+  else
+    second ? go(std::false_type(), std::true_type()) : go(std::false_type(), std::false_type());
+}
+
 template <class T>
 gcn_status norm_fwd(const NormArgs& a, bool drop, hipStream_t s) {
   ProfScope ps("layernorm_affine_fwd", s);
@@ -405,18 +434,17 @@ gcn_status norm_fwd(const NormArgs& a, bool drop, hipStream_t s) {
     GCN_HIP(hipGetLastError());
     return GCN_OK;
   }
-  auto run = [&](auto g, auto nv) {
+  return with_shape<T>(a.F, [&](auto g, auto nv) {
     constexpr int G = decltype(g)::value, NV = decltype(nv)::value;
-    using R = Rows<T, G, NV>;
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.n, (int64_t)R::kSlots), 2048));
-    if (drop)
-      hipLaunchKernelGGL((k_norm_fwd<T, G, NV, true>), grid, dim3(R::NT), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_norm_fwd<T, G, NV, false>), grid, dim3(R::NT), 0, s, a);
+    constexpr int slots = threads_of(G) / G;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.n, (int64_t)slots), 2048));
+    with_flags(drop, a.F == G * NV * kPiece<T>, [&](auto d, auto full) {
+      constexpr bool D = decltype(d)::value, FULL = decltype(full)::value;
+      hipLaunchKernelGGL((k_norm_fwd<T, G, NV, D, FULL>), grid, dim3(threads_of(G)), 0, s, a);
+    });
     GCN_HIP(hipGetLastError());
     return GCN_OK;
-  };
-  return with_shape<T>(a.F, run);
+  });
 }
 
 gcn_status norm_sums(const NormArgs& a, int64_t blocks, hipStream_t s) {
@@ -444,27 +472,16 @@ gcn_status norm_bwd(NormArgs a, bool drop, hipStream_t s) {
   }
   return with_shape<T>(a.F, [&](auto g, auto nv) {
     constexpr int G = decltype(g)::value, NV = decltype(nv)::value;
-    using R = Rows<T, G, NV>;
+    constexpr int slots = threads_of(G) / G;
     // four rows and more to a slot: with one workgroup the sums are the results
-    const int64_t blocks =
-        want_w ? std::min(ceil_div(a.n, (int64_t)4 * R::kSlots), most)
-               : std::min<int64_t>(ceil_div(a.n, (int64_t)R::kSlots), 2048);
+    const int64_t blocks = std::min(ceil_div(a.n, (int64_t)4 * slots), most);
     if (want_w && blocks > 1)
       GCN_CHECK(temps.alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients"));
-    auto run = [&](auto d) {
-      constexpr bool D = decltype(d)::value;
-      const dim3 grid((unsigned)blocks), threads(R::NT);
-      if (!want_w)
-        hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, true, false>), grid, threads, 0, s, a);
-      else if (a.out)
-        hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, true, true>), grid, threads, 0, s, a);
-      else
-        hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, false, true>), grid, threads, 0, s, a);
-    };
-    if (drop)
-      run(std::true_type());
-    else
-      run(std::false_type());
+    with_flags(drop, a.F == G * NV * kPiece<T>, [&](auto d, auto full) {
+      constexpr bool D = decltype(d)::value, FULL = decltype(full)::value;
+      hipLaunchKernelGGL((k_norm_bwd<T, G, NV, D, FULL>), dim3((unsigned)blocks),
+                         dim3(threads_of(G)), 0, s, a);
+    });
     GCN_HIP(hipGetLastError());
     return want_w && blocks > 1 ? norm_sums(a, blocks, s) : GCN_OK;
   });
