@@ -423,8 +423,8 @@ gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void* X, int64_t
  * the pass holds anyway). dX [n x F] of type dtype, may be dY or X itself (same
  * ld), and may not overlap them otherwise; dgamma and dbeta fp32 [F]. Each may be
  * NULL, not all three. With n = 0 dgamma and dbeta become zero. Rows are summed in
- * an order that n, F and the type alone decide. Takes temporaries for dgamma and
- * dbeta. Asynchronous. */
+ * an order that n, F, the type and the device decide, so results repeat bit for bit.
+ * Takes temporaries for dgamma and dbeta. Asynchronous. */
 gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
                                     const float* gamma, double eps, const gcn_dropout_spec* drop,
                                     const void* dY, int64_t lddy, void* dX, int64_t lddx,
