@@ -78,6 +78,11 @@ __device__ inline int64_t lane_value(int64_t v, int lane) {
          (int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32;
 }
 
+__device__ inline int64_t uniform(int64_t v) {
+  return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+         (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32;
+}
+
 // A tile's group and rows; beg >= end: nothing (first: the group's first tile).
 struct GroupTile {
   int g;
@@ -88,25 +93,16 @@ struct GroupTile {
 // every lane of the wavefront asks for one group of the range left.
 template <class Begins>
 __device__ inline GroupTile group_tile_from(const Groups& a, Begins begins) {
-  const int lane = threadIdx.x & 63;
-  GroupTile t;
-  if (a.n < 64) {  // every lane has an offset
-    const int64_t o = group_offset(a, lane <= a.n ? lane : a.n);
-    const uint64_t hit = __ballot(lane < a.n && begins(lane, o));
-    t.g = hit ? 63 - __clzll((long long)hit) : 0;
-    t.beg = t.first = lane_value(o, t.g);
-    t.end = lane_value(o, t.g + 1);
-    return t;
-  }
   int lo = 0, len = a.n;
   while (len > 1) {
     const int step = (len + 63) / 64;
-    const int g = lo + lane * step;
+    const int g = lo + (int)(threadIdx.x & 63) * step;
     const uint64_t hit = __ballot(g < lo + len && begins(g, group_offset(a, g)));
     const int last = hit ? 63 - __clzll((long long)hit) : 0;
     len = min(step, len - last * step);
     lo += last * step;
   }
+  GroupTile t;
   t.g = __builtin_amdgcn_readfirstlane(lo);
   t.beg = t.first = group_offset(a, t.g);
   t.end = group_offset(a, t.g + 1);
@@ -166,8 +162,8 @@ __device__ inline GroupTile counted_tile(const Groups& a, const TileCount& c, in
     const int j = in ? 63 - __clzll((long long)in) : 0;
     t -= __builtin_amdgcn_readlane(first, j);
     r.g = __builtin_amdgcn_readfirstlane(g + j);
-    r.first = group_offset(a, r.g);
-    r.end = group_offset(a, r.g + 1);
+    r.first = uniform(group_offset(a, r.g));
+    r.end = uniform(group_offset(a, r.g + 1));
   }
   r.beg = r.first + (int64_t)t * R;
   return r;
