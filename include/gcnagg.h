@@ -371,11 +371,21 @@ gcn_status gcn_sage3_step(const gcn_graph* g, const float* X, int64_t ldx, int64
  *            next one's, of B in NN and NT (>= 0; 0: one matrix for all), of C in
  *            TN (at least (K - 1) ldc + N). C may not overlap A or B.
  * 1 <= n_groups < 65536, 0 <= rows < 2^31, 1 <= K, N < 2^24. Results repeat bit for bit.
- * TN takes temporaries (sums of parts of long groups). Asynchronous on `stream`. */
+ *  work, work_bytes  scratch memory, for sums of parts of long groups (TN) and for
+ *            aligned copies of large bf16 operands whose rows are not aligned.
+ *            work_bytes NULL: the library takes temporaries; a captured call that
+ *            needs any fails with GCN_ESTATE, for they would become memory nodes
+ *            of the caller's graph. work NULL and work_bytes not: *work_bytes (host)
+ *            receives what the call would use, and nothing else is done. Both:
+ *            device memory of *work_bytes bytes, 256-byte aligned, that the call
+ *            may use until its work is done; too little of it -> GCN_EINVAL.
+ *            Without memory for the copies the product runs without them.
+ * GCN_ERANGE where the tiles are more than one launch takes (2^32 threads).
+ * Asynchronous on `stream`. */
 gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* offsets, int64_t rows,
                             int64_t N, int64_t K, const void* A, int64_t lda, const void* B,
                             int64_t ldb, int dtype, void* C, int64_t ldc, int dtype_c,
-                            int64_t stride_w, void* stream);
+                            int64_t stride_w, void* work, int64_t* work_bytes, void* stream);
 
 /* Which elements a dropout keeps: those whose 32-bit random word is at least
  * floor(p 2^32). The word of element (i, f) is word f % 4 of the block that
@@ -397,7 +407,8 @@ typedef struct {
 /* Y[i, f] = X[i, f] / (1 - p) where the element is kept, else +0 (also of an
  * infinity or NaN); computed in fp32 and rounded once to the type. The gradient is
  * the same call on dY. X and Y [n x F] are of type dtype (GCN_DT_F32 or
- * GCN_DT_BF16); Y may be X itself (same ld), and may not overlap it otherwise.
+ * GCN_DT_BF16), n < 2^31, F <= 2^30; Y may be X itself (same ld), and may not overlap
+ * it otherwise.
  * `drop` is a host pointer, read before the call returns. Asynchronous. */
 gcn_status gcn_dropout(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
                        const gcn_dropout_spec* drop, void* Y, int64_t ldy, void* stream);
@@ -406,8 +417,8 @@ gcn_status gcn_dropout(int64_t n, int64_t F, const void* X, int64_t ldx, int dty
  *   H = (X - mean) / sqrt(var + eps),  Y = dropout(H * gamma + beta)
  * over the F features of each row, biased variance, sums of the statistics in
  * double, the rest in fp32, rounded once to the type.
- *  X, Y      [n x F] of type dtype (GCN_DT_F32 or GCN_DT_BF16); Y may be X itself
- *            (same ld), and may not overlap it otherwise.
+ *  X, Y      [n x F] of type dtype (GCN_DT_F32 or GCN_DT_BF16), n < 2^31, F <= 2^30;
+ *            Y may be X itself (same ld), and may not overlap it otherwise.
  *  gamma, beta  fp32 [F], or NULL for 1 and 0.
  *  drop      NULL: no dropout; else as for gcn_dropout.
  * Asynchronous. Nothing is kept for the backward pass but X itself. */
@@ -424,11 +435,13 @@ gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void* X, int64_t
  * ld), and may not overlap them otherwise; dgamma and dbeta fp32 [F]. Each may be
  * NULL, not all three. With n = 0 dgamma and dbeta become zero. Rows are summed in
  * an order that n, F, the type and the device decide, so results repeat bit for bit.
- * Takes temporaries for dgamma and dbeta. Asynchronous. */
+ *  work, work_bytes  scratch memory for dgamma and dbeta, as for gcn_gemm_grouped.
+ * Asynchronous. */
 gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
                                     const float* gamma, double eps, const gcn_dropout_spec* drop,
                                     const void* dY, int64_t lddy, void* dX, int64_t lddx,
-                                    float* dgamma, float* dbeta, void* stream);
+                                    float* dgamma, float* dbeta, void* work, int64_t* work_bytes,
+                                    void* stream);
 
 /* ---- hybrid pre/post-aggregation (Algorithm 1, Sections 5.2 and 5.3) ---- */
 

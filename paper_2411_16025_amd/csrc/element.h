@@ -96,9 +96,9 @@ inline gcn_status launch_fits(int64_t blocks, int64_t threads) {
 
 // n rows of F columns of a known type.
 inline gcn_status check_rows(int64_t n, int64_t F, int dtype) {
-  if (n < 0 || F <= 0 || F >= (int64_t(1) << 31) ||
+  if (n < 0 || F <= 0 || F > (int64_t(1) << 30) ||
       (dtype != GCN_DT_F32 && dtype != GCN_DT_BF16)) {
-    set_error("need n >= 0, F in [1, 2^31) and a known dtype");
+    set_error("need n >= 0, F in [1, 2^30] and a known dtype");
     return GCN_EINVAL;
   }
   if (n >= (int64_t(1) << 31)) {

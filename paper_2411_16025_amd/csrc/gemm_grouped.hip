@@ -437,35 +437,38 @@ __global__ __launch_bounds__(256) void k_pad(Operand o, u4* out) {
   out[t] = load_piece(o.p + g * o.stride + (line - g * o.rows) * o.ld, (int)f, (int)o.cols);
 }
 
-// A copy with rows padded with zeros to whole pieces.
-gcn_status pad(Operand* o, TempScope* temps, hipStream_t s) {
-  u4* to = nullptr;
-  GCN_CHECK(temps->alloc(&to, o->pieces(), "padded operand"));
-  hipLaunchKernelGGL(k_pad, dim3((unsigned)ceil_div(o->pieces(), (int64_t)256)), dim3(256), 0, s, *o,
-                     to);
-  GCN_HIP(hipGetLastError());
-  o->p = reinterpret_cast<const bf16*>(to);
-  o->ld = (o->cols + 7) / 8 * 8;
-  o->stride = o->rows * o->ld;
-  return GCN_OK;
-}
-
-// Whether both operands can be loaded directly, after copies of those that cannot where the
-// product is large against them: of odd sizes a product runs at about 430 TFLOP/s through
-// registers and 900 directly, and a copy moves 32 bytes a piece (32,768 rows of 16 groups,
-// 2047 x 4093: 766 us, 1290 without). Without memory for the copies it stays with the registers.
-bool make_direct(Operand* a, Operand* b, double work, TempScope* temps, hipStream_t s) {
+// Whether both operands can be loaded directly, after copies of those that cannot, with rows
+// padded with zeros to whole pieces, where the product is large against them: of odd sizes a
+// product runs at about 430 TFLOP/s through registers and 900 directly, and a copy moves 32
+// bytes a piece (32,768 rows of 16 groups, 2047 x 4093: 766 us, 1290 without). Without memory for
+// the copies it stays with the registers.
+gcn_status make_direct(Operand* a, Operand* b, double work, Scratch* scratch, bool* direct,
+                       hipStream_t s) {
   int64_t pieces = 0;
   for (Operand* o : {a, b})
     if (!o->direct()) pieces += o->pieces();
-  if (pieces == 0) return true;
-  if (work < 0x1p34 || work / 2048 < (double)pieces || pieces >= (int64_t(1) << 31)) return false;
-  for (Operand* o : {a, b})
-    if (!o->direct() && pad(o, temps, s) != GCN_OK) {
-      clear_error();
-      return false;
-    }
-  return true;
+  *direct = pieces == 0;
+  if (*direct || work < 0x1p34 || work / 2048 < (double)pieces || pieces >= (int64_t(1) << 31))
+    return GCN_OK;
+  u4* to = nullptr;
+  if (scratch->alloc(&to, pieces, "aligned copies of operands") != GCN_OK) {
+    clear_error();
+    return GCN_OK;
+  }
+  if (scratch->asked()) return GCN_OK;
+  for (Operand* o : {a, b}) {
+    if (o->direct()) continue;
+    hipLaunchKernelGGL(k_pad, dim3((unsigned)ceil_div(o->pieces(), (int64_t)256)), dim3(256), 0, s,
+                       *o, to);
+    GCN_HIP(hipGetLastError());
+    const bf16* copy = reinterpret_cast<const bf16*>(to);
+    to += o->pieces();
+    o->p = copy;
+    o->ld = (o->cols + 7) / 8 * 8;
+    o->stride = o->rows * o->ld;
+  }
+  *direct = true;
+  return GCN_OK;
 }
 
 }  // namespace
@@ -476,9 +479,8 @@ bool gemm_grouped_bf16_takes(int64_t N, int64_t K, int64_t lda, int64_t ldb) {
 
 gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, const void* A,
                              int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
-                             bool c_bf16, int64_t stride_w, hipStream_t s) {
+                             bool c_bf16, int64_t stride_w, Scratch* scratch, hipStream_t s) {
   const bool tn = op == GCN_GEMM_TN;
-  TempScope temps(s);
   Operand oa{static_cast<const bf16*>(A), lda, 0, 1, g.rows, K}, ob = oa;
   ob.p = static_cast<const bf16*>(B);
   ob.ld = ldb;
@@ -488,7 +490,8 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
     ob.groups = stride_w == 0 ? 1 : g.n;
     ob.rows = op == GCN_GEMM_NT ? N : K;
   }
-  const bool direct = make_direct(&oa, &ob, (double)g.rows * (double)N * (double)K, &temps, s);
+  bool direct = false;
+  GCN_CHECK(make_direct(&oa, &ob, (double)g.rows * (double)N * (double)K, scratch, &direct, s));
   MulArgs a{};
   a.by = g;
   a.A = oa.p;
@@ -510,13 +513,15 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
         4096, std::max<int64_t>(256, ceil_div(ceil_div(g.rows * tiles, (int64_t)240), (int64_t)64) * 64));
     if (g.n * tiles >= 512) a.split = 4096;
     const int64_t parts = g.rows / a.split;
-    if (parts > 0) GCN_CHECK(temps.alloc(&a.part, parts * K * N, "grouped GEMM partials"));
+    if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * K * N, "grouped GEMM partials"));
+    if (scratch->asked()) return GCN_OK;
     GCN_CHECK(direct ? (mul<GCN_GEMM_TN, float, true>(a, s))
                      : (mul<GCN_GEMM_TN, float, false>(a, s)));
     return parts > 0 ? sum_group_partials(g, a.split, K, N, a.part, static_cast<float*>(C), ldc,
                                           stride_w, s)
                      : GCN_OK;
   }
+  if (scratch->asked()) return GCN_OK;
   a.K = (int)K;
   auto go = [&](auto kernel_nn, auto kernel_nt) {
     return op == GCN_GEMM_NN ? kernel_nn(a, s) : kernel_nt(a, s);

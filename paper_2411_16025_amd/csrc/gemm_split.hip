@@ -840,7 +840,7 @@ gcn_status gemm_split_grouped(int op, const Groups& g, int64_t N, int64_t K, con
 
 gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const float* A, int64_t lda,
                                  const float* B, int64_t ldb, float* C, int64_t ldc,
-                                 int64_t stride_w, hipStream_t stream) {
+                                 int64_t stride_w, Scratch* scratch, hipStream_t stream) {
   // tiles and chunks as in gemm_split_tn; chunks of at most 2048 rows
   const bool wide = K > 128 && N > 128 && g.rows / g.n >= 2048 && g.rows >= 131072;
   const int64_t tm = wide ? 256 : 128;
@@ -855,9 +855,9 @@ gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const fl
   const int64_t parts = g.rows / split;
   const int64_t blocks = tiles * ceil_div(slots, (int64_t)8) * 8;
   GCN_CHECK(launch_fits(blocks, 512));
-  TempScope temps(stream);
   float* part = nullptr;
-  if (parts > 0) GCN_CHECK(temps.alloc(&part, parts * K * N, "grouped GEMM partials"));
+  if (parts > 0) GCN_CHECK(scratch->alloc(&part, parts * K * N, "grouped GEMM partials"));
+  if (scratch->asked()) return GCN_OK;
   const TnArgs a{(int)K, (int)N, 0, split, 0, 1, slots, A, lda, B, ldb, part, (int)m_tiles,
                  (int)n_tiles, g, C, ldc, stride_w};
   auto go = [&](auto kern, int threads) {

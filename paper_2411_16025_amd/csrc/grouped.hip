@@ -355,7 +355,8 @@ using namespace gcn;
 extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* offsets,
                                        int64_t rows, int64_t N, int64_t K, const void* A,
                                        int64_t lda, const void* B, int64_t ldb, int dtype, void* C,
-                                       int64_t ldc, int dtype_c, int64_t stride_w, void* stream) {
+                                       int64_t ldc, int dtype_c, int64_t stride_w, void* work,
+                                       int64_t* work_bytes, void* stream) {
   clear_error();
   CallScope scope(stream);
   const bool tn = op == GCN_GEMM_TN;
@@ -373,6 +374,12 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     set_error("need a known dtype, and dtype_c fp32 or (NN, NT) the operands'");
     return GCN_EINVAL;
   }
+  if (work && !work_bytes) {
+    set_error("work memory needs work_bytes");
+    return GCN_EINVAL;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  Scratch scratch(work, work_bytes, s);
   if (rows == 0 && !tn) return GCN_OK;
   const int64_t big = int64_t(1) << 40;
   if (!offsets || !C || (rows > 0 && (!A || !B)) || lda < K || ldc < N ||
@@ -383,9 +390,9 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     return GCN_EINVAL;
   }
   const Groups by{(int)n_groups, offsets, rows};
-  hipStream_t s = (hipStream_t)stream;
   const GroupArgs a{by, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
   if (!tn && rows <= few_rows(dtype) * n_groups) {
+    if (scratch.asked()) return GCN_OK;
     if (dtype == GCN_DT_F32) return few<float, float>(op, a, s);
     return dtype_c == GCN_DT_F32 ? few<bf16, float>(op, a, s) : few<bf16, bf16>(op, a, s);
   }
@@ -393,14 +400,16 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
     const float *fa = static_cast<const float*>(A), *fb = static_cast<const float*>(B);
     float* fc = static_cast<float*>(C);
-    return tn ? gemm_split_tn_grouped(by, N, K, fa, lda, fb, ldb, fc, ldc, stride_w, s)
+    return tn ? gemm_split_tn_grouped(by, N, K, fa, lda, fb, ldb, fc, ldc, stride_w, &scratch, s)
+              : scratch.asked() ? GCN_OK
               : gemm_split_grouped(op, by, N, K, fa, lda, fb, ldb, stride_w, fc, ldc, s);
   }
   if (dtype == GCN_DT_BF16 && gemm_grouped_bf16_takes(N, K, lda, ldb)) {
     ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
     return gemm_grouped_bf16(op, by, N, K, A, lda, B, ldb, C, ldc, dtype_c == GCN_DT_BF16, stride_w,
-                             s);
+                             &scratch, s);
   }
+  if (scratch.asked()) return GCN_OK;
   if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, s);
   return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, s) : grouped<bf16, bf16>(op, a, s);
 }

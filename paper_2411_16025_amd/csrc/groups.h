@@ -9,6 +9,7 @@
 #pragma once
 
 #include "element.h"
+#include "scratch.h"
 
 namespace gcn {
 
@@ -30,12 +31,12 @@ gcn_status gemm_split_grouped(int op, const Groups& g, int64_t N, int64_t K, con
 // C_g [K x N] = A_g^T B_g, C_g at C + g stride_w.
 gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const float* A, int64_t lda,
                                  const float* B, int64_t ldb, float* C, int64_t ldc,
-                                 int64_t stride_w, hipStream_t stream);
+                                 int64_t stride_w, Scratch* scratch, hipStream_t stream);
 // bf16 products (gemm_grouped.hip): C = A op(B_g), or C_g = A_g^T B_g, C bf16 or fp32.
 bool gemm_grouped_bf16_takes(int64_t N, int64_t K, int64_t lda, int64_t ldb);
 gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, const void* A,
                              int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc,
-                             bool c_bf16, int64_t stride_w, hipStream_t stream);
+                             bool c_bf16, int64_t stride_w, Scratch* scratch, hipStream_t stream);
 // C_g += the partial sums of the chunks behind the first one of group g, in their
 // order; chunks of `split` rows, that of slot s at part + (s - g - 1) K N.
 gcn_status sum_group_partials(const Groups& g, int64_t split, int64_t K, int64_t N,

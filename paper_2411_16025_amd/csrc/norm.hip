@@ -6,6 +6,7 @@
 #include "dropout.h"
 #include "element.h"
 #include "lanes.h"
+#include "scratch.h"
 
 namespace gcn {
 namespace {
@@ -469,14 +470,14 @@ gcn_status norm_sums(const NormArgs& a, int64_t blocks, hipStream_t s) {
 }
 
 template <class T>
-gcn_status norm_bwd(NormArgs a, bool drop, hipStream_t s) {
+gcn_status norm_bwd(NormArgs a, bool drop, Scratch* scratch, hipStream_t s) {
   ProfScope ps("layernorm_affine_bwd", s);
-  TempScope temps(s);
   const bool want_w = a.dgamma || a.dbeta;
-  if (a.n == 0) return want_w ? norm_sums(a, 0, s) : GCN_OK;
+  if (a.n == 0) return want_w && !scratch->asked() ? norm_sums(a, 0, s) : GCN_OK;
   if (a.F > kLongest) {
     const int64_t blocks = std::min<int64_t>(a.n, 512);
-    if (want_w) GCN_CHECK(temps.alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients"));
+    if (want_w) GCN_CHECK(scratch->alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients"));
+    if (scratch->asked()) return GCN_OK;
     hipLaunchKernelGGL(k_norm_bwd_long<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
     GCN_HIP(hipGetLastError());
     return want_w ? norm_sums(a, blocks, s) : GCN_OK;
@@ -492,13 +493,13 @@ gcn_status norm_bwd(NormArgs a, bool drop, hipStream_t s) {
       static const int64_t fit = resident(kernel, threads_of(G));
       blocks = std::min(ceil_div(a.n, (int64_t)4 * slots), fit);
       if (want_w && blocks > 1)
-        st = temps.alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients");
-      if (st == GCN_OK)
+        st = scratch->alloc(&a.part, blocks * 2 * a.F, "sums of the weights' gradients");
+      if (st == GCN_OK && !scratch->asked())
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads_of(G)), 0, s, a);
     });
     GCN_CHECK(st);
     GCN_HIP(hipGetLastError());
-    return want_w && blocks > 1 ? norm_sums(a, blocks, s) : GCN_OK;
+    return want_w && blocks > 1 && !scratch->asked() ? norm_sums(a, blocks, s) : GCN_OK;
   });
 }
 
@@ -536,7 +537,8 @@ extern "C" gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void*
                                                int dtype, const float* gamma, double eps,
                                                const gcn_dropout_spec* drop, const void* dY,
                                                int64_t lddy, void* dX, int64_t lddx, float* dgamma,
-                                               float* dbeta, void* stream) {
+                                               float* dbeta, void* work, int64_t* work_bytes,
+                                               void* stream) {
   clear_error();
   CallScope scope(stream);
   GCN_CHECK(check_rows(n, F, dtype));
@@ -553,7 +555,13 @@ extern "C" gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void*
     set_error("at least one of dX, dgamma and dbeta must be non-NULL");
     return GCN_EINVAL;
   }
+  if (work && !work_bytes) {
+    set_error("work memory needs work_bytes");
+    return GCN_EINVAL;
+  }
   hipStream_t s = (hipStream_t)stream;
+  Scratch scratch(work, work_bytes, s);
   const bool on = a.drop.least > 0;
-  return dtype == GCN_DT_F32 ? norm_bwd<float>(a, on, s) : norm_bwd<bf16>(a, on, s);
+  return dtype == GCN_DT_F32 ? norm_bwd<float>(a, on, &scratch, s)
+                             : norm_bwd<bf16>(a, on, &scratch, s);
 }

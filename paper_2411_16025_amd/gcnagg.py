@@ -88,12 +88,12 @@ def lib():
         L.gcn_sage3_forward.argtypes = [P, P, i64, i64, i64, i64, P, P, P, P, ctypes.c_double, P,
                                         i64, P, i64, P, i64, P]
         L.gcn_gemm_grouped.argtypes = [i32, i64, P, i64, i64, i64, P, i64, P, i64, i32, P, i64, i32,
-                                       i64, P]
+                                       i64, P, P, P]
         L.gcn_dropout.argtypes = [i64, i64, P, i64, i32, P, P, i64, P]
         L.gcn_layernorm_affine_fwd.argtypes = [i64, i64, P, i64, i32, P, P, ctypes.c_double, P, P,
                                                i64, P]
         L.gcn_layernorm_affine_bwd.argtypes = [i64, i64, P, i64, i32, P, ctypes.c_double, P, P, i64,
-                                               P, i64, P, P, P]
+                                               P, i64, P, P, P, P, P]
         L.gcn_graph_free.argtypes = [P]
         L.gcn_graph_free.restype = None
         L.gcn_graph_info.argtypes = [P, P, P, P]
@@ -628,6 +628,31 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _capturing(stream):
+    """Whether the calls on a stream are recorded into a graph (of a raw handle: not known, and the
+    library refuses a captured call that needs memory)."""
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    if not isinstance(stream, torch.cuda.Stream):
+        return False
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _with_work(call, device, stream):
+    """call(work, work_bytes, stream). While the stream is captured the work memory is a tensor of
+    the graph's own memory, which lives as long as the graph; else the library's temporaries."""
+    s = _stream(stream)
+    if not _capturing(stream):
+        _check(call(None, None, s))
+        return
+    need = ctypes.c_int64(0)
+    _check(call(None, ctypes.byref(need), s))
+    work = _new((need.value,), torch.uint8, device, stream) if need.value else None
+    _check(call(work.data_ptr() if need.value else None,
+                ctypes.byref(need) if need.value else None, s))
+
+
 def _ld(t, name):
     """Row stride of a 2-D row-major tensor, also of one with a single row."""
     if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
@@ -679,9 +704,10 @@ def gcn_gemm_grouped(op: int, offsets: torch.Tensor, A: torch.Tensor, B: torch.T
     else:
         ldc, stride_w = _ld(C, "C"), B.stride(0)
     _on_current_device(offsets, A, B, C)
-    _check(lib().gcn_gemm_grouped(op, G, offsets.data_ptr(), rows, N, K, A.data_ptr(), lda,
-                                  B.data_ptr(), ldb, code, C.data_ptr(), ldc, _dtype_code(C),
-                                  stride_w, _stream(stream)))
+    code_c = _dtype_code(C)
+    _with_work(lambda work, size, s: lib().gcn_gemm_grouped(
+        op, G, offsets.data_ptr(), rows, N, K, A.data_ptr(), lda, B.data_ptr(), ldb, code,
+        C.data_ptr(), ldc, code_c, stride_w, work, size, s), A.device, stream)
     return C
 
 
@@ -784,10 +810,10 @@ def gcn_layernorm_affine_bwd(X: torch.Tensor, dY: torch.Tensor, gamma=None, eps:
     dbeta = _new((F,), torch.float32, X.device, stream) if weight_grad else None
     _on_current_device(X, dY, dX, gamma)
     ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    _check(lib().gcn_layernorm_affine_bwd(n, F, X.data_ptr(), ldx, code, _weight(gamma, F, "gamma"),
-                                          eps, _drop_ref(drop), dY.data_ptr(), lddy, ptr(dX),
-                                          _ld(dX, "dX") if dX is not None else 0, ptr(dgamma),
-                                          ptr(dbeta), _stream(stream)))
+    g, spec, lddx = _weight(gamma, F, "gamma"), _drop_ref(drop), _ld(dX, "dX") if input_grad else 0
+    _with_work(lambda work, size, s: lib().gcn_layernorm_affine_bwd(
+        n, F, X.data_ptr(), ldx, code, g, eps, spec, dY.data_ptr(), lddy, ptr(dX), lddx,
+        ptr(dgamma), ptr(dbeta), work, size, s), X.device, stream)
     return dX, dgamma, dbeta
 
 

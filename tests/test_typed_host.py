@@ -55,6 +55,7 @@ def test_dropout_refusals(L):
     ok = (4, 8, FAKE, 8, 0)
     assert f(-1, 8, FAKE, 8, 0, spec(), FAKE, 8, None) == EINVAL
     assert f(4, 0, FAKE, 8, 0, spec(), FAKE, 8, None) == EINVAL
+    assert f(4, (1 << 30) + 1, FAKE, 1 << 31, 0, spec(), FAKE, 1 << 31, None) == EINVAL
     assert f(4, 8, FAKE, 8, 2, spec(), FAKE, 8, None) == EINVAL   # unknown dtype
     assert f(1 << 31, 8, FAKE, 8, 0, spec(), FAKE, 8, None) == ERANGE
     assert f(*ok, None, FAKE, 8, None) == EINVAL
@@ -83,21 +84,22 @@ def test_layernorm_affine_refusals(L):
     assert f(0, 8, None, 8, 0, None, None, 1e-5, None, None, 8, None) == 0
     b = L.gcn_layernorm_affine_bwd
     other = ctypes.c_void_p(0x2000)
-    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 8, None, 0, None, None, None) == EINVAL
-    assert b(4, 8, None, 8, 0, None, 1e-5, None, other, 8, FAKE, 8, None, None, None) == EINVAL
-    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, None, 8, FAKE, 8, None, None, None) == EINVAL
-    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 4, FAKE, 8, None, None, None) == EINVAL
-    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 8, FAKE, 9, None, None, None) == EINVAL
-    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 8, other, 9, None, None, None) == EINVAL
-    assert b(4, 8, FAKE, 8, 0, None, -1.0, None, other, 8, other, 8, None, None, None) == EINVAL
+    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 8, None, 0, None, None, None, None, None) == EINVAL
+    assert b(4, 8, None, 8, 0, None, 1e-5, None, other, 8, FAKE, 8, None, None, None, None, None) == EINVAL
+    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, None, 8, FAKE, 8, None, None, None, None, None) == EINVAL
+    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 4, FAKE, 8, None, None, None, None, None) == EINVAL
+    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 8, FAKE, 9, None, None, None, None, None) == EINVAL
+    assert b(4, 8, FAKE, 8, 0, None, 1e-5, None, other, 8, other, 9, None, None, None, None, None) == EINVAL
+    assert b(4, 8, FAKE, 8, 0, None, -1.0, None, other, 8, other, 8, None, None, None, None, None) == EINVAL
     # no rows and no sums wanted: nothing to do
-    assert b(0, 8, None, 8, 0, None, 1e-5, None, None, 8, FAKE, 8, None, None, None) == 0
+    assert b(0, 8, None, 8, 0, None, 1e-5, None, None, 8, FAKE, 8, None, None, None, None, None) == 0
 
 
 def test_gemm_grouped_refusals(L):
     def f(op=0, G=2, off=FAKE, rows=4, N=8, K=8, A=FAKE, lda=8, B=FAKE, ldb=8, dt=0, C=FAKE, ldc=8,
-          dc=0, sw=64):
-        return L.gcn_gemm_grouped(op, G, off, rows, N, K, A, lda, B, ldb, dt, C, ldc, dc, sw, None)
+          dc=0, sw=64, work=None, size=None):
+        return L.gcn_gemm_grouped(op, G, off, rows, N, K, A, lda, B, ldb, dt, C, ldc, dc, sw,
+                                  work, size, None)
     for kw in (dict(op=3), dict(op=-1), dict(G=0), dict(G=65536), dict(rows=-1), dict(N=0),
                dict(K=0), dict(N=1 << 24), dict(K=1 << 24), dict(dt=2), dict(dc=2), dict(dc=1),
                dict(dt=1, dc=2), dict(op=2, dt=1, dc=1), dict(off=None), dict(A=None),
@@ -106,3 +108,12 @@ def test_gemm_grouped_refusals(L):
         assert f(**kw) == EINVAL, kw
     assert f(rows=1 << 31) == ERANGE
     assert f(rows=0) == 0  # no rows: nothing to write
+    assert f(work=FAKE) == EINVAL
+    # what a call would use: nothing for rows times a matrix, the chunks' sums for a weight gradient
+    size = ctypes.c_int64(-1)
+    assert f(size=ctypes.byref(size)) == 0 and size.value == 0
+    big = dict(op=2, rows=100000, N=256, K=256, lda=256, ldb=256, ldc=256, sw=65536)
+    assert f(size=ctypes.byref(size), **big) == 0
+    assert size.value % (256 * 256 * 4) == 0 and size.value > 0
+    less = ctypes.c_int64(size.value - 256)
+    assert f(work=FAKE, size=ctypes.byref(less), **big) == EINVAL
