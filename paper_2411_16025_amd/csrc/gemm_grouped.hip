@@ -10,6 +10,7 @@
 // the bytes of B and C (16,384 rows of 64 groups, 1024 x 512: 40 us for dX, 46 for dW).
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "element.h"
@@ -411,16 +412,25 @@ gcn_status launch(MulArgs a, hipStream_t s) {
   return GCN_OK;
 }
 
-// The shape of a workgroup's tile. Columns for more than one 128-wide tile, and rows to a
-// group that fill it mostly: 256 x 256, and 128 x 256 with two workgroups to a CU, whose
-// stores the other one's products hide, where the inner size is short (100,000 rows of 4
-// groups, 512 x 1024: 167 us and 180; 32,768 rows of 16 groups, 2048 x 4096: 616 us
-// and 593). Operands that are brought through registers have none left for 256 x 256.
+// Columns for more than one 128-wide tile, and rows to a group that fill a 256-high one mostly.
+// Operands that are brought through registers have none left for tiles of 256 x 256.
+inline bool wide_tiles(const Groups& g, int64_t N) { return N > 128 && g.rows / g.n >= 192; }
+
+// The shape of a workgroup's tile: 256 x 256 of wide products, else 128 x 128. With a short inner
+// size smaller tiles, several to a CU, whose stores the others' products hide: 128 x
+// 256 (100,000 rows of 4 groups, 512 x 1024: 148 us, 128 x 128 152; 256 x 256 12 more; but 32,768
+// rows of 16 groups, 2048 x 4096: 616 us and 593 in 256 x 256), and 128 x 128 where it is
+// shorter still or groups end inside many tiles (100,000 rows, 256 x 256: 31 us and 34; 16,384 rows of
+// 64 groups, 512 x 1024: 38 and 40).
 template <int OP, class TC, bool DIRECT>
 gcn_status mul(const MulArgs& a, hipStream_t s) {
-  const bool wide = a.N > 128 && a.by.rows / a.by.n >= 192;
+  const bool wide = wide_tiles(a.by, a.N);
   if constexpr (OP != GCN_GEMM_TN)
-    if (wide && a.K < 1024) return launch<OP, TC, DIRECT, 32, 2, 2, 2, 4>(a, s);
+    if (wide && a.K < 1024) {
+      if (a.K < 512 || a.by.rows / a.by.n < 1024)
+        return launch<OP, TC, DIRECT, 32, 2, 2, 2, 2>(a, s);
+      return launch<OP, TC, DIRECT, 32, 2, 2, 2, 4>(a, s);
+    }
   if constexpr (DIRECT)
     if (wide) return launch<OP, TC, true, 64, 4, 2, 2, 4>(a, s);
   return launch<OP, TC, DIRECT, 64, 2, 2, 2, 2>(a, s);
@@ -464,6 +474,7 @@ gcn_status make_direct(Operand* a, Operand* b, double work, Scratch* scratch, bo
     clear_error();
     return GCN_OK;
   }
+  *direct = true;
   if (scratch->asked()) return GCN_OK;
   for (Operand* o : {a, b}) {
     if (o->direct()) continue;
@@ -476,7 +487,6 @@ gcn_status make_direct(Operand* a, Operand* b, double work, Scratch* scratch, bo
     o->ld = (o->cols + 7) / 8 * 8;
     o->stride = o->rows * o->ld;
   }
-  *direct = true;
   return GCN_OK;
 }
 
@@ -514,13 +524,21 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
   if (tn) {
     a.M = (int)K;
     a.stride_c = stride_w;
-    // Chunks of 256 to 4096 rows: one workgroup of 256 x 256 of C to a CU where there are few
-    // groups (500,000 rows of 4 groups, 256 x 256: 131 us, with two to a CU and twice the partial
-    // sums 172); with many groups a chunk is a bound on the work of one.
-    const int64_t tiles = ceil_div(K, (int64_t)256) * ceil_div(N, (int64_t)256);
-    a.split = std::min<int64_t>(
-        4096, std::max<int64_t>(256, ceil_div(ceil_div(g.rows * tiles, (int64_t)240), (int64_t)64) * 64));
-    if (g.n * tiles >= 512) a.split = 4096;
+    // Chunks of rows for one workgroup of 256 x 256 of C to a CU or two of 128 x 128, up to 4096
+    // (500,000 rows of 4 groups, 256 x 256: 122 us, with two to a CU and twice the partial sums
+    // 172); where the groups' tiles are enough by themselves, 4096 bound the work of one
+    // (16,384 rows of 64 groups, 512 x 512: 26 us, 76 in chunks of 320). But a chunk costs time by
+    // its rows, and the partial sums by K N to each: their sum is least at a root of rows K N
+    // (65,536 rows of 64 groups, 256 x 256: 44 us, 53 without that bound; 32,768 of 8, 1024 x
+    // 1024: 107 and 152; 65,536 of 8, 2048 x 4096: 1.35 ms and 1.57; but 500,000 of 4, 512 x 512:
+    // 345 us and 320). 65536 rows bound the sums' chains.
+    const int64_t tile = direct && wide_tiles(g, N) ? 256 : 128, want = tile == 256 ? 240 : 480;
+    const int64_t tiles = ceil_div(K, tile) * ceil_div(N, tile);
+    const double even = (double)g.rows * (double)tiles / (double)want;  // a chunk to each
+    const double sums = std::sqrt(2e-4 * (double)g.rows * (double)K * (double)N);
+    const double chunk = std::min(
+        65536.0, std::max({256.0, sums, g.n * tiles < want ? std::min(even, 4096.0) : 4096.0}));
+    a.split = ceil_div((int64_t)chunk, (int64_t)64) * 64;
     const int64_t parts = g.rows / a.split;
     if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * K * N, "grouped GEMM partials"));
     if (scratch->asked()) return GCN_OK;

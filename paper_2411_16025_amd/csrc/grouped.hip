@@ -339,7 +339,7 @@ gcn_status sum_group_partials(const Groups& g, int64_t split, int64_t K, int64_t
                               hipStream_t stream) {
   const int64_t parts = g.rows / split;
   const int64_t blocks = std::min(ceil_div(K * N, (int64_t)kThreads),
-                                  std::max<int64_t>(16, ceil_div(4096, parts)));
+                                  std::max<int64_t>(16, ceil_div(1024, parts)));
   for (int64_t p = 0; p < parts; p += 65535) {  // (a grid's second axis)
     hipLaunchKernelGGL(k_group_sums, dim3((unsigned)blocks, (unsigned)std::min<int64_t>(parts - p, 65535)),
                        dim3(kThreads), 0, stream, g, split, K, N, p, part, C, ldc, stride_w);

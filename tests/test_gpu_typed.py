@@ -346,11 +346,12 @@ def test_grouped_larger(G, op, kind, sizes, K, N):
         run_grouped(G, op, sizes, 0, 2, K, N, kind, "f32", pad, shift, seed=1)
 
 
-# one for every shape of tile and way of loading: bf16 256 x 256 (K from 1024 on) and 128 x 256, with
-# aligned rows and without, 128 x 128, and widths below 8; fp32 256 x 256 (32,768 rows and more)
+# one for every shape of tile and way of loading: bf16 256 x 256 (K from 1024 on), 128 x 256 (from 512
+# on, groups of 1024 rows) and 128 x 128, with aligned rows and without, and widths below 8; fp32 256 x 256 (32,768 rows and more)
 @pytest.mark.parametrize("kind,out,sizes,K,N", [
     ("bf16", "bf16", [700, 300, 0, 520], 1032, 264), ("bf16", "f32", [257, 512], 1024, 520),
     ("bf16", "bf16", [700, 300, 0, 520], 136, 264), ("bf16", "bf16", [600, 511], 135, 263),
+    ("bf16", "bf16", [2300, 1], 520, 264), ("bf16", "f32", [1, 2300], 515, 261),
     ("bf16", "bf16", [600, 5], 40, 120), ("bf16", "f32", [600, 511], 5, 6),
     ("bf16", "bf16", [300], 64, 7), ("bf16", "f32", [300], 7, 64),
     ("f32", "f32", [33000, 1000, 7], 20, 160), ("f32", "f32", [400, 300], 33, 100)])
@@ -363,7 +364,8 @@ def test_grouped_tiles(G, op, kind, out, sizes, K, N):
 # weight gradients: several chunks to a group, tiles at the edges of C, and fp32's large tile
 @pytest.mark.parametrize("kind,sizes,K,N", [
     ("bf16", [5000, 0, 300, 257], 264, 520), ("bf16", [5000, 3], 47, 255), ("bf16", [3000], 9, 8),
-    ("bf16", [9000, 1], 128, 128), ("f32", [140000, 5], 136, 132), ("f32", [9000, 2500, 0], 40, 70)])
+    ("bf16", [9000, 1], 128, 128), ("bf16", [9000, 0, 700], 260, 272),
+    ("bf16", [9000, 300], 1096, 1000), ("f32", [140000, 5], 136, 132), ("f32", [9000, 2500, 0], 40, 70)])
 def test_grouped_weight_gradients(G, kind, sizes, K, N):
     note("grouped dW %s sizes=%s K=%d N=%d" % (kind, sizes, K, N))
     run_grouped(G, 2, sizes, 3, 1, K, N, kind, "f32", pad=8 if K % 8 == 0 else 1, seed=3)
@@ -673,7 +675,8 @@ def test_bf16_gradients_captured(G):
 
 
 @pytest.mark.parametrize("op,n,K,N", [("nt", 600, 40, 64), ("tn", 5000, 40, 64),
-                                      ("nt", 2400, 2049, 4001), ("tn", 2400, 2049, 4001)])
+                                      ("nt", 2400, 2049, 4001), ("tn", 2400, 2049, 4001),
+                                      ("tn", 70001, 515, 517)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_grouped_in_given_memory(G, op, n, K, N, dtype):
     """The same bits in the caller's work memory as in the library's, nothing written behind it."""
