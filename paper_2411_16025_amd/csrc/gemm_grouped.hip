@@ -348,8 +348,6 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
     wait_loads();  // those past the last stage
   }
 
-  // C past the caches, which hold A and B for the workgroups that still read them (32,768 x 4096 x
-  // 2048, one group: 521 us, 490 so)
   TC* C = static_cast<TC*>(a.C);
   int64_t ldc = a.ldc;
   if constexpr (OP == GCN_GEMM_TN) {
@@ -361,40 +359,56 @@ __global__ __launch_bounds__(64 * WR * WC, RB * CB > 8 ? 1 : 2) void k_mul(MulAr
       C += gt.g * a.stride_c;
     }
   }
+  auto write = [&](auto past) {
 #pragma unroll
-  for (int i = 0; i < RB; ++i)
+    for (int i = 0; i < RB; ++i)
 #pragma unroll
-    for (int j = 0; j < CB; ++j) {
-      const int64_t r0 = m0 + (wr * RB + i) * 32 + 4 * (lane >> 5);
-      const int c0 = n0 + (wc * CB + j) * 32;
-      if constexpr (sizeof(TC) == 4) {
-        const int c = c0 + (lane & 31);
+      for (int j = 0; j < CB; ++j) {
+        const int64_t r0 = m0 + (wr * RB + i) * 32 + 4 * (lane >> 5);
+        const int c0 = n0 + (wc * CB + j) * 32;
+        if constexpr (sizeof(TC) == 4) {
+          const int c = c0 + (lane & 31);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int64_t r = r0 + (e & 3) + 8 * (e >> 2);
-          if (r < m_end && c < a.N)
-            __builtin_nontemporal_store(acc[i][j][e], reinterpret_cast<float*>(C) + r * ldc + c);
-        }
-      } else {
-        // 4 x 4 values of 4 lanes change places, so that a lane has 4 columns of a row (one
-        // 8-byte store instead of 4 of 2 bytes)
-        const int c = c0 + (lane & 28);
+          for (int e = 0; e < 16; ++e) {
+            const int64_t r = r0 + (e & 3) + 8 * (e >> 2);
+            float* q = reinterpret_cast<float*>(C) + r * ldc + c;
+            if (r >= m_end || c >= a.N) continue;
+            if constexpr (decltype(past)::value)
+              __builtin_nontemporal_store(acc[i][j][e], q);
+            else
+              *q = acc[i][j][e];
+          }
+        } else {
+          // 4 x 4 values of 4 lanes change places, so that a lane has 4 columns of a row (one
+          // 8-byte store instead of 4 of 2 bytes)
+          const int c = c0 + (lane & 28);
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          const int64_t r = r0 + (lane & 3) + 2 * e;
-          const u2 v = quad_rows(acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]);
-          if (r >= m_end) continue;
-          uint16_t* q = reinterpret_cast<uint16_t*>(C) + r * ldc + c;
-          if (c + 4 <= a.N) {
-            __builtin_nontemporal_store(v, reinterpret_cast<u2a*>(q));
-          } else {
+          for (int e = 0; e < 16; e += 4) {
+            const int64_t r = r0 + (lane & 3) + 2 * e;
+            const u2 v = quad_rows(acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]);
+            if (r >= m_end) continue;
+            uint16_t* q = reinterpret_cast<uint16_t*>(C) + r * ldc + c;
+            if (c + 4 <= a.N) {
+              if constexpr (decltype(past)::value)
+                __builtin_nontemporal_store(v, reinterpret_cast<u2a*>(q));
+              else
+                *reinterpret_cast<u2a*>(q) = v;
+            } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (c + k < a.N) q[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+              for (int k = 0; k < 4; ++k)
+                if (c + k < a.N) q[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+            }
           }
         }
       }
-    }
+  };
+  // C past the caches, which hold A and B for the workgroups that still read them (32,768 x 4096 x
+  // 2048, one group: 521 us, 490 so), but only where its rows fill whole lines: parts of lines
+  // wait in the caches for the rest (300,000 rows of 4 groups, 48 x 252: 122 us past them, 43).
+  if (((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(ldc * (int64_t)sizeof(TC))) & 127) == 0)
+    write(std::true_type{});
+  else
+    write(std::false_type{});
 }
 
 template <int OP, class TC, bool DIRECT, int BK, int WR, int WC, int RB, int CB>

@@ -352,6 +352,7 @@ def test_grouped_larger(G, op, kind, sizes, K, N):
     ("bf16", "bf16", [700, 300, 0, 520], 1032, 264), ("bf16", "f32", [257, 512], 1024, 520),
     ("bf16", "bf16", [700, 300, 0, 520], 136, 264), ("bf16", "bf16", [600, 511], 135, 263),
     ("bf16", "bf16", [2300, 1], 520, 264), ("bf16", "f32", [1, 2300], 515, 261),
+    ("bf16", "bf16", [300, 270], 72, 248), ("bf16", "bf16", [300, 270], 72, 184),
     ("bf16", "bf16", [600, 5], 40, 120), ("bf16", "f32", [600, 511], 5, 6),
     ("bf16", "bf16", [300], 64, 7), ("bf16", "f32", [300], 7, 64),
     ("f32", "f32", [33000, 1000, 7], 20, 160), ("f32", "f32", [400, 300], 33, 100)])
