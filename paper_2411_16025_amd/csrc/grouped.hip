@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void k_grouped(GroupArgs a) {
 // row (column) l % 16 and 8 of the inner size from 8 (l / 16); fp32: v_mfma_f32_16x16x4_f32,
 // one of the inner size, at 4 (l / 16) + s in step s. Both sides may take the inner size in any
 // order as long as it is the same one.
-constexpr int kFewThreads = 512, kFewCols = 64;
+constexpr int kFewCols = 64;
 
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -201,9 +201,9 @@ struct Unit<float, OP, R> {
   }
 };
 
-template <class T, class TC, int OP, int R>
-__global__ __launch_bounds__(kFewThreads) void k_few(GroupArgs a) {
-  constexpr int kWaves = kFewThreads / 64, kRows = 16 * R;
+template <class T, class TC, int OP, int R, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void k_few(GroupArgs a) {
+  constexpr int kRows = 16 * R;
   __shared__ float sums[kWaves][kRows][kFewCols];
   const int col_tiles = (a.N + kFewCols - 1) / kFewCols;
   const uint32_t tile = blockIdx.x / col_tiles;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kFewThreads) void k_few(GroupArgs a) {
                                                              : 16 * j + (l & 15)] = acc[r][j][e];
   __syncthreads();
   TC* C = static_cast<TC*>(a.C) + gt.beg * a.ldc;
-  for (int t = threadIdx.x; t < rows * kFewCols; t += kFewThreads) {
+  for (int t = threadIdx.x; t < rows * kFewCols; t += 64 * kWaves) {
     const int i = t / kFewCols, c = t % kFewCols;
     float s = 0.f;
 #pragma unroll
@@ -256,19 +256,27 @@ __global__ __launch_bounds__(kFewThreads) void k_few(GroupArgs a) {
   }
 }
 
-// Up to this many rows per group on average. 16 groups, 2048 x 1024: bf16, 600 rows, 22.7 us here
-// and 27.5 in tiles, 1024 rows 31.8 and 28.3; fp32 1024 rows 90 and 122, 2048 rows 147 and 123.
-constexpr int64_t few_rows(int dtype) { return dtype == GCN_DT_F32 ? 96 : 48; }
+// Few rows to a group on average: of 16 groups, 2048 x 1024, bf16, 600 rows take 22.7 us here and
+// 27.5 in tiles, 1024 rows 31.8 and 28.3; fp32 1024 rows 90 and 122, 2048 rows 147 and 123. And rows
+// that are few large tiles, which would leave most CUs without work (4 groups of 433 rows,
+// 1712 x 256: fp32 18 us and 81, bf16 9 and 18; 2,500 rows of 2, 1024 x 512: 48 and 53, 21 and 30;
+// but 4,000 rows, 512 x 512, in 132 tiles: 36 and 31, 19 and 15; and more rows would read
+// B more often: 13,080 rows of 2, 3568 x 40: 145 and 122, 83 and 45).
+bool few_takes(const Groups& g, int64_t N, int dtype) {
+  const int64_t tiles = group_slots(g, 128) * ceil_div(N, (int64_t)128);
+  return g.rows <= (dtype == GCN_DT_F32 ? 96 : 48) * (int64_t)g.n ||
+         (tiles < 110 && g.rows <= 4096);
+}
 
-template <class T, class TC, int R>
+template <class T, class TC, int R, int W>
 gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
   const int64_t blocks = group_slots(a.by, 16 * R) * ceil_div((int64_t)a.N, (int64_t)kFewCols);
-  GCN_CHECK(launch_fits(blocks, kFewThreads));
+  GCN_CHECK(launch_fits(blocks, 64 * W));
   if (op == GCN_GEMM_NN)
-    hipLaunchKernelGGL((k_few<T, TC, GCN_GEMM_NN, R>), dim3((unsigned)blocks), dim3(kFewThreads), 0,
+    hipLaunchKernelGGL((k_few<T, TC, GCN_GEMM_NN, R, W>), dim3((unsigned)blocks), dim3(64 * W), 0,
                        s, a);
   else
-    hipLaunchKernelGGL((k_few<T, TC, GCN_GEMM_NT, R>), dim3((unsigned)blocks), dim3(kFewThreads), 0,
+    hipLaunchKernelGGL((k_few<T, TC, GCN_GEMM_NT, R, W>), dim3((unsigned)blocks), dim3(64 * W), 0,
                        s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
@@ -277,7 +285,15 @@ gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
 template <class T, class TC>
 gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
   ProfScope ps(op == GCN_GEMM_NN ? "grouped_nn_few" : "grouped_nt_few", s);
-  return a.by.rows <= 16 * a.by.n ? few<T, TC, 1>(op, a, s) : few<T, TC, 2>(op, a, s);
+  // 16 rows to a workgroup where 32 would leave CUs without work (53 rows, 3032 x 2816 fp32: 31 us
+  // and 48; 433 rows of 4 groups, 1712 x 256: 18 and 28)
+  const bool one = a.by.rows <= 16 * a.by.n ||
+                   group_slots(a.by, 32) * ceil_div((int64_t)a.N, (int64_t)kFewCols) < 256;
+  // two wavefronts where a short inner size leaves the others none (232 rows of 100 groups, 48 x 3208:
+  // fp32 21 us and 56, bf16 24 and 95)
+  if (a.K <= 4 * Unit<T, GCN_GEMM_NN, 1>::K)
+    return one ? few<T, TC, 1, 2>(op, a, s) : few<T, TC, 2, 2>(op, a, s);
+  return one ? few<T, TC, 1, 8>(op, a, s) : few<T, TC, 2, 8>(op, a, s);
 }
 
 template <class T, class TC>
@@ -391,7 +407,7 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
   }
   const Groups by{(int)n_groups, offsets, rows};
   const GroupArgs a{by, (int)N, (int)K, A, lda, B, ldb, C, ldc, stride_w};
-  if (!tn && rows <= few_rows(dtype) * n_groups) {
+  if (!tn && few_takes(by, N, dtype)) {
     if (scratch.asked()) return GCN_OK;
     if (dtype == GCN_DT_F32) return few<float, float>(op, a, s);
     return dtype_c == GCN_DT_F32 ? few<bf16, float>(op, a, s) : few<bf16, bf16>(op, a, s);

@@ -372,6 +372,51 @@ def test_grouped_weight_gradients(G, kind, sizes, K, N):
     run_grouped(G, 2, sizes, 3, 1, K, N, kind, "f32", pad=8 if K % 8 == 0 else 1, seed=3)
 
 
+# More rows than the kernel of few rows takes (4096): the same shapes of tiles, and the general product
+# (bf16 widths below 8).
+@pytest.mark.parametrize("kind,out,sizes,K,N", [
+    ("bf16", "bf16", [2700, 300, 0, 1520], 1032, 264), ("bf16", "f32", [2257, 2512], 1024, 520),
+    ("bf16", "bf16", [2700, 300, 0, 1520], 136, 264), ("bf16", "bf16", [2600, 2511], 135, 263),
+    ("bf16", "bf16", [2300, 1900], 520, 264), ("bf16", "f32", [1, 4400], 515, 261),
+    ("bf16", "bf16", [2300, 2270], 72, 248), ("bf16", "bf16", [2300, 2270], 72, 184),
+    ("bf16", "bf16", [4600, 5], 40, 120), ("bf16", "f32", [2600, 2511], 5, 6),
+    ("bf16", "bf16", [4300], 64, 7), ("bf16", "f32", [4300], 7, 64),
+    ("bf16", "bf16", [70] * 64, 72, 200), ("bf16", "f32", [0, 64] * 70, 1, 1),
+    ("f32", "f32", [2400, 2300], 33, 100), ("f32", "f32", [2400, 1900], 50, 160),
+    ("f32", "f32", [4300, 3], 20, 20), ("f32", "f32", [3, 0, 4300], 21, 60),
+    ("f32", "f32", [110] * 64, 1, 1)])
+@pytest.mark.parametrize("op", [0, 1])
+def test_grouped_tiles_of_many_rows(G, op, kind, out, sizes, K, N):
+    note("grouped tiles of many rows op=%d %s sizes=%s K=%d N=%d" % (op, kind, sizes[:4], K, N))
+    run_grouped(G, op, sizes, 1, 2, K, N, kind, out, pad=7 if K % 8 else 8, seed=2)
+
+
+# Rows of a few large tiles, by 16 and by 32, deep and shallow.
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("sizes,K,N", [([433], 300, 65), ([200, 0, 1], 129, 130), ([200, 33], 128, 70),
+                                       ([1900, 1], 257, 512), ([4096], 16, 64), ([2000, 2096], 256, 300)])
+def test_grouped_few_tiles(G, op, kind, sizes, K, N):
+    note("grouped few tiles op=%d %s sizes=%s K=%d N=%d" % (op, kind, sizes, K, N))
+    run_grouped(G, op, sizes, 0, 0, K, N, kind, "f32", pad=1, shift=1, seed=5)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_matrix_rows_far_apart(G, kind):
+    """A matrix whose rows are 2^22 elements apart: the general product, rows behind the first 4096."""
+    import torch
+    n, K, N, ld = 4200, 12, 24, 1 << 22
+    note("matrix rows far apart %s" % kind)
+    flat = torch.empty((N - 1) * ld + K, dtype=tdtype(kind), device="cuda:0")
+    far = torch.as_strided(flat, (1, N, K), (0, ld, 1))
+    x, b = values(4, n, K, kind), values(5, N, K, kind)
+    far.copy_(dev(b[None]).to(tdtype(kind)))
+    ends = np.array([0, n], np.int64)
+    got = G.gcn_gemm_grouped(1, dev(ends), dev(x).to(tdtype(kind)), far, out_dtype=torch.float32)
+    want, mag = ref.grouped(1, ends, x, b[None])
+    within(back(got), want, ref.grouped_bound(want, mag, K, "f32"), "C")
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_rows_far_apart(G, kind):
     """Rows 2^22 elements apart: elements beyond 2^31 of the first one, and strides that only the
