@@ -391,6 +391,33 @@ def test_grouped_tiles_of_many_rows(G, op, kind, out, sizes, K, N):
     run_grouped(G, op, sizes, 1, 2, K, N, kind, out, pad=7 if K % 8 else 8, seed=2)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("op", [0, 1])
+def test_grouped_few_tails(G, op, kind):
+    """The last unit of the inner size and the last columns overlap those before them: infinities in
+    what is read twice come out as such, and not as NaN."""
+    import torch
+    note("grouped few tails op=%d %s" % (op, kind))
+    for K, N in ((31, 63), (33, 64), (65, 65), (71, 66), (127, 100), (129, 127), (300, 129), (515, 70)):
+        ends, n, a, b = make_grouped(op, [5, 0, 20], 0, 0, K, N, kind, K)
+        a, b = np.abs(a) + 0.5, np.abs(b) + 0.5
+        if kind == "bf16":
+            a, b = bf16_round(a), bf16_round(b)
+        unit = 64 if kind == "bf16" else 32
+        k = max(0, (K - 1) // unit * unit - 1)  # the last one before the last unit
+        b[(0, k, -1) if op == 0 else (0, -1, k)] = np.inf  # one column of C
+        t = tdtype(kind)
+        C = G.gcn_gemm_grouped(op, dev(ends), rows(a, kind, 1, 1), dev(b).to(t), out_dtype=torch.float32)
+        want, mag = ref.grouped(op, ends, a, b)
+        col = np.zeros(N, bool)
+        col[-1] = True
+        got = back(C)
+        assert np.isposinf(got[:5, col]).all()
+        keep = np.ones_like(got, bool)
+        keep[:5, col] = False
+        within(got[keep], want[keep], ref.grouped_bound(want[keep], mag[keep], K, "f32"), "C")
+
+
 # Rows of a few large tiles, by 16 and by 32, deep and shallow.
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("op", [0, 1])
