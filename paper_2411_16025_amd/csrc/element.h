@@ -48,6 +48,18 @@ __device__ inline u4 load_piece(const T* row, int f, int F) {
   return r;
 }
 
+// A piece's elements moved down by n (at least 0), zeros behind them.
+template <class T>
+__device__ inline u4 move_down(u4 v, int n) {
+  const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+  constexpr int kHalf = kPiece<T> / 2;
+  const int bits = 8 * (int)sizeof(T) * (n & (kHalf - 1));
+  const uint64_t a = n & kHalf ? hi : lo, b = n & kHalf ? 0 : hi;
+  uint64_t x = a >> bits | (bits ? b << (64 - bits) : 0), y = b >> bits;
+  if (n >= kPiece<T>) x = y = 0;
+  return u4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)};
+}
+
 template <class T>
 __device__ inline void unpack(u4 r, float (&v)[kPiece<T>]) {
 #pragma unroll

@@ -83,16 +83,6 @@ struct Tile {
   }
 };
 
-// A piece's elements moved down by n (of 2 bytes), zeros behind them.
-__device__ inline u4 move_down(u4 v, int n) {
-  const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
-  const int bits = 16 * (n & 3);
-  const uint64_t a = n & 4 ? hi : lo, b = n & 4 ? 0 : hi;
-  uint64_t x = a >> bits | (bits ? b << (64 - bits) : 0), y = b >> bits;
-  if (n >= 8) x = y = 0;
-  return u4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)};
-}
-
 // The pieces of an operand that a thread brings to LDS: their offsets in memory from the
 // operand's first element of a stage. DIRECT: rows start on 16 bytes and hold whole
 // pieces, and the loads go to LDS themselves. Else through registers, without a branch between
@@ -169,7 +159,7 @@ struct Loader {
         u4 x = v[p];
         if (!whole) {
           const int64_t over = (KC ? element_of(p) - had : (int64_t)element_of(p) - have) + 8;
-          x = move_down(x, (int)std::min<int64_t>(8, std::max<int64_t>(0, over)));
+          x = move_down<bf16>(x, (int)std::min<int64_t>(8, std::max<int64_t>(0, over)));
           if (!KC && line_of(p) >= had) x = u4{0, 0, 0, 0};
         }
         *reinterpret_cast<u4*>(lds + (threadIdx.x + p * NT) * 16) = x;
