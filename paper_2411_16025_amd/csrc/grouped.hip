@@ -314,12 +314,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_few(GroupArgs a) {
 // 27.5 in tiles, 1024 rows 31.8 and 28.3; fp32 1024 rows 90 and 122, 2048 rows 147 and 123. And rows
 // that are few large tiles, which would leave most CUs without work (4 groups of 433 rows,
 // 1712 x 256: fp32 18 us and 81, bf16 9 and 18; 2,500 rows of 2, 1024 x 512: 48 and 53, 21 and 30;
-// but 4,000 rows, 512 x 512, in 132 tiles: 36 and 31, 19 and 15; and more rows would read
-// B more often: 13,080 rows of 2, 3568 x 40: 145 and 122, 83 and 45).
+// 6,865 rows of 4, 3728 x 59 fp32: 79 and 135; but 4,000 rows, 512 x 512, in 132 tiles: 36 and 31,
+// 19 and 15; and more rows would read B more often: 13,080 rows of 2, 3568 x 40: 145 and 122, bf16
+// 83 and 45).
 bool few_takes(const Groups& g, int64_t N, int dtype) {
   const int64_t tiles = group_slots(g, 128) * ceil_div(N, (int64_t)128);
   return g.rows <= (dtype == GCN_DT_F32 ? 96 : 48) * (int64_t)g.n ||
-         (tiles < 110 && g.rows <= 4096);
+         (tiles < 110 && g.rows <= (dtype == GCN_DT_F32 ? 8192 : 4096));
 }
 
 template <class T, class TC, int R, int W>

@@ -372,7 +372,7 @@ def test_grouped_weight_gradients(G, kind, sizes, K, N):
     run_grouped(G, 2, sizes, 3, 1, K, N, kind, "f32", pad=8 if K % 8 == 0 else 1, seed=3)
 
 
-# More rows than the kernel of few rows takes (4096): the same shapes of tiles, and the general product
+# More rows than the kernel of few rows takes (4096, fp32 8192): the same shapes of tiles, and the general product
 # (bf16 widths below 8).
 @pytest.mark.parametrize("kind,out,sizes,K,N", [
     ("bf16", "bf16", [2700, 300, 0, 1520], 1032, 264), ("bf16", "f32", [2257, 2512], 1024, 520),
@@ -384,7 +384,9 @@ def test_grouped_weight_gradients(G, kind, sizes, K, N):
     ("bf16", "bf16", [70] * 64, 72, 200), ("bf16", "f32", [0, 64] * 70, 1, 1),
     ("f32", "f32", [2400, 2300], 33, 100), ("f32", "f32", [2400, 1900], 50, 160),
     ("f32", "f32", [4300, 3], 20, 20), ("f32", "f32", [3, 0, 4300], 21, 60),
-    ("f32", "f32", [110] * 64, 1, 1)])
+    ("f32", "f32", [110] * 64, 1, 1), ("f32", "f32", [8400, 3], 20, 20),
+    ("f32", "f32", [3, 0, 8300], 21, 60), ("f32", "f32", [5000, 3400], 33, 100),
+    ("f32", "f32", [5000, 3400], 50, 160), ("f32", "f32", [140] * 64, 1, 1)])
 @pytest.mark.parametrize("op", [0, 1])
 def test_grouped_tiles_of_many_rows(G, op, kind, out, sizes, K, N):
     note("grouped tiles of many rows op=%d %s sizes=%s K=%d N=%d" % (op, kind, sizes[:4], K, N))
@@ -430,9 +432,9 @@ def test_grouped_few_tiles(G, op, kind, sizes, K, N):
 
 @pytest.mark.parametrize("kind", KINDS)
 def test_matrix_rows_far_apart(G, kind):
-    """A matrix whose rows are 2^22 elements apart: the general product, rows behind the first 4096."""
+    """A matrix whose rows are 2^22 elements apart: the general product."""
     import torch
-    n, K, N, ld = 4200, 12, 24, 1 << 22
+    n, K, N, ld = 8300, 12, 24, 1 << 22
     note("matrix rows far apart %s" % kind)
     flat = torch.empty((N - 1) * ld + K, dtype=tdtype(kind), device="cuda:0")
     far = torch.as_strided(flat, (1, N, K), (0, ld, 1))
