@@ -573,8 +573,8 @@ extern "C" gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void*
     set_error("at least one of dX, dgamma and dbeta must be non-NULL");
     return GCN_EINVAL;
   }
-  if (work && !work_bytes) {
-    set_error("work memory needs work_bytes");
+  if (work && (!work_bytes || reinterpret_cast<uintptr_t>(work) % 256 != 0)) {
+    set_error("work memory needs work_bytes and an alignment of 256 bytes");
     return GCN_EINVAL;
   }
   hipStream_t s = (hipStream_t)stream;

@@ -808,6 +808,30 @@ def test_norm_in_given_memory(G, n, F):
     assert bool((work[need.value:] == 0xA5).all())
 
 
+def test_captured_without_memory_refused(G):
+    """A captured call that would need the library's temporaries is refused before it launches."""
+    import torch
+    note("captured without memory")
+    n, F = 5000, 64
+    x, y = dev(values(1, n, F, "f32")), dev(values(2, n, F, "f32"))
+    ends = dev(np.array([0, n], np.int64))
+    dw, dx, dg, db = (torch.full(s, 7.0, device="cuda:0") for s in ((1, F, F), (n, F), (F,), (F,)))
+    L, mark = G.lib(), torch.zeros(4, device="cuda:0")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        mark.add_(1)
+        s = torch.cuda.current_stream().cuda_stream
+        a = L.gcn_gemm_grouped(G.GCN_GEMM_TN, 1, ends.data_ptr(), n, F, F, x.data_ptr(), F, y.data_ptr(),
+                               F, 0, dw.data_ptr(), F, 0, F * F, None, None, s)
+        b = L.gcn_layernorm_affine_bwd(n, F, x.data_ptr(), F, 0, None, 1e-5, None, y.data_ptr(), F,
+                                       dx.data_ptr(), F, dg.data_ptr(), db.data_ptr(), None, None, s)
+    assert (a, b) == (5, 5)  # GCN_ESTATE
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(bool((t == 7).all()) for t in (dw, dx, dg, db)) and bool((mark == 1).all())
+
+
 def test_layer_on_two_streams(G):
     """Two layers at once on streams of their own, each with its own temporaries."""
     import torch

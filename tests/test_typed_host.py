@@ -109,6 +109,10 @@ def test_gemm_grouped_refusals(L):
     assert f(rows=1 << 31) == ERANGE
     assert f(rows=0) == 0  # no rows: nothing to write
     assert f(work=FAKE) == EINVAL
+    some = ctypes.c_int64(1 << 30)
+    assert f(work=ctypes.c_void_p(0x1010), size=ctypes.byref(some)) == EINVAL  # 256-byte aligned
+    assert L.gcn_layernorm_affine_bwd(4, 8, FAKE, 8, 0, None, 1e-5, None, ctypes.c_void_p(0x2000), 8, FAKE, 8,
+                                      None, None, ctypes.c_void_p(0x1010), ctypes.byref(some), None) == EINVAL
     # what a call would use: nothing for rows times a matrix, the chunks' sums for a weight gradient
     size = ctypes.c_int64(-1)
     assert f(size=ctypes.byref(size)) == 0 and size.value == 0
