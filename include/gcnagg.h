@@ -420,6 +420,9 @@ gcn_status gcn_dropout(int64_t n, int64_t F, const void* X, int64_t ldx, int dty
  *  X, Y      [n x F] of type dtype (GCN_DT_F32 or GCN_DT_BF16), n < 2^31, F <= 2^30;
  *            Y may be X itself (same ld), and may not overlap it otherwise.
  *  gamma, beta  fp32 [F], or NULL for 1 and 0.
+ *  eps       >= 0. A row whose var + eps lies below 2^-256 has no 1 / sqrt in
+ *            fp32's range (with eps = 0 a constant row, 0 / 0): what is computed
+ *            of it is infinite or NaN, also its part of dgamma.
  *  drop      NULL: no dropout; else as for gcn_dropout.
  * Asynchronous. Nothing is kept for the backward pass but X itself. */
 gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,

@@ -215,7 +215,9 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
     R::values(x, rx, a.F);
     R::values(g, rg, a.F);
     if (KEEP) load(i + step);
-    const float rstd = R::center(x, a.F, a.eps, red);
+    float rstd = R::center(x, a.F, a.eps, red);
+    // a slot without a row has zeros, no deviation and with eps = 0 no root: nothing of it counts
+    if (R::kSlots > 1) rstd = i < a.n ? rstd : 0.f;
     if (!KEEP) R::weights(gamma, a.gamma, 1.f, a.F);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(threads_of(G)) void k_norm_bwd(NormArgs a) {
       if (DROP) drop_piece<V>(a.drop, call, (uint32_t)i, R::column(j), g[j]);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[j][e] *= rstd;  // H; G is 0 behind the rows and the row
+        x[j][e] *= rstd;  // H; G and H are 0 behind the rows, G behind the row
         sg[j][e] = __builtin_fmaf(g[j][e], x[j][e], sg[j][e]);
         sb[j][e] += g[j][e];
         g[j][e] *= gamma[j][e];  // T
