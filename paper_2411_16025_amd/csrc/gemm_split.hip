@@ -688,6 +688,34 @@ bool gemm_split_tn_takes(int64_t M, int64_t N, int64_t K, int64_t lda, int64_t l
 
 namespace {
 
+// Rows of a chunk of A^T B (M x N, K rows, so many tiles): at most those after which the sums are as
+// close to 64 bits as the fp32 instruction's were in chunks of `most` rows (1024, or more where C
+// has many tiles and K many rows): 1408 rows here are like 1024 there (300 x 300
+// x 500,000 in 1312 rows 5.9e-7 against 6.1e-7; in 1968 rows 7.0e-7). And 1024 for small
+// outputs, 2048 for most, so that long sums stay below that (256 x 96 x 2.45M
+// 6.5e-7 against 7.2e-7; 512 x 256 7.4e-7 against 11.7e-7). A multiple of 512
+// workgroups, a fixed count so that the order of the sums does not depend on
+// the device. longest: 8192, or of products by group 2048, whose last chunks are of any length
+// (60,000 rows of 3 groups, 4096 x 2048: 9.99 ms in chunks of 7504, 6.50 in 2000).
+struct TnChunk {
+  int64_t most, rows;
+};
+
+TnChunk tn_chunk(int64_t M, int64_t N, int64_t K, int64_t tiles, int64_t longest) {
+  const int64_t fp32_tiles = ceil_div(M, (int64_t)128) * ceil_div(N, (int64_t)(N <= 64 ? 64 : 128));
+  int64_t most = 8192;
+  while (most > 1024 && fp32_tiles * ceil_div(K, most) < 4096) most /= 2;
+  const int64_t rows = std::min<int64_t>(
+      M * N <= 32768 ? 1024 : (M * N <= 262144 ? 2048 : longest), most + most * 3 / 8);
+  const int64_t rounds = std::max<int64_t>(1, ceil_div(K * tiles, (int64_t)512 * rows));
+  const int64_t want = std::max<int64_t>(1, 512 * rounds / tiles);
+  // Short sums are chains of steps: at least 64 rows (3,000 x 64 x 10: 17.6 us with
+  // 256, 11.9; 128 for outputs whose partials take longer to add, 512 x 256: 25 and 22).
+  const int64_t least = M * N <= 32768 ? 64 : 128;
+  return {most, std::max<int64_t>(
+                    least, std::min(rows, ceil_div(ceil_div(K, want), (int64_t)kKs) * kKs))};
+}
+
 template <bool BT>
 hipError_t launch_split_tall(const TallArgs& a, int per, hipStream_t stream) {
   auto go = [&](auto kern, int threads, int64_t rows) {
@@ -737,26 +765,7 @@ gcn_status gemm_split_tn(int64_t M, int64_t N, int64_t K, const float* A, int64_
   const int64_t tm = wide ? 256 : 128;
   const int64_t tn = wide ? 256 : (N <= 32 ? 32 : (N <= 64 ? 64 : 128));
   const int64_t m_tiles = ceil_div(M, tm), n_tiles = ceil_div(N, tn), tiles = m_tiles * n_tiles;
-  // Rows of a chunk: at most those after which the sums are as close to 64 bits as
-  // the fp32 instruction's were in chunks of `most` rows (1024, or more where C
-  // has many tiles and K many rows): 1408 rows here are like 1024 there (300 x 300
-  // x 500,000 in 1312 rows 5.9e-7 against 6.1e-7; in 1968 rows 7.0e-7). And 1024 for small
-  // outputs, 2048 for most, so that long sums stay below that (256 x 96 x 2.45M
-  // 6.5e-7 against 7.2e-7; 512 x 256 7.4e-7 against 11.7e-7). A multiple of 512
-  // workgroups, a fixed count so that the order of the sums does not depend on
-  // the device.
-  const int64_t fp32_tiles = ceil_div(M, (int64_t)128) * ceil_div(N, (int64_t)(N <= 64 ? 64 : 128));
-  int64_t most = 8192;
-  while (most > 1024 && fp32_tiles * ceil_div(K, most) < 4096) most /= 2;
-  const int64_t rows = std::min<int64_t>(
-      M * N <= 32768 ? 1024 : (M * N <= 262144 ? 2048 : 8192), most + most * 3 / 8);
-  const int64_t rounds = std::max<int64_t>(1, ceil_div(K * tiles, (int64_t)512 * rows));
-  const int64_t want = std::max<int64_t>(1, 512 * rounds / tiles);
-  // Short sums are chains of steps: at least 64 rows (3,000 x 64 x 10: 17.6 us with
-  // 256, 11.9; 128 for outputs whose partials take longer to add, 512 x 256: 25 and 22).
-  const int64_t least = M * N <= 32768 ? 64 : 128;
-  const int64_t split =
-      std::max<int64_t>(least, std::min(rows, ceil_div(ceil_div(K, want), (int64_t)kKs) * kKs));
+  const auto [most, split] = tn_chunk(M, N, K, tiles, 8192);
   const int64_t chunks = ceil_div(K, split);
   // The partials take about the memory of those of `most` rows (at most 1.3 times
   // it), or of 512 workgroups (134 MB), if that is more: a workgroup adds up several
@@ -841,16 +850,12 @@ gcn_status gemm_split_grouped(int op, const Groups& g, int64_t N, int64_t K, con
 gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const float* A, int64_t lda,
                                  const float* B, int64_t ldb, float* C, int64_t ldc,
                                  int64_t stride_w, Scratch* scratch, hipStream_t stream) {
-  // tiles and chunks as in gemm_split_tn; chunks of at most 2048 rows
+  // tiles and chunks as in gemm_split_tn
   const bool wide = K > 128 && N > 128 && g.rows / g.n >= 2048 && g.rows >= 131072;
   const int64_t tm = wide ? 256 : 128;
   const int64_t tn = wide ? 256 : (N <= 32 ? 32 : (N <= 64 ? 64 : 128));
   const int64_t m_tiles = ceil_div(K, tm), n_tiles = ceil_div(N, tn), tiles = m_tiles * n_tiles;
-  const int64_t rounds = std::max<int64_t>(1, ceil_div(g.rows * tiles, (int64_t)512 * 2048));
-  const int64_t want = std::max<int64_t>(1, 512 * rounds / tiles);
-  const int64_t least = K * N <= 32768 ? 64 : 128;
-  const int64_t split = std::max<int64_t>(
-      least, std::min<int64_t>(2048, ceil_div(ceil_div(g.rows, want), (int64_t)kKs) * kKs));
+  const int64_t split = tn_chunk(K, N, g.rows, tiles, 2048).rows;
   const int64_t slots = group_slots(g, split);
   const int64_t parts = g.rows / split;
   const int64_t blocks = tiles * ceil_div(slots, (int64_t)8) * 8;

@@ -373,7 +373,8 @@ gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
 // Partial sum p (blockIdx.y) belongs to the last group that begins in chunk p of all rows or
 // before it, if that has so many: a group of several chunks reaches the next multiple of
 // `split`. The workgroups of a group's partial sums share its elements, each element
-// the sum of all of them in chunk order.
+// the sum of all of them in chunk order, in double: the chain of 1276 partial sums of
+// 2,449,029 x 256 x 96 in fp32 made 9.3e-7 of 6.5e-7.
 constexpr int kAhead = 16;  // loads on their way at a time
 
 __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t split, int64_t K,
@@ -388,7 +389,7 @@ __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t spli
   for (int64_t t = ((p - p0) * gridDim.x + blockIdx.x) * kThreads + threadIdx.x; t < K * N;
        t += more * gridDim.x * kThreads) {
     float* c = C + t / N * ldc + t % N;
-    float s = *c;
+    double s = *c;
     const float* q = part + t;
     int64_t j = 0;
     for (; j + kAhead <= more; j += kAhead, q += kAhead * K * N) {
@@ -396,10 +397,10 @@ __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t spli
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) v[i] = q[i * K * N];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) s += v[i];
+      for (int i = 0; i < kAhead; ++i) s += (double)v[i];
     }
-    for (; j < more; ++j, q += K * N) s += *q;
-    *c = s;
+    for (; j < more; ++j, q += K * N) s += (double)*q;
+    *c = (float)s;
   }
 }
 

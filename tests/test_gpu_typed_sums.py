@@ -45,3 +45,44 @@ def test_layernorm_without_eps(G, n, F, kind):
         within(back(dX), dx, bx, "dX")
         within(back(dgamma), dg, bg, "dgamma")
         within(back(dbeta), db, bb, "dbeta")
+
+
+# ---- weight gradients of many rows -------------------------------------------------------
+
+
+def product64(x, dy, step=100000):
+    """x^T dy in 64 bits, by pieces of the rows, on the GPU."""
+    import torch
+    c = torch.zeros(x.shape[1], dy.shape[1], dtype=torch.float64, device="cuda:0")
+    for i in range(0, x.shape[0], step):
+        c += x[i:i + step].double().t().contiguous() @ dy[i:i + step].double()
+    return c
+
+
+@pytest.mark.parametrize("n,K,N", [(2449029, 256, 96), (1000000, 256, 96), (500000, 300, 300),
+                                   (500000, 512, 256), (300000, 70, 65)])
+def test_weight_gradients_as_close_as_one_product(G, n, K, N):
+    """gcn_gemm_f32's sums: a group's weight gradient is as close to 64 bits (in the matrices' norm) as
+    that product of all rows; 5% for another order of the partial sums. Of a part of the rows too, against the
+    product of all: in chunks of r rows each element of a chunk's sum has an error e(r) of its own
+    sign, so that m chunks have e(r) sqrt(m) and the result, of independent terms, grows as sqrt(m) as
+    well: the ratio is the chunk's, whatever m is."""
+    import torch
+    note("dW precision n=%d %dx%d" % (n, K, N))
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(n + K)
+    x = torch.randn(n, K, generator=gen, device="cuda:0")
+    dy = torch.randn(n, N, generator=gen, device="cuda:0")
+    cut = n // 3 + 7
+    ends = torch.tensor([0, n, n], device="cuda:0"), torch.tensor([0, cut, n], device="cuda:0")
+    err = lambda c, want: float((c.double() - want).norm() / want.norm())  # noqa: E731
+    want = product64(x, dy)
+    most = err(G.gcn_gemm_f32(G.GCN_GEMM_TN, x, dy), want)
+    one = G.gcn_gemm_grouped(G.GCN_GEMM_TN, ends[0], x, dy)
+    note("dW error %.3e, one product %.3e" % (err(one[0], want), most))
+    assert err(one[0], want) <= 1.05 * most and not one[1].any()
+    two = G.gcn_gemm_grouped(G.GCN_GEMM_TN, ends[1], x, dy)
+    for c, rows_ in ((two[0], slice(0, cut)), (two[1], slice(cut, n))):
+        want = product64(x[rows_], dy[rows_])
+        note("dW error of a part %.3e" % err(c, want))
+        assert err(c, want) <= 1.05 * most
