@@ -469,8 +469,8 @@ struct TnArgs {
   int64_t ldb;
   float* part;  // [groups][M][N]
   int m_tiles, n_tiles;
-  Groups by;    // products by group: chunks of a group's rows (groups.h), the first one's sums
-  float* C;     // in C + g stride_c, those of the others in part
+  Groups by;    // products by group: runs of chunks of a group's rows (groups.h), the first
+  float* C;     // one's sums in C + g stride_c, those of the others in part
   int64_t ldc, stride_c;
 };
 
@@ -480,7 +480,11 @@ struct TnArgs {
 // their loads were issued (PF = 1 where the accumulators leave no registers for two).
 // A is negated in every other chunk (see the head of this file). RUN: a workgroup
 // takes several chunks, one after the other, and adds their sums to its partial
-// C (without it the loop is gone, and with it the registers it costs).
+// C (without it the loop is gone, and with it the registers it costs). GROUPED: a run is of one
+// group, and as groups end inside runs, runs do not divide evenly among the XCDs: from
+// kSharedTiles tiles on each XCD takes an eighth of every run's.
+constexpr int kSharedTiles = 64;
+
 template <int WR, int WC, int RBW, int NBW, int PF, bool RUN, bool GROUPED = false>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
   constexpr int RB = WR * RBW, NB = WC * NBW, NT = 64 * WR * WC;
@@ -493,12 +497,17 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
   // same rows of A and B
   const int tiles = a.m_tiles * a.n_tiles;
   const int64_t idx = blockIdx.x >> 3;
-  const int tile = (int)(idx % tiles);
-  const int64_t group = idx / tiles * 8 + (blockIdx.x & 7);
+  int tile = (int)(idx % tiles);
+  int64_t group = idx / tiles * 8 + (blockIdx.x & 7);
+  if (GROUPED && RUN && tiles >= kSharedTiles) {
+    const int share = (tiles + 7) / 8;
+    tile = (int)(blockIdx.x & 7) * share + (int)(idx % share);
+    group = tile < tiles ? idx / share : a.groups;
+  }
   if (group >= a.groups) return;  // the whole workgroup
   GroupTile gt;
   if constexpr (GROUPED) {
-    gt = group_tile(a.by, group, (int)a.split);
+    gt = group_tile(a.by, group, (int)(a.split * a.run));
     if (gt.beg >= gt.end && (gt.beg != gt.first || gt.end < gt.first)) {
       // no chunk; but the first one of an empty group is its zeros
       if (gt.beg != gt.first) return;
@@ -526,10 +535,10 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
   auto sum_chunk = [&](int64_t chunk, bool add) {
     int64_t kb = chunk * a.split;
     int64_t ke = kb + a.split < a.K ? kb + a.split : a.K;
-    if constexpr (GROUPED) {
-      kb = gt.beg;
+    if constexpr (GROUPED) {  // (chunk: of the run)
+      kb = gt.beg + chunk * a.split;
       ke = kb + a.split < gt.end ? kb + a.split : gt.end;
-      chunk = (gt.beg - gt.first) / a.split;
+      chunk = (kb - gt.first) / a.split;
     }
     const float sign = chunk & 1 ? -kUp : kUp;
     float down = chunk & 1 ? -kDown : kDown;
@@ -613,7 +622,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
     int wm = m0 + wr * RBW * 32, wn = n0 + wc * NBW * 32, N = a.N;
     int64_t ldp = N;
     if constexpr (GROUPED) {
-      if (chunk == 0) {
+      if (gt.beg == gt.first) {
         part = a.C + gt.g * a.stride_c;
         ldp = a.ldc;
       } else {
@@ -658,11 +667,14 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_split_tn(TnArgs a) {
         }
       }
   };
-  if constexpr (RUN) {
+  if constexpr (RUN && GROUPED) {
+    for (int64_t c = 0; c < a.run && (c == 0 || gt.beg + c * a.split < gt.end); ++c)
+      sum_chunk(c, c > 0);
+  } else if constexpr (RUN) {
     const int64_t first = group * a.run;
     for (int64_t c = first; c < first + a.run && c < a.chunks; ++c) sum_chunk(c, c != first);
   } else {
-    sum_chunk(group, false);
+    sum_chunk(GROUPED ? 0 : group, false);
   }
 }
 
@@ -855,29 +867,37 @@ gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const fl
   const int64_t tm = wide ? 256 : 128;
   const int64_t tn = wide ? 256 : (N <= 32 ? 32 : (N <= 64 ? 64 : 128));
   const int64_t m_tiles = ceil_div(K, tm), n_tiles = ceil_div(N, tn), tiles = m_tiles * n_tiles;
-  const int64_t split = tn_chunk(K, N, g.rows, tiles, 2048).rows;
-  const int64_t slots = group_slots(g, split);
-  const int64_t parts = g.rows / split;
-  const int64_t blocks = tiles * ceil_div(slots, (int64_t)8) * 8;
+  const auto [most, split] = tn_chunk(K, N, g.rows, tiles, 2048);
+  // Runs as there, so that the partials take about as much memory as its (500,000 rows, 4096 x
+  // 4096: 4.1 GB instead of 16.4); but enough of them that they divide evenly, whatever lengths the
+  // groups' last ones have (200,000 rows of 3 groups, 1024 x 1024: 2.30 ms in 128 chunks, 2.54 in 64 runs).
+  const int64_t chunks = ceil_div(g.rows, split);
+  const int64_t run = std::max<int64_t>(
+      1, std::min(ceil_div(chunks * most - 3 * g.rows / 10, std::max<int64_t>(1, g.rows)),
+                  tiles >= kSharedTiles ? chunks * tiles / 2048 : chunks / 128));
+  const int64_t slots = group_slots(g, split * run);
+  const int64_t parts = g.rows / (split * run);
+  const int64_t blocks = run > 1 && tiles >= kSharedTiles ? ceil_div(tiles, (int64_t)8) * 8 * slots
+                                                          : tiles * ceil_div(slots, (int64_t)8) * 8;
   GCN_CHECK(launch_fits(blocks, 512));
   float* part = nullptr;
   if (parts > 0) GCN_CHECK(scratch->alloc(&part, parts * K * N, "grouped GEMM partials"));
   if (scratch->asked()) return GCN_OK;
-  const TnArgs a{(int)K, (int)N, 0, split, 0, 1, slots, A, lda, B, ldb, part, (int)m_tiles,
+  const TnArgs a{(int)K, (int)N, 0, split, 0, run, slots, A, lda, B, ldb, part, (int)m_tiles,
                  (int)n_tiles, g, C, ldc, stride_w};
-  auto go = [&](auto kern, int threads) {
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), 0, stream, a);
+  auto go = [&](auto kern, auto kern_run, int threads) {
+    hipLaunchKernelGGL(run > 1 ? kern_run : kern, dim3((unsigned)blocks), dim3(threads), 0, stream, a);
   };
   if (wide)
-    go(k_split_tn<4, 2, 2, 4, 1, false, true>, 512);
+    go(k_split_tn<4, 2, 2, 4, 1, false, true>, k_split_tn<4, 2, 2, 4, 1, true, true>, 512);
   else if (tn == 128)
-    go(k_split_tn<2, 2, 2, 2, 2, false, true>, 256);
+    go(k_split_tn<2, 2, 2, 2, 2, false, true>, k_split_tn<2, 2, 2, 2, 2, true, true>, 256);
   else if (tn == 64)
-    go(k_split_tn<4, 1, 1, 2, 2, false, true>, 256);
+    go(k_split_tn<4, 1, 1, 2, 2, false, true>, k_split_tn<4, 1, 1, 2, 2, true, true>, 256);
   else
-    go(k_split_tn<4, 1, 1, 1, 2, false, true>, 256);
+    go(k_split_tn<4, 1, 1, 1, 2, false, true>, k_split_tn<4, 1, 1, 1, 2, true, true>, 256);
   GCN_HIP(hipGetLastError());
-  return parts > 0 ? sum_group_partials(g, split, K, N, part, C, ldc, stride_w, stream) : GCN_OK;
+  return parts > 0 ? sum_group_partials(g, split * run, K, N, part, C, ldc, stride_w, stream) : GCN_OK;
 }
 
 }  // namespace gcn

@@ -86,3 +86,34 @@ def test_weight_gradients_as_close_as_one_product(G, n, K, N):
         want = product64(x[rows_], dy[rows_])
         note("dW error of a part %.3e" % err(c, want))
         assert err(c, want) <= 1.05 * most
+
+
+def whole(gen, kind, *shape):
+    """Whole numbers from -3 to 3: sums of their products below 2^24 are exact in any order."""
+    import torch
+    return torch.randint(-3, 4, shape, generator=gen, device="cuda:0").to(tdtype(kind))
+
+
+def cuts(sizes):
+    return np.concatenate([[0], np.cumsum(sizes)]).astype(np.int64)
+
+
+# several chunks of a group: a workgroup for each, and runs of them, by tiles shared among the XCDs and not
+@pytest.mark.parametrize("kind,sizes,K,N", [
+    ("f32", [140000, 5], 136, 132), ("f32", [9000, 2500, 0], 40, 70), ("f32", [120000], 256, 96),
+    ("f32", [30011, 0, 5, 31984], 2047, 2050), ("f32", [70001, 129999], 1024, 1024),
+    ("f32", [100003, 0, 100000], 8192, 64), ("f32", [150000, 50010], 8200, 32),
+    ("bf16", [140000, 5], 136, 132), ("bf16", [9000, 2500, 0], 40, 70), ("bf16", [70001, 9], 520, 264),
+    ("bf16", [70001, 0, 30000], 515, 517), ("bf16", [200003], 64, 64)])
+def test_weight_gradients_exact(G, kind, sizes, K, N):
+    """No row, chunk or operand part is lost, doubled or misplaced."""
+    import torch
+    note("dW exact %s sizes=%s K=%d N=%d" % (kind, sizes, K, N))
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(K)
+    n, ends = sum(sizes), cuts(sizes)
+    x, dy = whole(gen, kind, n, K), whole(gen, kind, n, N)
+    got = G.gcn_gemm_grouped(G.GCN_GEMM_TN, dev(ends), x, dy)
+    for g in range(len(sizes)):
+        r = slice(int(ends[g]), int(ends[g + 1]))
+        assert torch.equal(got[g].double(), product64(x[r], dy[r])), g

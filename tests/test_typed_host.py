@@ -121,3 +121,15 @@ def test_gemm_grouped_refusals(L):
     assert size.value % (256 * 256 * 4) == 0 and size.value > 0
     less = ctypes.c_int64(size.value - 256)
     assert f(work=FAKE, size=ctypes.byref(less), **big) == EINVAL
+
+
+@pytest.mark.parametrize("rows,K,N,most", [
+    (2449029, 512, 256, 350e6),     # 637 runs of two chunks
+    (500000, 4096, 4096, 4.2e9),    # about 8192 rows to a run, 64 MB each
+    (65536, 4096, 14336, 2.0e9), (131072, 16384, 16384, 18e9), (500000, 256, 256, 134e6)])
+def test_grouped_weight_gradients_memory(L, rows, K, N, most):
+    """The partial sums of fp32 weight gradients take about as much memory as those of the ungrouped product."""
+    size = ctypes.c_int64(-1)
+    assert L.gcn_gemm_grouped(2, 4, FAKE, rows, N, K, FAKE, K, FAKE, N, 0, FAKE, N, 0, K * N, None,
+                              ctypes.byref(size), None) == 0
+    assert 0 < size.value <= most
