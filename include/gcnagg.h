@@ -365,8 +365,9 @@ gcn_status gcn_sage3_step(const gcn_graph* g, const float* X, int64_t ldx, int64
  *  A group without rows takes no part in NN and NT; in TN its C_g is zero.
  *  dtype     GCN_DT_F32 or GCN_DT_BF16: the type of A and B. dtype_c: that of C,
  *            GCN_DT_F32 or, for NN and NT, that of A and B (rounded once).
- *            Products and sums as in gcn_gemm_f32 for fp32 operands; exact
- *            products and fp32 sums for bf16 ones.
+ *            fp32 operands: exactly split into three bf16 parts as in gcn_gemm_f32, at
+ *            any K and as close to the exact result as its products are; of few rows
+ *            on the fp32 matrix instruction. bf16: exact products and fp32 sums.
  *  lda, ldb, ldc  row strides; stride_w: elements from one group's matrix to the
  *            next one's, of B in NN and NT (>= 0; 0: one matrix for all), of C in
  *            TN (at least (K - 1) ldc + N). C may not overlap A or B.

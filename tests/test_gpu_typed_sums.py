@@ -117,3 +117,76 @@ def test_weight_gradients_exact(G, kind, sizes, K, N):
     for g in range(len(sizes)):
         r = slice(int(ends[g]), int(ends[g + 1]))
         assert torch.equal(got[g].double(), product64(x[r], dy[r])), g
+
+
+# ---- long inner sizes ----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("n,K,N,positive", [(8300, 5000, 160, False), (8300, 20000, 160, True),
+                                            (8300, 20003, 130, False), (8300, 300007, 160, True),
+                                            (7000, 1200003, 160, True)])
+def test_long_inner_sizes(G, op, n, K, N, positive):
+    """fp32 products by group are as close to 64 bits as gcn_gemm_f32's, which takes the fp32
+    instruction there; also of positive operands, whose sums keep every bias (5% for another order)."""
+    import torch
+    note("long inner size op=%d K=%d positive=%d" % (op, K, positive))
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(K)
+    a = torch.randn(n, K, generator=gen, device="cuda:0")
+    b = torch.randn(2, K, N, generator=gen, device="cuda:0")
+    if positive:
+        a.abs_().add_(0.5)
+        b.abs_().add_(0.5)
+    ends = torch.tensor([0, n - 3000, n], device="cuda:0")
+    w = b if op == 0 else b.transpose(1, 2).contiguous()
+    got = G.gcn_gemm_grouped(op, ends, a, w)
+    for g, r in enumerate((slice(0, n - 3000), slice(n - 3000, n))):
+        want = torch.zeros(r.stop - r.start, N, dtype=torch.float64, device="cuda:0")
+        for k in range(0, K, 20000):
+            want += a[r, k:k + 20000].double() @ b[g, k:k + 20000].double()
+        err = lambda c: float((c.double() - want).norm() / want.norm())  # noqa: E731
+        one = err(G.gcn_gemm_f32(op, a[r].contiguous(), w[g]))
+        note("error %.3e, one product %.3e" % (err(got[r]), one))
+        assert err(got[r]) <= 1.05 * one
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("op", [0, 1])
+@pytest.mark.parametrize("n,K,N", [(8300, 4096, 160), (8300, 16384, 130), (8300, 16385, 160),
+                                   (40000, 32801, 256), (8300, 49153, 33), (9000, 20007, 300)])
+def test_long_inner_sizes_exact(G, op, kind, n, K, N):
+    """Whole numbers: nothing of the inner size is lost or taken twice, rows of no group are left."""
+    import torch
+    note("long inner size exact op=%d K=%d N=%d %s" % (op, K, N, kind))
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(K + N)
+    a, b = whole(gen, kind, n, K), whole(gen, kind, 2, K, N)
+    ends = [3, n // 2, n - 2]
+    w = b if op == 0 else b.transpose(1, 2).contiguous()
+    got = torch.full((n, N), 7.0, device="cuda:0")
+    G.gcn_gemm_grouped(op, dev(np.array(ends, np.int64)), a, w, got, out_dtype=torch.float32)
+    assert bool((got[:3] == 7.0).all()) and bool((got[n - 2:] == 7.0).all())
+    for g in range(2):
+        r = slice(ends[g], ends[g + 1])
+        want = torch.zeros(r.stop - r.start, N, dtype=torch.float64, device="cuda:0")
+        for k in range(0, K, 20000):
+            want += a[r, k:k + 20000].double() @ b[g, k:k + 20000].double()
+        assert torch.equal(got[r].double(), want), g
+
+
+def test_long_inner_size_special_values(G):
+    """Infinities and NaN of one piece of the inner size reach their own sums and no others."""
+    import torch
+    note("long inner size special values")
+    n, K, N = 8300, 33000, 140
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(1)
+    a, b = whole(gen, "f32", n, K), whole(gen, "f32", 1, K, N).abs() + 1
+    a[5, 20000], a[700, 3], a[700, 32999], a[8000, 16384] = np.inf, np.inf, -np.inf, np.nan
+    got = G.gcn_gemm_grouped(0, dev(np.array([0, n], np.int64)), a, b)
+    assert bool(torch.isposinf(got[5]).all())
+    assert bool(torch.isnan(got[700]).all()) and bool(torch.isnan(got[8000]).all())
+    rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
+    rest[[5, 700, 8000]] = False
+    assert torch.equal(got[rest].double(), a[rest].double() @ b[0].double())
