@@ -814,8 +814,8 @@ gcn_status gemm_split_tn(int64_t M, int64_t N, int64_t K, const float* A, int64_
 
 // ---- products by group -------------------------------------------------------------
 
-// Any inner size: gcn_gemm_f32 takes the fp32 instruction beyond 4096, which is no closer to 64 bits (300
-// columns and fewer, error in the norm here and there: normal operands, 20,003 2.3e-6 and 2.5e-6;
+// Any inner size: gcn_gemm_f32 takes the fp32 instruction beyond 4096, which is no closer to 64 bits
+// (errors in the norm here and there, 130 and 160 columns: normal operands, 20,003 2.3e-6 and 2.5e-6;
 // positive ones, whose sums keep the matrix core's bias, 20,000 1.2e-6 and 1.9e-6, 300,007
 // 7.6e-6 and 7.3e-6, 1,200,003 1.43e-5 and 1.46e-5).
 bool gemm_split_grouped_takes(int op, int64_t N, int64_t K, int64_t lda, int64_t ldb, int64_t ldc) {

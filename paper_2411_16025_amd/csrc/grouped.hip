@@ -23,7 +23,8 @@ struct GroupArgs {
 };
 
 // The general kernel: one 64 x 64 tile of C per workgroup, fp32 products, any
-// type, size and alignment.
+// type, size and alignment. The tiles lie along the grid's first axis, which alone takes all that a
+// launch does.
 constexpr int kTile = 64, kDepth = 16;
 
 template <class T, class TC, int OP>
@@ -33,18 +34,21 @@ __global__ __launch_bounds__(kThreads) void k_grouped(GroupArgs a) {
   const T* B = static_cast<const T*>(a.B);
   TC* C = static_cast<TC*>(a.C);
   const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
-  const int n0 = blockIdx.y * kTile;
+  const uint32_t col_tiles = (a.N + kTile - 1) / kTile;
+  const uint32_t tile = blockIdx.x / col_tiles;
+  const int n0 = (int)(blockIdx.x % col_tiles) * kTile;
   int64_t i0 = 0;  // first row of C
   int64_t m_end, k0 = 0, k1 = a.K;
   if constexpr (OP == GCN_GEMM_TN) {
-    const int g = blockIdx.x;
+    const uint32_t row_tiles = (a.K + kTile - 1) / kTile;
+    const int g = (int)(tile / row_tiles);
     k0 = group_offset(a.by, g);
     k1 = group_offset(a.by, g + 1);
-    i0 = (int64_t)blockIdx.z * kTile;
+    i0 = (int64_t)(tile % row_tiles) * kTile;
     m_end = a.K;
     C += g * a.stride_w;
   } else {
-    const GroupTile gt = group_tile(a.by, blockIdx.x, kTile);
+    const GroupTile gt = group_tile(a.by, tile, kTile);
     i0 = gt.beg;
     m_end = gt.end;
     if (i0 >= m_end) return;
@@ -353,19 +357,19 @@ gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
 
 template <class T, class TC>
 gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
-  const unsigned cols = (unsigned)ceil_div((int64_t)a.N, (int64_t)kTile);
-  if (op == GCN_GEMM_TN) {
-    ProfScope ps("grouped_tn", s);
-    const dim3 grid((unsigned)a.by.n, cols, (unsigned)ceil_div((int64_t)a.K, (int64_t)kTile));
+  const bool tn = op == GCN_GEMM_TN;
+  const int64_t blocks = ceil_div((int64_t)a.N, (int64_t)kTile) *
+                         (tn ? a.by.n * ceil_div((int64_t)a.K, (int64_t)kTile)
+                             : group_slots(a.by, kTile));
+  GCN_CHECK(launch_fits(blocks, kThreads));
+  const dim3 grid((unsigned)blocks);
+  ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
+  if (tn)
     hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_TN>), grid, dim3(kThreads), 0, s, a);
-  } else {
-    ProfScope ps(op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
-    const dim3 grid((unsigned)group_slots(a.by, kTile), cols);
-    if (op == GCN_GEMM_NN)
-      hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NN>), grid, dim3(kThreads), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NT>), grid, dim3(kThreads), 0, s, a);
-  }
+  else if (op == GCN_GEMM_NN)
+    hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NN>), grid, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NT>), grid, dim3(kThreads), 0, s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }

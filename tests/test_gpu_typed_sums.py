@@ -190,3 +190,30 @@ def test_long_inner_size_special_values(G):
     rest = torch.ones(n, dtype=torch.bool, device="cuda:0")
     rest[[5, 700, 8000]] = False
     assert torch.equal(got[rest].double(), a[rest].double() @ b[0].double())
+
+
+# ---- sizes of the general product ------------------------------------------------------------
+
+
+@pytest.mark.parametrize("op", [0, 1, 2])
+def test_more_columns_than_a_second_axis(G, op):
+    """More than 65,535 tiles of 64 columns (NN, TN) or rows of C (TN): bf16 rows of 2^22 elements and more
+    take the general product."""
+    import torch
+    wide = (1 << 22) + 70
+    note("general product, many tiles op=%d" % op)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(op)
+    if op == 2:  # both ways round
+        for K, N in ((wide, 3), (3, wide)):
+            x, dy = whole(gen, "bf16", 70, K), whole(gen, "bf16", 70, N)
+            got = G.gcn_gemm_grouped(2, dev(np.array([0, 30, 69], np.int64)), x, dy)
+            for g, r in enumerate((slice(0, 30), slice(30, 69))):
+                assert torch.equal(got[g], x[r].float().t().contiguous() @ dy[r].float())
+        return
+    n, K = 130, 9
+    a = whole(gen, "bf16", n, K)
+    b = whole(gen, "bf16", 1, K, wide) if op == 0 else whole(gen, "bf16", 1, wide, K)
+    got = G.gcn_gemm_grouped(op, dev(np.array([0, n], np.int64)), a, b, out_dtype=torch.float32)
+    want = a.float() @ (b[0].float() if op == 0 else b[0].float().t().contiguous())
+    assert torch.equal(got, want)

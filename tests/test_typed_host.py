@@ -133,3 +133,20 @@ def test_grouped_weight_gradients_memory(L, rows, K, N, most):
     assert L.gcn_gemm_grouped(2, 4, FAKE, rows, N, K, FAKE, K, FAKE, N, 0, FAKE, N, 0, K * N, None,
                               ctypes.byref(size), None) == 0
     assert 0 < size.value <= most
+
+
+def test_grouped_more_tiles_than_a_launch(L):
+    """Every kernel of the products refuses what one launch does not take before it starts."""
+    def f(op, G, rows, N, K, dt, lda=None, ldb=None):
+        ldb = ldb or (K if op == 1 else N)
+        return L.gcn_gemm_grouped(op, G, FAKE, rows, N, K, FAKE, lda or K, FAKE, ldb, dt, FAKE, N, 0,
+                                  K * N, None, None, None)
+    top = (1 << 31) - 1
+    for op in (0, 1):
+        assert f(op, 2, top, 4, 4, 1) == ERANGE              # bf16, the general product
+        assert f(op, 2, top, 4, 4, 0, lda=1 << 22) == ERANGE  # fp32 in rows far apart
+        assert f(op, 1, 1 << 20, 1 << 23, 4, 1) == ERANGE    # many columns
+        assert f(op, 2, top, 4096, 64, 1) == ERANGE and f(op, 2, top, 4096, 64, 0) == ERANGE
+    assert f(2, 65535, 100, 1 << 23, 4, 1) == ERANGE
+
+
