@@ -215,5 +215,6 @@ def test_more_columns_than_a_second_axis(G, op):
     a = whole(gen, "bf16", n, K)
     b = whole(gen, "bf16", 1, K, wide) if op == 0 else whole(gen, "bf16", 1, wide, K)
     got = G.gcn_gemm_grouped(op, dev(np.array([0, n], np.int64)), a, b, out_dtype=torch.float32)
-    want = a.float() @ (b[0].float() if op == 0 else b[0].float().t().contiguous())
-    assert torch.equal(got, want)
+    w = b[0].float() if op == 0 else b[0].float().t()
+    for c in range(0, wide, 1 << 20):  # (by pieces: the library's product of 2 GB leaves a part of it zero)
+        assert torch.equal(got[:, c:c + (1 << 20)], a.float() @ w[:, c:c + (1 << 20)].contiguous()), c
