@@ -20,11 +20,14 @@ struct GroupArgs {
   void* C;
   int64_t ldc;
   int64_t stride_w;
+  int64_t split = 0;      // TN: rows of a chunk (groups.h), the sums of a group's first one in C,
+  float* part = nullptr;  // of the others here
 };
 
 // The general kernel: one 64 x 64 tile of C per workgroup, fp32 products, any
 // type, size and alignment. The tiles lie along the grid's first axis, which alone takes all that a
-// launch does.
+// launch does. TN: a group's rows in chunks, so that a narrow C has workgroups (bf16, 500,000 rows of 4
+// groups, 256 x 4: 17.4 ms in one chunk each, 0.39 so).
 constexpr int kTile = 64, kDepth = 16;
 
 template <class T, class TC, int OP>
@@ -41,12 +44,19 @@ __global__ __launch_bounds__(kThreads) void k_grouped(GroupArgs a) {
   int64_t m_end, k0 = 0, k1 = a.K;
   if constexpr (OP == GCN_GEMM_TN) {
     const uint32_t row_tiles = (a.K + kTile - 1) / kTile;
-    const int g = (int)(tile / row_tiles);
-    k0 = group_offset(a.by, g);
-    k1 = group_offset(a.by, g + 1);
+    const int64_t slot = tile / row_tiles;
+    const GroupTile gt = group_tile(a.by, slot, (int)a.split);
+    if (gt.beg >= gt.end && gt.beg != gt.first) return;  // an empty group's first chunk: zeros
+    k0 = gt.beg;
+    k1 = std::min(gt.beg + a.split, gt.end);
     i0 = (int64_t)(tile % row_tiles) * kTile;
     m_end = a.K;
-    C += g * a.stride_w;
+    if (gt.beg == gt.first) {
+      C += gt.g * a.stride_w;
+    } else {
+      C = reinterpret_cast<TC*>(a.part) + (slot - gt.g - 1) * a.K * a.N;
+      a.ldc = a.N;
+    }
   } else {
     const GroupTile gt = group_tile(a.by, tile, kTile);
     i0 = gt.beg;
@@ -356,12 +366,29 @@ gcn_status few(int op, const GroupArgs& a, hipStream_t s) {
 }
 
 template <class T, class TC>
-gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
+gcn_status grouped(int op, GroupArgs a, Scratch* scratch, hipStream_t s) {
   const bool tn = op == GCN_GEMM_TN;
-  const int64_t blocks = ceil_div((int64_t)a.N, (int64_t)kTile) *
-                         (tn ? a.by.n * ceil_div((int64_t)a.K, (int64_t)kTile)
-                             : group_slots(a.by, kTile));
+  int64_t tiles = ceil_div((int64_t)a.N, (int64_t)kTile), slots, parts = 0;
+  if (tn) {
+    // four workgroups to a CU, chunks of 128 to 4096 rows (4096 where the groups' tiles are enough, longer
+    // for more than a launch would take); partial sums as in the other kernels
+    tiles *= ceil_div((int64_t)a.K, (int64_t)kTile);
+    GCN_CHECK(launch_fits(tiles, kThreads));
+    const int64_t even = ceil_div(ceil_div(a.by.rows * tiles, (int64_t)1024), (int64_t)kDepth) * kDepth;
+    a.split = std::max(a.by.n * tiles >= 512
+                           ? 4096
+                           : std::min<int64_t>(4096, std::max<int64_t>(128, even)),
+                       std::min(a.by.rows, ceil_div(a.by.rows * tiles, int64_t(1) << 22)));
+    slots = group_slots(a.by, a.split);
+    parts = a.by.rows / a.split;
+  } else {
+    slots = group_slots(a.by, kTile);
+  }
+  const int64_t blocks = tiles * slots;
   GCN_CHECK(launch_fits(blocks, kThreads));
+  if (parts > 0)
+    GCN_CHECK(scratch->alloc(&a.part, parts * a.K * a.N, "grouped GEMM partials"));
+  if (scratch->asked()) return GCN_OK;
   const dim3 grid((unsigned)blocks);
   ProfScope ps(tn ? "grouped_tn" : op == GCN_GEMM_NN ? "grouped_nn" : "grouped_nt", s);
   if (tn)
@@ -371,7 +398,9 @@ gcn_status grouped(int op, const GroupArgs& a, hipStream_t s) {
   else
     hipLaunchKernelGGL((k_grouped<T, TC, GCN_GEMM_NT>), grid, dim3(kThreads), 0, s, a);
   GCN_HIP(hipGetLastError());
-  return GCN_OK;
+  return parts > 0 ? sum_group_partials(a.by, a.split, a.K, a.N, a.part, static_cast<float*>(a.C),
+                                        a.ldc, a.stride_w, s)
+                   : GCN_OK;
 }
 
 // Partial sum p (blockIdx.y) belongs to the last group that begins in chunk p of all rows or
@@ -485,7 +514,7 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     return gemm_grouped_bf16(op, by, N, K, A, lda, B, ldb, C, ldc, dtype_c == GCN_DT_BF16, stride_w,
                              &scratch, s);
   }
-  if (scratch.asked()) return GCN_OK;
-  if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, s);
-  return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, s) : grouped<bf16, bf16>(op, a, s);
+  if (dtype == GCN_DT_F32) return grouped<float, float>(op, a, &scratch, s);
+  return dtype_c == GCN_DT_F32 ? grouped<bf16, float>(op, a, &scratch, s)
+                               : grouped<bf16, bf16>(op, a, &scratch, s);
 }

@@ -104,7 +104,9 @@ def cuts(sizes):
     ("f32", [30011, 0, 5, 31984], 2047, 2050), ("f32", [70001, 129999], 1024, 1024),
     ("f32", [100003, 0, 100000], 8192, 64), ("f32", [150000, 50010], 8200, 32),
     ("bf16", [140000, 5], 136, 132), ("bf16", [9000, 2500, 0], 40, 70), ("bf16", [70001, 9], 520, 264),
-    ("bf16", [70001, 0, 30000], 515, 517), ("bf16", [200003], 64, 64)])
+    ("bf16", [70001, 0, 30000], 515, 517), ("bf16", [200003], 64, 64),
+    ("bf16", [0, 70001, 0, 1, 30000], 256, 4), ("bf16", [150000, 7], 7, 130), ("bf16", [99999, 31], 1, 1),
+    ("bf16", [1000, 0, 2000] * 30, 70, 3)])
 def test_weight_gradients_exact(G, kind, sizes, K, N):
     """No row, chunk or operand part is lost, doubled or misplaced."""
     import torch

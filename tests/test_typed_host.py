@@ -150,3 +150,12 @@ def test_grouped_more_tiles_than_a_launch(L):
     assert f(2, 65535, 100, 1 << 23, 4, 1) == ERANGE
 
 
+
+
+def test_grouped_narrow_weight_gradients_are_cut(L):
+    """bf16 weight gradients of fewer than 8 columns have partial sums: several workgroups to a group."""
+    for K, N in ((256, 4), (4, 256), (1, 1)):
+        size = ctypes.c_int64(-1)
+        assert L.gcn_gemm_grouped(2, 4, FAKE, 500000, N, K, FAKE, K, FAKE, N, 1, FAKE, N, 0, K * N, None,
+                                  ctypes.byref(size), None) == 0
+        assert size.value >= 100 * 4 * K * N
