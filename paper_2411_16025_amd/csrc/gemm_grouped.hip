@@ -464,15 +464,17 @@ __global__ __launch_bounds__(256) void k_pad(Operand o, u4* out) {
 // padded with zeros to whole pieces, where the product is large against them: of odd sizes a
 // product runs at about 430 TFLOP/s through registers and 900 directly, and a copy moves 32
 // bytes a piece (32,768 rows of 16 groups, 2047 x 4093: 766 us, 1290 without). Without memory for
-// the copies it stays with the registers.
+// the copies it stays with the registers; meant: whether the sizes alone call for direct loads, so
+// that what decides the order of the sums does not depend on the memory.
 gcn_status make_direct(Operand* a, Operand* b, double work, Scratch* scratch, bool* direct,
-                       hipStream_t s) {
+                       bool* meant, hipStream_t s) {
   int64_t pieces = 0;
   for (Operand* o : {a, b})
     if (!o->direct()) pieces += o->pieces();
-  *direct = pieces == 0;
+  *direct = *meant = pieces == 0;
   if (*direct || work < 0x1p34 || work / 2048 < (double)pieces || pieces >= (int64_t(1) << 31))
     return GCN_OK;
+  *meant = true;
   u4* to = nullptr;
   if (scratch->alloc(&to, pieces, "aligned copies of operands") != GCN_OK) {
     clear_error();
@@ -513,8 +515,8 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
     ob.groups = stride_w == 0 ? 1 : g.n;
     ob.rows = op == GCN_GEMM_NT ? N : K;
   }
-  bool direct = false;
-  GCN_CHECK(make_direct(&oa, &ob, (double)g.rows * (double)N * (double)K, scratch, &direct, s));
+  bool direct = false, meant = false;
+  GCN_CHECK(make_direct(&oa, &ob, (double)g.rows * (double)N * (double)K, scratch, &direct, &meant, s));
   MulArgs a{};
   a.by = g;
   a.A = oa.p;
@@ -536,7 +538,7 @@ gcn_status gemm_grouped_bf16(int op, const Groups& g, int64_t N, int64_t K, cons
     // (65,536 rows of 64 groups, 256 x 256: 44 us, 53 without that bound; 32,768 of 8, 1024 x
     // 1024: 107 and 152; 65,536 of 8, 2048 x 4096: 1.35 ms and 1.57; but 500,000 of 4, 512 x 512:
     // 345 us and 320). 65536 rows bound the sums' chains.
-    const int64_t tile = direct && wide_tiles(g, N) ? 256 : 128, want = tile == 256 ? 240 : 480;
+    const int64_t tile = meant && wide_tiles(g, N) ? 256 : 128, want = tile == 256 ? 240 : 480;
     const int64_t tiles = ceil_div(K, tile) * ceil_div(N, tile);
     const double even = (double)g.rows * (double)tiles / (double)want;  // a chunk to each
     const double sums = std::sqrt(2e-4 * (double)g.rows * (double)K * (double)N);

@@ -220,3 +220,39 @@ def test_more_columns_than_a_second_axis(G, op):
     w = b[0].float() if op == 0 else b[0].float().t()
     for c in range(0, wide, 1 << 20):  # (by pieces: the library's product of 2 GB leaves a part of it zero)
         assert torch.equal(got[:, c:c + (1 << 20)], a.float() @ w[:, c:c + (1 << 20)].contiguous()), c
+
+
+# ---- memory ----------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("op,n,K,N", [(0, 2400, 2049, 4001), (1, 2400, 2049, 4001), (2, 70001, 515, 517),
+                                      (2, 2400, 2049, 4001), (2, 40000, 1025, 700)])
+def test_same_bits_without_copies(G, op, n, K, N):
+    """Large bf16 products of odd widths, with work memory for the aligned copies and with too little for
+    them: the same bits."""
+    import ctypes
+    import torch
+    note("same bits without copies op=%d %d %d %d" % (op, n, K, N))
+    t, L = torch.bfloat16, G.lib()
+    ends = dev(np.array([0, n * 7 // 12, n * 7 // 12, n], np.int64))
+    A = dev(values(50, n, K, "bf16")).to(t)
+    if op == 2:
+        B, C = dev(values(60, n, N, "bf16")).to(t), (3, K, N)
+    else:
+        w = np.random.default_rng(7).standard_normal((3, K, N) if op == 0 else (3, N, K))
+        B, C = dev(w.astype(np.float32)).to(t), (n, N)
+    pieces = sum(r * ((c + 7) // 8) for r, c in ((n, K), B.reshape(-1, B.shape[-1]).shape) if c % 8)
+
+    def call(out, work, size):
+        return L.gcn_gemm_grouped(op, 3, ends.data_ptr(), n, N, K, A.data_ptr(), K, B.data_ptr(),
+                                  B.shape[-1], 1, out.data_ptr(), N, 0, K * N, work, ctypes.byref(size),
+                                  torch.cuda.current_stream().cuda_stream)
+    need = ctypes.c_int64(-1)
+    got = [torch.full(C, 7.0, device="cuda:0") for _ in range(2)]
+    assert call(got[0], None, need) == 0
+    less = ctypes.c_int64(need.value - (16 * pieces + 255) // 256 * 256)
+    assert pieces > 0 and 0 <= less.value < 16 * pieces
+    work = torch.empty(need.value, dtype=torch.uint8, device="cuda:0")
+    assert call(got[0], work.data_ptr(), need) == 0
+    assert call(got[1], work.data_ptr(), less) == 0
+    assert torch.equal(*got)
