@@ -37,6 +37,12 @@
  *    256 MiB of it when the last graph on the device is freed. The partial rows
  *    of an aggregation, which come from the device's default memory pool, are
  *    given back with their graph.
+ *    While `stream` is captured, temporaries become memory nodes of the caller's
+ *    graph: gcn_gemm_f32 (TN), aggregations with chunked or column-blocked rows,
+ *    gcn_softmax_xent, gcn_gcn2_step and the gcn_sage3 calls have some. Two graphs
+ *    with such nodes, of other calls, ended in a GPU fault when they were replayed
+ *    in turn, and its cause is not known; no test captures the calls named here.
+ *    gcn_aggregate_fwd_noalloc, and the calls with work memory, record kernels only.
  */
 #ifndef GCNAGG_H
 #define GCNAGG_H

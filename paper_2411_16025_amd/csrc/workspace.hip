@@ -40,7 +40,9 @@ void dfree(void* p) {
 //    that the default pool holds nothing of a graph that was only built (what
 //    calls that promise to take nothing from it are measured by).
 //  * While a stream is being captured, its temporaries are nodes of the graph
-//    (hipMallocAsync / hipFreeAsync), as a graph may be replayed on any stream.
+//    (hipMallocAsync / hipFreeAsync), as a graph may be replayed on any stream. Two
+//    graphs with such nodes ended in a GPU fault when they were replayed in turn, its
+//    cause unknown: newer calls take the caller's memory then (scratch.h).
 //  * At most a quarter of the device's memory is kept idle (or GCN_IDLE_MAX bytes,
 //    if that is less when a graph is built), the oldest blocks going first; all of
 //    it is given back when an allocation fails, and all but kKeepIdle when the
