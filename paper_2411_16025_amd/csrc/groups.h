@@ -134,6 +134,9 @@ __device__ inline TileCount count_tiles(const Groups& a, int R, int least) {
       c.end = group_offset(a, lane * per + i + 1);
       mine += tiles_of(c.end - c.first, R, least);
     }
+  // All groups' tiles are fewer than 2^24 + n (R >= 128, or few rows); of offsets that decrease, whose
+  // groups overlap, no more are counted than an int holds.
+  mine = min(mine, (1 << 25) - 1);
   const int upto = wave_inclusive(mine);
   c.before = upto - mine;
   c.total = __builtin_amdgcn_readlane(upto, 63);

@@ -125,6 +125,13 @@ def test_dropout(model, n, F, dt):
         model("dropout", n, F, dt, pad)
 
 
+@pytest.mark.parametrize("groups,rows,R", [(1024, 1610612736, 128), (1024, (1 << 31) - 1, 128), (1000, 1 << 30, 128),
+                                           (1023, 300000, 256), (64, 5000, 16)])
+def test_tiles_of_overlapping_groups(model, groups, rows, R):
+    """Offsets that decrease are against the rules, but the tiles counted from them stay inside the rows."""
+    model("bad_offsets", groups, rows, R)
+
+
 def test_tiles_of_groups(model):
     """Every row of a group is in one tile of it, and with empty groups that need one, each has one."""
     for seed in range(100):
