@@ -225,6 +225,34 @@ def test_more_columns_than_a_second_axis(G, op):
 # ---- memory ----------------------------------------------------------------------------------
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_captured_calls_record_kernels_only(G, kind):
+    """A captured gradient takes its work memory from the graph's own: no memory is allocated, freed, set
+    or copied by its nodes. (The graph is looked at and not launched.)"""
+    import ctypes
+    import torch
+    note("captured nodes %s" % kind)
+    hip = ctypes.CDLL("libamdhip64.so")
+    t, n, K, N = tdtype(kind), 9000, 72, 136
+    x, dy = dev(values(1, n, K, kind)).to(t), dev(values(2, n, N, kind)).to(t)
+    w = dev(np.ones((2, K, N), np.float32)).to(t)
+    ends = dev(np.array([0, 4000, n], np.int64))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        out = [G.gcn_gemm_grouped(G.GCN_GEMM_NT, ends, dy, w), G.gcn_gemm_grouped(G.GCN_GEMM_TN, ends, x, dy),
+               *G.gcn_layernorm_affine_bwd(x, x, None, 1e-5, G.Dropout(0.5, 1))]
+    raw, count = ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t(0)
+    assert hip.hipGraphGetNodes(raw, None, ctypes.byref(count)) == 0 and count.value >= 5
+    nodes = (ctypes.c_void_p * count.value)()
+    assert hip.hipGraphGetNodes(raw, nodes, ctypes.byref(count)) == 0
+    for node in nodes:
+        kind_of = ctypes.c_int(-1)
+        assert hip.hipGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind_of)) == 0
+        assert kind_of.value == 0  # hipGraphNodeTypeKernel
+    del graph, out
+
+
 @pytest.mark.parametrize("op,n,K,N", [(0, 2400, 2049, 4001), (1, 2400, 2049, 4001), (2, 70001, 515, 517),
                                       (2, 2400, 2049, 4001), (2, 40000, 1025, 700)])
 def test_same_bits_without_copies(G, op, n, K, N):
