@@ -115,10 +115,16 @@ def _check(status: int):
         raise GcnError(status, lib().gcn_last_error().decode())
 
 
+# The current stream's handle alone: torch.cuda.current_stream() makes a Stream object first (2.6 us a
+# call). A name of torch's own, so not needed.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
-        # the raw handle: torch.cuda.current_stream() makes a Stream object first (2.6 us a call)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))

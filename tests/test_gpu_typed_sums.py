@@ -284,3 +284,20 @@ def test_same_bits_without_copies(G, op, n, K, N):
     assert call(got[0], work.data_ptr(), need) == 0
     assert call(got[1], work.data_ptr(), less) == 0
     assert torch.equal(*got)
+
+
+# ---- the caller's stream ---------------------------------------------------------------------
+
+
+def test_current_stream_by_either_name(G, monkeypatch):
+    """Calls run on the current stream, whether or not torch has the quicker name for its handle."""
+    import torch
+    from paper_2411_16025_amd import gcnagg
+    note("current stream")
+    side = torch.cuda.Stream()
+    for raw in (gcnagg._raw_stream, None):
+        monkeypatch.setattr(gcnagg, "_raw_stream", raw)
+        for s in (torch.cuda.default_stream(), side):
+            with torch.cuda.stream(s):
+                got = gcnagg._stream(None)
+                assert (getattr(got, "value", got) or 0) == s.cuda_stream
