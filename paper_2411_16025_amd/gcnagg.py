@@ -735,6 +735,8 @@ class Dropout:
         for v, nm in ((seed, "seed"), (call, "call")):
             if not 0 <= v < 1 << 64:
                 raise ValueError("%s must be in [0, 2^64)" % nm)
+        if not -(1 << 63) <= row0 < 1 << 63:
+            raise ValueError("row0 must be a 64-bit number")
         self.p, self.seed, self.call, self.row0, self.step = p, seed, call, row0, step
 
     def _ref(self):

@@ -159,3 +159,12 @@ def test_grouped_narrow_weight_gradients_are_cut(L):
         assert L.gcn_gemm_grouped(2, 4, FAKE, 500000, N, K, FAKE, K, FAKE, N, 1, FAKE, N, 0, K * N, None,
                                   ctypes.byref(size), None) == 0
         assert size.value >= 100 * 4 * K * N
+
+
+def test_row0_is_not_cut(L):
+    """A row number that does not fit the call's is refused, not taken modulo 2^64."""
+    import paper_2411_16025_amd as pkg
+    for row0 in (1 << 64, (1 << 64) + 5, 1 << 63, -(1 << 63) - 1):
+        with pytest.raises(ValueError):
+            pkg.Dropout(0.5, 1, row0=row0)
+    assert L.gcn_dropout(4, 8, FAKE, 8, 0, spec(row0=(1 << 63) - 1), FAKE, 8, None) == ERANGE
