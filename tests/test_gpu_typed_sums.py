@@ -121,6 +121,49 @@ def test_weight_gradients_exact(G, kind, sizes, K, N):
         assert torch.equal(got[g].double(), product64(x[r], dy[r])), g
 
 
+# ---- roundings as they add up -----------------------------------------------------------------
+
+
+@pytest.mark.parametrize("op,kind,sizes,K,N,longest", [
+    (0, "f32", [9000, 0, 500], 516, 200, 516), (1, "f32", [9000, 0, 500], 4096, 130, 4096),
+    (0, "f32", [33000, 2000], 100, 256, 100), (0, "f32", [3] * 40, 700, 300, 700),
+    (2, "f32", [140000, 5], 136, 132, 2048), (2, "f32", [70001, 129999], 1024, 1024, 4096),
+    (2, "f32", [9000, 2500, 0], 40, 70, 2048),
+    (0, "bf16", [9000, 0, 500], 1032, 520, 1032), (1, "bf16", [9000, 0, 500], 4099, 261, 4099),
+    (0, "bf16", [3] * 40, 700, 300, 700), (2, "bf16", [140000, 5], 136, 132, 65536),
+    (2, "bf16", [70001, 9], 520, 264, 65536), (2, "bf16", [150000, 7], 7, 130, 4096)])
+def test_products_of_normal_values(G, op, kind, sizes, K, N, longest):
+    """Errors as independent roundings make them, in the matrix's norm. A chain of m normal products, r
+    roundings to every 16 of them, has partial sums of sqrt(16 k) after 16 k, so an error of
+    U / sqrt(3) sqrt(r sum 16 k) = U sqrt(r / 96) m against sqrt(m): U sqrt(r m / 96). r is 6 of the three parts
+    (the products left out of them are below a rounding), 4 of the fp32 instruction, 16 of multiplications
+    one by one: twice 0.41 sqrt(m) covers all, and a row, a chunk or a part less is thousands of times that."""
+    import torch
+    note("normal values op=%d %s sizes=%s K=%d N=%d" % (op, kind, sizes[:4], K, N))
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(K * 7 + N)
+    n, ends, t = sum(sizes), cuts(sizes), tdtype(kind)
+    normal = lambda *s: torch.randn(*s, generator=gen, device="cuda:0").to(t)  # noqa: E731
+    a = normal(n, K)
+    b = normal(n, N) if op == 2 else normal(len(sizes), K, N) if op == 0 else normal(len(sizes), N, K)
+    got = G.gcn_gemm_grouped(op, dev(ends), a, b, out_dtype=torch.float32)
+    worst = ref.U * (1 + 0.82 * np.sqrt(longest))
+    for g in range(len(sizes)):
+        r = slice(int(ends[g]), int(ends[g + 1]))
+        if op == 2:
+            c, want = got[g], product64(a[r], b[r])
+        else:
+            w = b[g].double() if op == 0 else b[g].double().t().contiguous()
+            c, want = got[r], a[r].double() @ w
+        if want.numel() and sizes[g]:
+            err = float((c.double() - want).norm() / want.norm())
+            if sizes[g] > 100:
+                note("error %.2e, at most %.2e" % (err, worst))
+            assert err <= worst, (g, err)
+        elif op == 2:
+            assert not c.any()
+
+
 # ---- long inner sizes ----------------------------------------------------------------------
 
 
