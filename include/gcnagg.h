@@ -366,10 +366,9 @@ gcn_status gcn_sage3_step(const gcn_graph* g, const float* X, int64_t ldx, int64
  *            is read when the kernels run, so a captured call follows it. Rows
  *            before the first and behind the last offset belong to no group: NN
  *            and NT leave those rows of C as they were, TN leaves them out.
- *            Offsets outside [0, rows] are taken as 0 or rows and a group that
- *            ends before it begins as an empty one; no error is reported. Of
- *            groups that then overlap no values are defined in C, but nothing is
- *            read or written outside of the arrays.
+ *            Offsets outside [0, rows] are taken as 0 or rows. Where they
+ *            decrease no values are defined in C, but nothing is read or written
+ *            outside of the arrays. No error is reported for either.
  *  A group without rows takes no part in NN and NT; in TN its C_g is zero.
  *  dtype     GCN_DT_F32 or GCN_DT_BF16: the type of A and B. dtype_c: that of C,
  *            GCN_DT_F32 or, for NN and NT, that of A and B (rounded once).

@@ -91,6 +91,7 @@ inline uint64_t __ballot(bool p) {
     if (g.lanes >> l & 1 && g.of<bool>(l)) m |= 1ull << l;
   return m;
 }
+inline bool __any(bool p) { return __ballot(p) != 0; }
 template <class T>
 T __shfl_xor(T v, int off, int) {
   return model::from_lane("shfl_xor", v, model::lane() ^ off);
@@ -169,6 +170,13 @@ inline model::f16 __builtin_amdgcn_mfma_f32_32x32x16_bf16(model::bf8 a, model::b
   typedef ModelOperands<32, 8, model::bf8> O;
   const O o(a, b);
   const model::Given& g = model::give("mfma_32x32x16", &o, sizeof o);
+  for (int e = 0; e < 16; ++e) c[e] += O::row(g, (e & 3) + 8 * (e >> 2) + 4 * (model::lane() >> 5));
+  return c;
+}
+inline model::f16 __builtin_amdgcn_mfma_f32_32x32x2f32(float a, float b, model::f16 c, int, int, int) {
+  typedef ModelOperands<32, 1, float> O;
+  const O o(a, b);
+  const model::Given& g = model::give("mfma_32x32x2", &o, sizeof o);
   for (int e = 0; e < 16; ++e) c[e] += O::row(g, (e & 3) + 8 * (e >> 2) + 4 * (model::lane() >> 5));
   return c;
 }

@@ -282,14 +282,8 @@ gcn_status tmalloc(void** p, size_t bytes, hipStream_t, const char*, const void*
   return GCN_OK;
 }
 void tfree(void* p, hipStream_t) { model::release(p); }
-// (the three-part products are not modelled: fp32 goes to the other kernels)
-bool gemm_split_grouped_takes(int, int64_t, int64_t, int64_t, int64_t, int64_t) { return false; }
-gcn_status gemm_split_grouped(int, const Groups&, int64_t, int64_t, const float*, int64_t, const float*,
-                              int64_t, int64_t, float*, int64_t, hipStream_t) {
-  return GCN_EINVAL;
-}
-gcn_status gemm_split_tn_grouped(const Groups&, int64_t, int64_t, const float*, int64_t, const float*,
-                                 int64_t, float*, int64_t, int64_t, Scratch*, hipStream_t) {
+// (of the ungrouped products)
+gcn_status sum_partials(int64_t, int64_t, int64_t, const float*, float*, int64_t, hipStream_t) {
   return GCN_EINVAL;
 }
 
@@ -360,6 +354,7 @@ void grouped(int c, char** v) {
   ends[0] = before;
   for (int g = 0; g < G; ++g) ends[g + 1] = ends[g] + arg(v, 9 + g);
   const int64_t rows = ends[G] + after;
+  if (!model::g_at_end && rows * K * N > 12000000000) return;  // (seconds; the smaller ones do)
   auto number = [&](int64_t, int64_t) { return (float)(int)(g_rng() % 7) - 3.f; };
   auto of_group = [&](int64_t i) { return i >= before && i < ends[G]; };
   const bool tn = op == GCN_GEMM_TN;
@@ -409,6 +404,25 @@ void grouped(int c, char** v) {
     for (int64_t j = N; i + 1 < C.n && j < C.ld; ++j)
       CHECK(std::isnan(C.get(i, j)), "between the rows %ld and the next", (long)i);
   }
+}
+
+// unordered seed: offsets in any order, beyond the rows and negative: no address leaves the arrays.
+void unordered(int, char** v) {
+  g_rng.seed(arg(v, 0));
+  auto upto = [](int64_t n) { return (int64_t)(g_rng() % (uint64_t)(n + 1)); };
+  const int op = (int)upto(2), dt = (int)upto(1), G = 1 + (int)upto(upto(3) ? 8 : 1100);
+  const int64_t rows = 1 + upto(upto(1) ? 9000 : 400), K = 1 + upto(140), N = 1 + upto(140);
+  int64_t* ends = (int64_t*)model::array((G + 1) * 8);
+  for (int g = 0; g <= G; ++g) ends[g] = upto(9) ? upto(rows) : (upto(1) ? -1 : 1) * (int64_t)(g_rng() >> upto(40) >> 1);
+  const bool tn = op == GCN_GEMM_TN;
+  Matrix A(dt, rows, K, K), B(dt, tn ? rows : G * (op == GCN_GEMM_NT ? N : K), op == GCN_GEMM_NT ? K : N,
+                             op == GCN_GEMM_NT ? K : N);
+  Matrix C(GCN_DT_F32, tn ? G * K : rows, N, N);
+  for (Matrix* m : {&A, &B, &C}) m->fill([](int64_t, int64_t) { return 1.f; });
+  CHECK(gcn_gemm_grouped(op, G, ends, rows, N, K, A.p, A.ld, B.p, B.ld, dt, C.p, C.ld, GCN_DT_F32,
+                         tn ? K * N : B.n / G * B.ld, nullptr, nullptr, nullptr) == GCN_OK,
+        "call");
+  model::check_margins();
 }
 
 // norm n F dtype pad eps p: forward and backward, within roundings of what the formulas give in 64 bits.
@@ -569,6 +583,7 @@ int main(int c, char** v) {
     model::g_at_end = at_end;
     g_rng.seed(1);
     if (what == "grouped") grouped(c - 2, v + 2);
+    else if (what == "unordered") unordered(c - 2, v + 2);
     else if (what == "norm") norm(c - 2, v + 2);
     else if (what == "dropout") dropout(c - 2, v + 2);
     else if (what == "tiles") tiles(c - 2, v + 2);
