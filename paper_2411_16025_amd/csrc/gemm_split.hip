@@ -877,8 +877,8 @@ gcn_status gemm_split_tn_grouped(const Groups& g, int64_t N, int64_t K, const fl
   // groups' last ones have (200,000 rows of 3 groups, 1024 x 1024: 2.30 ms in 128 chunks, 2.54 in 64 runs).
   const int64_t chunks = ceil_div(g.rows, split);
   const int64_t run = std::max<int64_t>(
-      1, std::min(ceil_div(chunks * most - 3 * g.rows / 10, std::max<int64_t>(1, g.rows)),
-                  tiles >= kSharedTiles ? chunks * tiles / 2048 : chunks / 128));
+      1, std::min({ceil_div(chunks * most - 3 * g.rows / 10, std::max<int64_t>(1, g.rows)),
+                   chunks * tiles / 512, tiles >= kSharedTiles ? chunks * tiles / 2048 : chunks / 128}));
   const int64_t slots = group_slots(g, split * run);
   const int64_t parts = g.rows / (split * run);
   const int64_t blocks = run > 1 && tiles >= kSharedTiles ? ceil_div(tiles, (int64_t)8) * 8 * slots

@@ -168,3 +168,13 @@ def test_row0_is_not_cut(L):
         with pytest.raises(ValueError):
             pkg.Dropout(0.5, 1, row0=row0)
     assert L.gcn_dropout(4, 8, FAKE, 8, 0, spec(row0=(1 << 63) - 1), FAKE, 8, None) == ERANGE
+
+
+def test_grouped_weight_gradients_keep_their_workgroups(L):
+    """A workgroup adds up several chunks only where 512 are left: of a small matrix every chunk but the
+    first ones has a partial sum."""
+    size = ctypes.c_int64(-1)
+    rows, K, N = 176075, 47, 32
+    assert L.gcn_gemm_grouped(2, 12, FAKE, rows, N, K, FAKE, K, FAKE, N, 0, FAKE, N, 0, K * N, None,
+                              ctypes.byref(size), None) == 0
+    assert size.value >= 480 * 4 * K * N
