@@ -1,6 +1,7 @@
 // Products of rows sorted by group with one matrix per group (gcn_gemm_grouped).
 
 #include <algorithm>
+#include <type_traits>
 
 #include "element.h"
 #include "groups.h"
@@ -406,10 +407,9 @@ gcn_status grouped(int op, GroupArgs a, Scratch* scratch, hipStream_t s) {
 // Partial sum p (blockIdx.y) belongs to the last group that begins in chunk p of all rows or
 // before it, if that has so many: a group of several chunks reaches the next multiple of
 // `split`. The workgroups of a group's partial sums share its elements, each element
-// the sum of all of them in chunk order, in double: the chain of 1276 partial sums of
-// 2,449,029 x 256 x 96 in fp32 made 9.3e-7 of 6.5e-7.
-constexpr int kAhead = 16;  // loads on their way at a time
-
+// the sum of all of them in an order that their number decides: sixteen at a time (and fewer at
+// the end) by pairs, those sums in double. (The chain of 1276 partial sums of 2,449,029 x 256 x 96 in fp32
+// made 9.3e-7 of 6.5e-7; one load at a time 58 us of 113,045 rows of 22 groups, 1024 x 256.)
 __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t split, int64_t K,
                                                          int64_t N, int64_t p, const float* part, float* C,
                                                          int64_t ldc, int64_t stride_w) {
@@ -422,18 +422,29 @@ __global__ __launch_bounds__(kThreads) void k_group_sums(Groups by, int64_t spli
   for (int64_t t = ((p - p0) * gridDim.x + blockIdx.x) * kThreads + threadIdx.x; t < K * N;
        t += more * gridDim.x * kThreads) {
     float* c = C + t / N * ldc + t % N;
-    double s = *c;
+    const float first = *c;  // (not waited for before the loads of the others)
+    double s = 0.0;
     const float* q = part + t;
-    int64_t j = 0;
-    for (; j + kAhead <= more; j += kAhead, q += kAhead * K * N) {
-      float v[kAhead];
+    int64_t left = more;
+    auto add = [&](auto ahead) {  // so many, pairs first, their loads on their way at a time
+      constexpr int n = decltype(ahead)::value;
+      float v[n];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) v[i] = q[i * K * N];
+      for (int i = 0; i < n; ++i) v[i] = q[i * K * N];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) s += (double)v[i];
-    }
-    for (; j < more; ++j, q += K * N) s += (double)*q;
-    *c = (float)s;
+      for (int h = n / 2; h > 0; h /= 2)
+#pragma unroll
+        for (int i = 0; i < h; ++i) v[i] += v[i + h];
+      s += (double)v[0];
+      q += n * K * N;
+      left -= n;
+    };
+    while (left >= 16) add(std::integral_constant<int, 16>());
+    if (left >= 8) add(std::integral_constant<int, 8>());
+    if (left >= 4) add(std::integral_constant<int, 4>());
+    if (left >= 2) add(std::integral_constant<int, 2>());
+    if (left >= 1) add(std::integral_constant<int, 1>());
+    *c = (float)(s + (double)first);
   }
 }
 
