@@ -430,7 +430,7 @@ gcn_status gcn_dropout(int64_t n, int64_t F, const void* X, int64_t ldx, int dty
  *  gamma, beta  fp32 [F], or NULL for 1 and 0.
  *  eps       >= 0. A row whose var + eps lies below 2^-256 has no 1 / sqrt in
  *            fp32's range (with eps = 0 a constant row, 0 / 0): what is computed
- *            of it is infinite or NaN, also its part of dgamma.
+ *            of it is infinite or NaN, and so is dgamma, which sums over the rows.
  *  drop      NULL: no dropout; else as for gcn_dropout.
  * Asynchronous. Nothing is kept for the backward pass but X itself. */
 gcn_status gcn_layernorm_affine_fwd(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype,
