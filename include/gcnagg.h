@@ -454,6 +454,144 @@ gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t
                                     float* dgamma, float* dbeta, void* work, int64_t* work_bytes,
                                     void* stream);
 
+/* ---- routed layers: rows to their groups and back ------------------------------ */
+
+/* Positions sorted by group: the plan that the calls below share. For ids[i], i < n:
+ *   offsets  int64 [n_groups + 1]: group g's positions are the places
+ *            [offsets[g], offsets[g + 1]) of the sorted order (what gcn_gemm_grouped takes)
+ *   order    int32 [n] or NULL: the position at each place; within a group increasing
+ *   slot     int32 [n] or NULL: the place of each position
+ * An id outside [0, n_groups) (padding, a dropped choice) belongs to no group: its slot is
+ * -1, and the places from offsets[n_groups] on hold -1 in `order`. So the sizes of what
+ * follows are those of n, whatever the ids are, and a captured call follows them.
+ *  ids  int32 device [n]; 0 <= n < 2^31, 1 <= n_groups <= 2^30.
+ *  work, work_bytes  scratch memory, as for gcn_gemm_grouped.
+ * No atomics on results: the one stable order. Asynchronous on `stream`. */
+gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_groups, int64_t* offsets,
+                         int32_t* order, int32_t* slot, void* work, int64_t* work_bytes,
+                         void* stream);
+
+/* Rows of a learned table, scaled: Y[i] = scale * T[ids[i] / per] for i < n, computed in
+ * fp32 and rounded once. Rows whose id lies outside [0, V per) become +0.
+ *  per    >= 1: 1 for a lookup. With the `order` of gcn_group_ids over the k choices of
+ *         each token, per = k brings the tokens' rows into the groups' order.
+ *  T [V x F] (ldt) of type dtype, Y [n x F] (ldy) of type dtype_y: GCN_DT_F32 or
+ *  GCN_DT_BF16 each; Y may not overlap T. ids int32 device [n]. n < 2^31,
+ *  1 <= V < 2^31, F <= 2^30, scale finite. Asynchronous. */
+gcn_status gcn_embed_fwd(int64_t n, int64_t F, int64_t V, const int32_t* ids, int64_t per,
+                         const void* T, int64_t ldt, int dtype, double scale, void* Y, int64_t ldy,
+                         int dtype_y, void* stream);
+
+/* gcn_embed_bwd flags */
+enum { GCN_ACCUMULATE = 1u /* add to what dT holds */ };
+
+/* The table's gradient of gcn_embed_fwd (per = 1), by sorted ids:
+ *   dT[v] = scale * sum over offsets[v] <= j < offsets[v + 1] of dY[order[j]]
+ * with offsets [V + 1] and order [n] of gcn_group_ids(ids, V). Rows of ids that do not
+ * occur become 0; with GCN_ACCUMULATE the sums are added to dT, whose other rows are not
+ * touched. Sums in fp32 over at most 256 rows, those sums in double, one rounding to dT's
+ * type; each in an order that n, offsets and order decide, so results repeat bit for bit.
+ *  dY [n x F] (lddy) of type dtype, dT [V x F] (lddt) of type dtype_t, which may not overlap.
+ *  Entries of `order` outside [0, n) are left out; offsets outside [0, n] are taken as 0 or n.
+ *  Where they decrease no values are defined in dT, but nothing is read or written outside of
+ *  the arrays.
+ *  n < 2^31, 1 <= V <= 2^30, F <= 2^30, scale finite.
+ *  work, work_bytes  scratch memory, as for gcn_gemm_grouped.
+ * Asynchronous. */
+gcn_status gcn_embed_bwd(int64_t n, int64_t F, int64_t V, const int64_t* offsets,
+                         const int32_t* order, const void* dY, int64_t lddy, int dtype,
+                         double scale, void* dT, int64_t lddt, int dtype_t, uint32_t flags,
+                         void* work, int64_t* work_bytes, void* stream);
+
+/* gcn_route_fwd, gcn_route_bwd flags */
+enum { GCN_ROUTE_NORMALIZE = 1u /* a row's weights are divided by their sum */ };
+
+/* A router's choice: for each of n rows of E logits z the k largest ones, their weights,
+ * and what keeps the experts evenly used.
+ *   p = softmax(z) over the row;  experts[t k + i] the index of the i-th largest logit
+ *   (of equal ones the lowest index first);  weights[t k + i] its p, with
+ *   GCN_ROUTE_NORMALIZE divided by the sum of the chosen ones'
+ *   counts[e] = how often e was chosen, counts[E] = N, the rows that chose any
+ *   loss = coef E sum_e (counts[e] / sum counts) (sum_t p[t, e] / N)
+ * A logit of -inf (an expert that is closed) or NaN is never chosen: where fewer than k
+ * are left, the rest of `experts` is -1 (no group to gcn_group_ids) with weight 0. A row
+ * with mask[t] = 0, or of -inf alone, chooses none, and its p is 0. A row that holds a NaN,
+ * or +inf, has NaN as p and weights, and the loss is NaN. Without any choice the loss is 0.
+ *  logits [n x E] (ldz) of type dtype (GCN_DT_F32 or GCN_DT_BF16); 1 <= E <= 1024,
+ *  1 <= k <= min(E, 64), n k < 2^31. mask uint8 [n] or NULL. experts int32 [n k], weights fp32
+ *  [n k], counts int64 [E + 1], loss fp32 or NULL (device). fp32; sums over rows in an order
+ *  that n, E and the type decide, then in double; results repeat bit for bit.
+ *  work, work_bytes  scratch memory, as for gcn_gemm_grouped.
+ * Asynchronous. */
+gcn_status gcn_route_fwd(int64_t n, int64_t E, const void* logits, int64_t ldz, int dtype,
+                         int64_t k, uint32_t flags, const uint8_t* mask, double coef,
+                         int32_t* experts, float* weights, int64_t* counts, float* loss,
+                         void* work, int64_t* work_bytes, void* stream);
+
+/* Gradient of gcn_route_fwd with respect to the logits, from its outputs:
+ *   dz_j = [j chosen] p_j g_j - p_j sum_i g_i p_i       (g = dweights, i over the chosen)
+ *          or, with GCN_ROUTE_NORMALIZE, [j chosen] w_j (g_j - sum_i g_i w_i),
+ *        + p_j (a_j - sum_e a_e p_e),  a_e = dloss coef E counts[e] / (N sum counts)
+ * The choice and the counts are constants. p is formed again from the logits. Rows that
+ * chose none get 0 (whatever mask said is in `experts`). counts may be the sums over
+ * several workers, whose batch is then one.
+ *  dweights  fp32 [n k] or NULL for 0; dloss  fp32 (device) or NULL for 1; coef = 0: no
+ *            balance loss (counts may be NULL).
+ *  dlogits   [n x E] (ldd) of type dtype, may be the logits themselves (same ld).
+ * Asynchronous. */
+gcn_status gcn_route_bwd(int64_t n, int64_t E, const void* logits, int64_t ldz, int dtype,
+                         int64_t k, uint32_t flags, const int32_t* experts, const float* weights,
+                         const int64_t* counts, double coef, const float* dweights,
+                         const float* dloss, void* dlogits, int64_t ldd, void* stream);
+
+/* Back from the groups' order: Y[t] = sum over i < k of weights[t k + i] Z[slot[t k + i]],
+ * in fp32 in the order of i, rounded once. Slots outside [0, rows) (dropped choices) take no
+ * part; a row without any becomes +0.
+ *  Z [rows x F] (ldz), Y [n x F] (ldy) of type dtype; slot int32 [n k]; weights fp32 [n k], or
+ *  NULL for 1: then it is the gradient of gcn_embed_fwd with per = k.
+ *  n < 2^31, 0 <= rows < 2^31, 1 <= k <= 2^16, F <= 2^30. Y may not overlap Z. Asynchronous. */
+gcn_status gcn_combine_fwd(int64_t n, int64_t k, int64_t F, const void* Z, int64_t rows,
+                           int64_t ldz, int dtype, const int32_t* slot, const float* weights,
+                           void* Y, int64_t ldy, void* stream);
+
+/* Gradients of gcn_combine_fwd: dZ[slot[t k + i]] = weights[t k + i] dY[t] and
+ * dweights[t k + i] = <dY[t], Z[slot[t k + i]]> (0 for a slot outside [0, rows)).
+ * No slot may occur twice. Rows of dZ that are no slot's are left as they were.
+ *  dZ [rows x F] (lddz) or NULL, may be Z itself (same ld); dweights fp32 [n k] or NULL (Z may
+ *  be NULL then); not both NULL. Products and sums in fp32. Asynchronous. */
+gcn_status gcn_combine_bwd(int64_t n, int64_t k, int64_t F, const void* Z, int64_t rows,
+                           int64_t ldz, int dtype, const int32_t* slot, const float* weights,
+                           const void* dY, int64_t lddy, void* dZ, int64_t lddz, float* dweights,
+                           void* stream);
+
+/* Rows kept in 8 bits for the backward pass. Each 32 columns of a row (the last ones may
+ * be fewer) share a power of two: x ~ q 2^(b - 127), q an int8 code, b a scale byte:
+ *   b - 127 = the least e in [-126, 121] with max |x| <= 127 2^e, q = rint(x 2^-e) (half to
+ *   even) in [-127, 127]
+ * so |x - q 2^e| <= 2^(e - 1), which is less than max |x| / 127 where e > -126; magnitudes
+ * above 127.5 2^121 become 127 2^121. Every value is exact in bf16 and fp32. 32 columns with an
+ * infinity or NaN: b = 255 and codes 0, which stand for NaN.
+ *  X [n x F] (ldx) of type dtype; Q int8 [n x F] (ldq); S uint8 [n x (F + 31) / 32] (lds).
+ *  n < 2^31, F <= 2^30. Asynchronous. */
+gcn_status gcn_pack8(int64_t n, int64_t F, const void* X, int64_t ldx, int dtype, int8_t* Q,
+                     int64_t ldq, uint8_t* S, int64_t lds, void* stream);
+
+/* Y = the values that gcn_pack8's codes stand for (Y [n x F], ldy, of type dtype). */
+gcn_status gcn_unpack8(int64_t n, int64_t F, const int8_t* Q, int64_t ldq, const uint8_t* S,
+                       int64_t lds, void* Y, int64_t ldy, int dtype, void* stream);
+
+/* Weight gradients from rows kept in 8 bits: C_g [K x N] = X_g^T B_g over the rows of each
+ * group, X [rows x K] what the codes Q (ldq) and scale bytes S (lds) stand for. Everything
+ * else as for gcn_gemm_grouped with GCN_GEMM_TN: offsets, rows outside of all groups, empty
+ * groups (zeros), the types of B (fp32 or bf16) and C (fp32), limits, work memory, errors.
+ * bf16: exact products and fp32 sums; fp32: B exactly split into three bf16 parts, products
+ * exact too. */
+gcn_status gcn_gemm_grouped_q8(int64_t n_groups, const int64_t* offsets, int64_t rows, int64_t N,
+                               int64_t K, const int8_t* Q, int64_t ldq, const uint8_t* S,
+                               int64_t lds, const void* B, int64_t ldb, int dtype, float* C,
+                               int64_t ldc, int64_t stride_w, void* work, int64_t* work_bytes,
+                               void* stream);
+
 /* ---- hybrid pre/post-aggregation (Algorithm 1, Sections 5.2 and 5.3) ---- */
 
 /* Split the cut edges that a sending worker has into a receiving worker.

@@ -1,0 +1,288 @@
+// Positions sorted by group (gcn_group_ids): a stable radix sort of the ids that ends in the sorted
+// positions, their places and the groups' offsets.
+//
+// Digits of up to 11 bits, as even as the ids' bits allow: up to 2047 groups take one pass, 2^22
+// two. A pass has three launches: every tile counts its digits, the counts are summed down the
+// tiles digit by digit, and every tile places its ids. A wavefront ranks 64 consecutive ids at a
+// time: ballots, bit by bit, give the lanes of the same digit; a counter of the wavefront's own in
+// LDS those before them. No atomics but the tiles' counts (whole numbers), so the order is the one
+// stable order. Ids outside of the groups are sorted as the group behind the last one.
+
+#include <algorithm>
+
+#include "common.h"
+#include "scratch.h"
+
+namespace gcn {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMaxBits = 11, kMaxDigits = 1 << kMaxBits;
+
+struct SortArgs {
+  uint32_t n, groups;
+  int shift, bits;      // of the pass
+  uint32_t digits;      // 2^bits, or in a single pass the groups and one more
+  const int32_t* ids;   // first pass
+  const uint64_t* in;   // later ones: key << 32 | position
+  uint64_t* out;        // but in the last
+  uint32_t* hist;       // [tiles][digits]: counts, then those of the tiles before
+  uint32_t* total;      // [digits]
+  uint32_t tiles;
+  int32_t* order;
+  int32_t* slot;
+  uint32_t* sorted;     // the keys in order (last of several passes)
+  int64_t* offsets;     // (single pass)
+};
+
+template <bool FIRST>
+__device__ inline uint64_t load_key(const SortArgs& a, uint32_t i) {
+  if constexpr (FIRST) {
+    const uint32_t id = (uint32_t)a.ids[i];
+    return (uint64_t)(id < a.groups ? id : a.groups) << 32 | i;
+  } else {
+    return a.in[i];
+  }
+}
+
+__device__ inline uint32_t digit(const SortArgs& a, uint64_t key) {
+  return (uint32_t)(key >> (32 + a.shift)) & ((1u << a.bits) - 1);
+}
+
+template <bool FIRST, int ITEMS>
+__global__ __launch_bounds__(kThreads) void k_count(SortArgs a) {
+  __shared__ uint32_t cnt[kMaxDigits];
+  for (uint32_t d = threadIdx.x; d < a.digits; d += kThreads) cnt[d] = 0;
+  __syncthreads();
+  const uint32_t base = blockIdx.x * (kThreads * ITEMS);
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    const uint32_t i = base + j * kThreads + threadIdx.x;
+    if (i < a.n) atomicAdd(&cnt[digit(a, load_key<FIRST>(a, i))], 1u);
+  }
+  __syncthreads();
+  for (uint32_t d = threadIdx.x; d < a.digits; d += kThreads)
+    a.hist[(uint64_t)blockIdx.x * a.digits + d] = cnt[d];
+}
+
+// 64 digits to a workgroup; its sixteen wavefronts share the tiles.
+__global__ __launch_bounds__(1024) void k_sum_tiles(SortArgs a) {
+  __shared__ uint32_t sums[16][64];
+  const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+  const uint32_t per = (a.tiles + 15) / 16, beg = min(w * per, a.tiles), end = min(beg + per, a.tiles);
+  const bool in = d < a.digits;
+  uint32_t s = 0;
+  for (uint32_t t = beg; t < end; ++t) s += in ? a.hist[(uint64_t)t * a.digits + d] : 0;
+  sums[w][lane] = s;
+  __syncthreads();
+  uint32_t run = 0, all = 0;
+  for (uint32_t q = 0; q < 16; ++q) {
+    run += q < w ? sums[q][lane] : 0;
+    all += sums[q][lane];
+  }
+  if (!in) return;
+  if (w == 0) a.total[d] = all;
+  for (uint32_t t = beg; t < end; ++t) {
+    uint32_t* h = &a.hist[(uint64_t)t * a.digits + d];
+    const uint32_t v = *h;
+    *h = run;
+    run += v;
+  }
+}
+
+template <bool FIRST, bool LAST, int ITEMS>
+__global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
+  __shared__ uint32_t first[kMaxDigits];         // the place of the tile's first id of a digit
+  __shared__ uint32_t cnt[kWaves][kMaxDigits];   // ids of a wavefront, then of those before it
+  __shared__ uint32_t wave_sum[kWaves];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  for (uint32_t d = t; d < kWaves * a.digits; d += kThreads) cnt[d / a.digits][d % a.digits] = 0;
+  // each thread sums a run of digits
+  const uint32_t per = (a.digits + kThreads - 1) / kThreads;
+  uint32_t mine = 0;
+  for (uint32_t i = 0; i < per; ++i) {
+    const uint32_t d = t * per + i;
+    if (d < a.digits) mine += a.total[d];
+  }
+  uint32_t upto = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t v = __shfl_up(upto, off, 64);
+    if (lane >= off) upto += v;
+  }
+  if (lane == 63) wave_sum[w] = upto;
+  __syncthreads();
+  uint32_t run = upto - mine;
+  for (int q = 0; q < w; ++q) run += wave_sum[q];
+  for (uint32_t i = 0; i < per; ++i) {
+    const uint32_t d = t * per + i;
+    if (d >= a.digits) break;
+    if (FIRST && LAST && blockIdx.x == 0) a.offsets[d] = run;
+    first[d] = run + a.hist[(uint64_t)blockIdx.x * a.digits + d];
+    run += a.total[d];
+  }
+  uint64_t key[ITEMS];
+  uint32_t rank[ITEMS];
+  const uint32_t base = blockIdx.x * (kThreads * ITEMS) + w * (64 * ITEMS) + lane;
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j)
+    key[j] = base + j * 64 < a.n ? load_key<FIRST>(a, base + j * 64) : ~0ull;
+  const uint64_t below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    const bool valid = base + j * 64 < a.n;
+    const uint32_t d = digit(a, key[j]);
+    uint64_t peers = __ballot(valid);
+    for (int bit = 0; bit < a.bits; ++bit) {
+      const bool b = (d >> bit) & 1u;
+      const uint64_t m = __ballot(b);
+      peers &= b ? m : ~m;
+    }
+    const uint32_t before = (uint32_t)__popcll(peers & below);
+    const uint32_t have = valid ? cnt[w][d] : 0;
+    // (LDS operations of one wavefront take effect in order; the fence keeps
+    // the compiler from moving the store before the other lanes' loads)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (valid && before == 0) cnt[w][d] = have + (uint32_t)__popcll(peers);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    rank[j] = have + before;
+  }
+  __syncthreads();
+  for (uint32_t d = t; d < a.digits; d += kThreads) {
+    uint32_t s = first[d];
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) {
+      const uint32_t c = cnt[q][d];
+      cnt[q][d] = s;
+      s += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < ITEMS; ++j) {
+    if (base + j * 64 >= a.n) continue;
+    const uint32_t place = cnt[w][digit(a, key[j])] + rank[j];
+    if constexpr (LAST) {
+      const uint32_t id = (uint32_t)(key[j] >> 32), at = (uint32_t)key[j];
+      const bool in = id < a.groups;
+      if (a.order) a.order[place] = in ? (int32_t)at : -1;
+      if (a.slot) a.slot[at] = in ? (int32_t)place : -1;
+      if constexpr (!FIRST) a.sorted[place] = id;
+    } else {
+      a.out[place] = key[j];
+    }
+  }
+}
+
+// The first place of a key that is at least v, in [lo, hi].
+__device__ inline uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t v) {
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (keys[mid] < v)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// Offsets from the sorted keys: a workgroup's groups are found in the range between its own ends.
+__global__ __launch_bounds__(kThreads) void k_offsets(const uint32_t* sorted, uint32_t n,
+                                                      uint32_t groups, int64_t* offsets) {
+  const uint32_t v0 = blockIdx.x * kThreads, v = v0 + threadIdx.x;
+  const uint32_t lo = lower_bound(sorted, 0, n, v0);
+  const uint32_t hi = lower_bound(sorted, lo, n, min(v0 + kThreads, groups));
+  if (v <= groups) offsets[v] = lower_bound(sorted, lo, hi, v);
+}
+
+__global__ __launch_bounds__(kThreads) void k_zero_offsets(int64_t* offsets, int64_t count) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < count) offsets[i] = 0;
+}
+
+template <bool FIRST, bool LAST, int ITEMS>
+gcn_status pass(const SortArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_count<FIRST, ITEMS>), dim3(a.tiles), dim3(kThreads), 0, s, a);
+  GCN_HIP(hipGetLastError());
+  hipLaunchKernelGGL(k_sum_tiles, dim3((a.digits + 63) / 64), dim3(1024), 0, s, a);
+  GCN_HIP(hipGetLastError());
+  hipLaunchKernelGGL((k_place<FIRST, LAST, ITEMS>), dim3(a.tiles), dim3(kThreads), 0, s, a);
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
+template <int ITEMS>
+gcn_status sort_ids(SortArgs a, int bits, int passes, uint64_t* pairs[2], hipStream_t s) {
+  if (passes == 1) return pass<true, true, ITEMS>(a, s);
+  for (int p = 0; p < passes; ++p) {
+    a.shift = bits * p / passes;
+    a.bits = bits * (p + 1) / passes - a.shift;
+    a.digits = 1u << a.bits;
+    a.in = pairs[(p + 1) & 1];
+    a.out = pairs[p & 1];
+    GCN_CHECK((p == 0            ? pass<true, false, ITEMS>(a, s)
+               : p + 1 == passes ? pass<false, true, ITEMS>(a, s)
+                                 : pass<false, false, ITEMS>(a, s)));
+  }
+  hipLaunchKernelGGL(k_offsets, dim3((unsigned)ceil_div((int64_t)a.groups + 1, (int64_t)kThreads)),
+                     dim3(kThreads), 0, s, a.sorted, a.n, a.groups, a.offsets);
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
+}  // namespace
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_groups,
+                                    int64_t* offsets, int32_t* order, int32_t* slot, void* work,
+                                    int64_t* work_bytes, void* stream) {
+  clear_error();
+  CallScope scope(stream);
+  if (n < 0 || n_groups < 1 || !offsets || (n > 0 && !ids)) {
+    set_error("need n >= 0, n_groups >= 1 and non-NULL ids and offsets");
+    return GCN_EINVAL;
+  }
+  if (n >= (int64_t(1) << 31) || n_groups > (int64_t(1) << 30)) {
+    set_error("need n < 2^31 and n_groups <= 2^30");
+    return GCN_ERANGE;
+  }
+  GCN_CHECK(check_work(work, work_bytes));
+  hipStream_t s = (hipStream_t)stream;
+  Scratch scratch(work, work_bytes, s);
+  const int64_t zero_blocks = ceil_div(n_groups + 1, (int64_t)kThreads);
+  if (n == 0) {
+    if (scratch.asked()) return GCN_OK;
+    ProfScope ps("group_ids", s);
+    hipLaunchKernelGGL(k_zero_offsets, dim3((unsigned)zero_blocks), dim3(kThreads), 0, s, offsets,
+                       n_groups + 1);
+    GCN_HIP(hipGetLastError());
+    return GCN_OK;
+  }
+  const int bits = bits_for((uint64_t)n_groups);
+  const int passes = std::max(1, (bits + kMaxBits - 1) / kMaxBits);
+  const bool small = n <= (1 << 19);  // tiles of 1024 ids, so that there are enough of them
+  SortArgs a{};
+  a.n = (uint32_t)n;
+  a.groups = (uint32_t)n_groups;
+  a.ids = ids;
+  a.order = order;
+  a.slot = slot;
+  a.offsets = offsets;
+  a.bits = bits;
+  a.digits = (uint32_t)n_groups + 1;
+  a.tiles = (uint32_t)ceil_div(n, (int64_t)kThreads * (small ? 4 : 16));
+  const int64_t digits = passes == 1 ? n_groups + 1 : int64_t(1) << ((bits + passes - 1) / passes);
+  GCN_CHECK(scratch.alloc(&a.hist, (int64_t)a.tiles * digits, "digit counts"));
+  GCN_CHECK(scratch.alloc(&a.total, digits, "digit totals"));
+  uint64_t* pairs[2] = {nullptr, nullptr};
+  if (passes > 1) {
+    GCN_CHECK(scratch.alloc(&pairs[0], n, "sorted ids"));
+    if (passes > 2) GCN_CHECK(scratch.alloc(&pairs[1], n, "sorted ids"));
+    GCN_CHECK(scratch.alloc(&a.sorted, n, "sorted ids"));
+  }
+  if (scratch.asked()) return GCN_OK;
+  ProfScope ps("group_ids", s);
+  return small ? sort_ids<4>(a, bits, passes, pairs, s) : sort_ids<16>(a, bits, passes, pairs, s);
+}

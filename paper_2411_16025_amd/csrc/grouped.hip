@@ -491,10 +491,7 @@ extern "C" gcn_status gcn_gemm_grouped(int op, int64_t n_groups, const int64_t* 
     set_error("need a known dtype, and dtype_c fp32 or (NN, NT) the operands'");
     return GCN_EINVAL;
   }
-  if (work && (!work_bytes || reinterpret_cast<uintptr_t>(work) % 256 != 0)) {
-    set_error("work memory needs work_bytes and an alignment of 256 bytes");
-    return GCN_EINVAL;
-  }
+  GCN_CHECK(check_work(work, work_bytes));
   hipStream_t s = (hipStream_t)stream;
   Scratch scratch(work, work_bytes, s);
   if (rows == 0 && !tn) return GCN_OK;

@@ -1,0 +1,408 @@
+// A router's choice, the balance loss and their gradient (gcn_route_fwd, gcn_route_bwd).
+//
+// G neighbouring lanes hold a row, V logits each in registers, so it is read once: the largest
+// logit, the exponentials and their sum, then k times the largest of those left. Ties go to the
+// lowest index: the largest value first, then the least index that has it.
+
+#include <cmath>
+
+#include "groups.h"
+#include "lanes.h"
+#include "rows.h"
+
+namespace gcn {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMaxExperts = 1024;
+
+struct RouteArgs {
+  int64_t n;
+  int E, k;
+  const void* z;
+  int64_t ldz;
+  bool normalize;
+  const uint8_t* mask;
+  float* weights;
+  int32_t* experts;
+  // partial sums of the workgroups: choices [blocks][E + 1] (the last: rows with one), sums of p
+  // [blocks][E]
+  uint32_t* part_counts;
+  float* part_p;
+  int blocks;
+  double coef;
+  int64_t* counts;
+  float* loss;
+  // backward
+  const int32_t* chosen;
+  const float* w;
+  const int64_t* all_counts;
+  const float* dw;
+  const float* dloss;
+  void* dz;
+  int64_t ldd;
+};
+
+template <int G, int OFF = 1>
+__device__ inline float slot_max(float v) {
+  if constexpr (OFF < G) return slot_max<G, 2 * OFF>(fmaxf(v, slot_partner<OFF>(v)));
+  return v;
+}
+template <int G, int OFF = 1>
+__device__ inline int slot_min(int v) {
+  if constexpr (OFF < G) return slot_min<G, 2 * OFF>(min(v, slot_partner<OFF>(v)));
+  return v;
+}
+
+// The V logits of a lane, -inf behind the row's end.
+template <class T, int V>
+__device__ inline void load_logits(const T* row, int f, int E, float (&z)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; i += 8) {
+    float v[8];
+    unpack8(load8(row, f + i, E), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[i + e] = f + i + e < E ? v[e] : -INFINITY;
+  }
+}
+
+// p of the row: e / sum. A row of -inf alone: zeros, and false.
+template <int G, int V>
+__device__ inline bool softmax(const float (&z)[V], float (&p)[V], float* top) {
+  float m = -INFINITY, s = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    m = fmaxf(m, z[i]);
+    nan |= z[i] != z[i];
+  }
+  m = slot_max<G>(m);
+  *top = m;
+  const bool any = m > -INFINITY;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    p[i] = any || nan ? expf(z[i] - (any ? m : 0.f)) : 0.f;
+    s += p[i];
+  }
+  s = slot_sum<G>(s);
+  const float inv = s == 0.f ? 0.f : 1.f / s;
+#pragma unroll
+  for (int i = 0; i < V; ++i) p[i] *= inv;
+  return any;
+}
+
+template <int V>
+__device__ inline float element(const float (&v)[V], int i) {
+  float r = v[0];
+#pragma unroll
+  for (int e = 1; e < V; ++e) r = i == e ? v[e] : r;
+  return r;
+}
+
+// counts, their number of rows and the loss from the workgroups' sums, by one workgroup.
+__device__ inline void finish(const RouteArgs& a, int threads) {
+  __shared__ double sums[2][16];
+  double cp = 0.0, c = 0.0;
+  int64_t rows = 0;
+  for (int e = threadIdx.x; e <= a.E; e += threads) {
+    int64_t n = 0;
+    for (int b = 0; b < a.blocks; ++b) n += a.part_counts[(int64_t)b * (a.E + 1) + e];
+    a.counts[e] = n;
+    if (e == a.E || !a.loss) continue;
+    double p = 0.0;
+    for (int b = 0; b < a.blocks; ++b) p += (double)a.part_p[(int64_t)b * a.E + e];
+    cp += (double)n * p;
+    c += (double)n;
+  }
+  if (!a.loss) return;
+  const int w = threadIdx.x >> 6;
+  cp = slot_sum<64>(cp);
+  c = slot_sum<64>(c);
+  if ((threadIdx.x & 63) == 0) {
+    sums[0][w] = cp;
+    sums[1][w] = c;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int q = 1; q < threads / 64; ++q) {
+      cp += sums[0][q];
+      c += sums[1][q];
+    }
+    for (int b = 0; b < a.blocks; ++b) rows += a.part_counts[(int64_t)b * (a.E + 1) + a.E];
+    // (without a choice p is 0 or, of rows that hold a NaN alone, NaN)
+    const double all = c * (double)rows;
+    *a.loss = (float)(a.coef * a.E * (all > 0.0 ? cp / all : cp));
+  }
+}
+
+template <class T, int G, int V>
+__global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
+  constexpr int kSlots = kThreads / G;  // rows at a time
+  __shared__ uint32_t cnt[kMaxExperts + 1];
+  __shared__ float sums[kWaves][G * V];
+  // a row's choices, until their sum is known (k <= min(E, 64) <= 8 G)
+  constexpr int kMost = V * G < 64 ? V * G : 64;
+  __shared__ int32_t found_at[kSlots][kMost];
+  __shared__ float found_p[kSlots][kMost];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, in = threadIdx.x % G, f = in * V;
+  for (int e = threadIdx.x; e <= a.E; e += kThreads) cnt[e] = 0;
+  __syncthreads();
+  float acc[V] = {};
+  for (int64_t t0 = (int64_t)blockIdx.x * kSlots; t0 < a.n; t0 += (int64_t)gridDim.x * kSlots) {
+    const int64_t t = t0 + threadIdx.x / G;
+    const bool row = t < a.n && (!a.mask || a.mask[t] != 0);
+    float z[V], p[V], top;
+    load_logits(static_cast<const T*>(a.z) + (row ? t : 0) * a.ldz, f, row ? a.E : 0, z);
+    const bool any = softmax<G>(z, p, &top);
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] += p[i];
+    if (any && in == 0) atomicAdd(&cnt[a.E], 1u);
+    const int slot = threadIdx.x / G;
+    float sum = 0.f;
+    for (int i = 0; i < a.k; ++i) {
+      if (i > 0) {
+        top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < V; ++e) top = fmaxf(top, z[e]);
+        top = slot_max<G>(top);
+      }
+      int at = G * V;
+#pragma unroll
+      for (int e = V - 1; e >= 0; --e) at = z[e] == top ? f + e : at;
+      at = slot_min<G>(at);
+      const bool found = top > -INFINITY && at < a.E;
+      if (found ? at / V == in : in == 0) {
+        float pi = 0.f;
+        if (found) {
+          pi = element(p, at - f);
+#pragma unroll
+          for (int e = 0; e < V; ++e) z[e] = e == at - f ? -INFINITY : z[e];
+          atomicAdd(&cnt[at], 1u);
+        }
+        sum += pi;
+        found_at[slot][i] = found ? at : -1;
+        found_p[slot][i] = pi;
+      }
+    }
+    sum = slot_sum<G>(sum);
+    // (a row's lanes are of one wavefront, whose LDS operations take effect in order; the fence
+    // keeps the compiler from moving the loads before the stores)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (t < a.n)
+      for (int i = in; i < a.k; i += G) {
+        const int at = found_at[slot][i];
+        const float w = found_p[slot][i];
+        a.experts[t * a.k + i] = at;
+        a.weights[t * a.k + i] = a.normalize && at >= 0 ? w / sum : w;
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e <= a.E; e += kThreads)
+    a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = cnt[e];
+  if (!a.loss) return;
+  // the slots of a wavefront, then the wavefronts, in their order
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+#pragma unroll
+    for (int off = G; off < 64; off *= 2) acc[i] += __shfl_xor(acc[i], off, 64);
+    if (lane < G) sums[w][f + i] = acc[i];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.E; e += kThreads) {
+    float s = 0.f;
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) s += sums[q][e];
+    a.part_p[(int64_t)blockIdx.x * a.E + e] = s;
+  }
+}
+
+__global__ __launch_bounds__(1024) void k_finish(RouteArgs a) { finish(a, 1024); }
+
+template <class T, int G, int V>
+__global__ __launch_bounds__(kThreads) void k_route_bwd(RouteArgs a) {
+  constexpr int kSlots = kThreads / G;
+  const int in = threadIdx.x % G, f = in * V;
+  // a_e of the balance loss
+  float bal[V] = {};
+  if (a.coef != 0.0) {
+    double c[V], all = 0.0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      c[i] = f + i < a.E ? (double)a.all_counts[f + i] : 0.0;
+      all += c[i];
+    }
+    all = slot_sum<G>(all) * (double)a.all_counts[a.E];
+    const double s = all > 0.0 ? a.coef * a.E * (a.dloss ? (double)*a.dloss : 1.0) / all : 0.0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) bal[i] = (float)(s * c[i]);
+  }
+  for (int64_t t0 = (int64_t)blockIdx.x * kSlots; t0 < a.n; t0 += (int64_t)gridDim.x * kSlots) {
+    const int64_t t = t0 + threadIdx.x / G;
+    const bool in_rows = t < a.n;
+    const bool row = in_rows && a.chosen[t * a.k] >= 0;
+    float z[V], p[V], d[V] = {}, top;
+    load_logits(static_cast<const T*>(a.z) + (row ? t : 0) * a.ldz, f, row ? a.E : 0, z);
+    softmax<G>(z, p, &top);
+    float inner = 0.f;  // sum of g w over the chosen
+    if (row && a.dw)
+      for (int i = 0; i < a.k; ++i)
+        if (a.chosen[t * a.k + i] >= 0) inner += a.dw[t * a.k + i] * a.w[t * a.k + i];
+    if (row && a.dw)
+      for (int i = 0; i < a.k; ++i) {
+        const int at = a.chosen[t * a.k + i];
+        if (at < 0 || at >= a.E) continue;
+        const float g = a.dw[t * a.k + i];
+        const float x = a.w[t * a.k + i] * (a.normalize ? g - inner : g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] += f + e == at ? x : 0.f;
+      }
+    float mean = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) mean += bal[i] * p[i];
+    mean = slot_sum<G>(mean) + (a.normalize ? 0.f : inner);
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] += p[i] * (bal[i] - mean);
+    if (in_rows)
+#pragma unroll
+      for (int i = 0; i < V; i += 8) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = row ? d[i + e] : 0.f;
+        store8(static_cast<T*>(a.dz) + t * a.ldd, f + i, a.E, v);
+      }
+  }
+}
+
+// Rows at a time of a workgroup.
+inline int route_lanes(int64_t E) {
+  int g = 1;
+  while (g < 64 && g * 8 < E) g *= 2;
+  return g;
+}
+int route_blocks(int64_t n, int64_t E) {
+  return (int)std::min<int64_t>(512, ceil_div(n, (int64_t)(kThreads / route_lanes(E))));
+}
+
+template <class T, bool BWD>
+gcn_status launch(const RouteArgs& a, int blocks, hipStream_t s) {
+  auto go = [&](auto lanes, auto values) {
+    constexpr int G = decltype(lanes)::value, V = decltype(values)::value;
+    if constexpr (BWD)
+      hipLaunchKernelGGL((k_route_bwd<T, G, V>), dim3(blocks), dim3(kThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL((k_route<T, G, V>), dim3(blocks), dim3(kThreads), 0, s, a);
+  };
+  std::integral_constant<int, 8> v8;
+  switch (route_lanes(a.E)) {
+    case 1: go(std::integral_constant<int, 1>(), v8); break;
+    case 2: go(std::integral_constant<int, 2>(), v8); break;
+    case 4: go(std::integral_constant<int, 4>(), v8); break;
+    case 8: go(std::integral_constant<int, 8>(), v8); break;
+    case 16: go(std::integral_constant<int, 16>(), v8); break;
+    case 32: go(std::integral_constant<int, 32>(), v8); break;
+    default:
+      if (a.E <= 512)
+        go(std::integral_constant<int, 64>(), v8);
+      else
+        go(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+  }
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
+gcn_status check_route(int64_t n, int64_t E, int dtype, int64_t k, uint32_t flags, double coef) {
+  GCN_CHECK(check_rows(n, std::max<int64_t>(E, 0), dtype));
+  if (E > kMaxExperts || k < 1 || k > std::min<int64_t>(E, 64) || (flags & ~GCN_ROUTE_NORMALIZE) ||
+      !std::isfinite(coef)) {
+    set_error("need E in [1, 1024], k in [1, min(E, 64)], known flags and a finite coef");
+    return GCN_EINVAL;
+  }
+  if (n * k >= (int64_t(1) << 31)) {
+    set_error("need n k < 2^31");
+    return GCN_ERANGE;
+  }
+  return GCN_OK;
+}
+
+}  // namespace
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" gcn_status gcn_route_fwd(int64_t n, int64_t E, const void* logits, int64_t ldz,
+                                    int dtype, int64_t k, uint32_t flags, const uint8_t* mask,
+                                    double coef, int32_t* experts, float* weights, int64_t* counts,
+                                    float* loss, void* work, int64_t* work_bytes, void* stream) {
+  clear_error();
+  CallScope scope(stream);
+  GCN_CHECK(check_route(n, E, dtype, k, flags, coef));
+  GCN_CHECK(check_work(work, work_bytes));
+  hipStream_t s = (hipStream_t)stream;
+  Scratch scratch(work, work_bytes, s);
+  if (!counts || (n > 0 && (!logits || !experts || !weights || ldz < E))) {
+    set_error("logits, experts, weights and counts must be non-NULL with ldz >= E");
+    return GCN_EINVAL;
+  }
+  RouteArgs a{};
+  a.n = n;
+  a.E = (int)E;
+  a.k = (int)k;
+  a.z = logits;
+  a.ldz = ldz;
+  a.normalize = flags & GCN_ROUTE_NORMALIZE;
+  a.mask = mask;
+  a.weights = weights;
+  a.experts = experts;
+  a.coef = coef;
+  a.counts = counts;
+  a.loss = loss;
+  a.blocks = route_blocks(n, E);
+  if (a.blocks > 0) {
+    GCN_CHECK(scratch.alloc(&a.part_counts, a.blocks * (E + 1), "counts of workgroups"));
+    if (loss) GCN_CHECK(scratch.alloc(&a.part_p, a.blocks * E, "sums of workgroups"));
+  }
+  if (scratch.asked()) return GCN_OK;
+  ProfScope ps("route_fwd", s);
+  if (a.blocks > 0)
+    GCN_CHECK((dtype == GCN_DT_F32 ? launch<float, false>(a, a.blocks, s)
+                                   : launch<bf16, false>(a, a.blocks, s)));
+  hipLaunchKernelGGL(k_finish, dim3(1), dim3(1024), 0, s, a);
+  GCN_HIP(hipGetLastError());
+  return GCN_OK;
+}
+
+extern "C" gcn_status gcn_route_bwd(int64_t n, int64_t E, const void* logits, int64_t ldz,
+                                    int dtype, int64_t k, uint32_t flags, const int32_t* experts,
+                                    const float* weights, const int64_t* counts, double coef,
+                                    const float* dweights, const float* dloss, void* dlogits,
+                                    int64_t ldd, void* stream) {
+  clear_error();
+  GCN_CHECK(check_route(n, E, dtype, k, flags, coef));
+  if (n == 0) return GCN_OK;
+  if (!logits || !experts || (dweights && !weights) || (coef != 0.0 && !counts) || !dlogits ||
+      ldz < E || ldd < E || (logits == dlogits && ldz != ldd)) {
+    set_error("logits, experts, dlogits, the weights of dweights and the counts of coef must be "
+              "non-NULL, with ldz, ldd >= E (and one stride where dlogits are the logits)");
+    return GCN_EINVAL;
+  }
+  RouteArgs a{};
+  a.n = n;
+  a.E = (int)E;
+  a.k = (int)k;
+  a.z = logits;
+  a.ldz = ldz;
+  a.normalize = flags & GCN_ROUTE_NORMALIZE;
+  a.coef = coef;
+  a.chosen = experts;
+  a.w = weights;
+  a.all_counts = counts;
+  a.dw = dweights;
+  a.dloss = dloss;
+  a.dz = dlogits;
+  a.ldd = ldd;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps("route_bwd", s);
+  const int blocks = (int)std::min<int64_t>(2048, ceil_div(n, (int64_t)(kThreads / route_lanes(E))));
+  return dtype == GCN_DT_F32 ? launch<float, true>(a, blocks, s) : launch<bf16, true>(a, blocks, s);
+}

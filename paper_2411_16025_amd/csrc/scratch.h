@@ -5,6 +5,12 @@
 
 namespace gcn {
 
+inline gcn_status check_work(const void* work, const int64_t* work_bytes) {
+  if (!work || (work_bytes && reinterpret_cast<uintptr_t>(work) % 256 == 0)) return GCN_OK;
+  set_error("work memory needs work_bytes and an alignment of 256 bytes");
+  return GCN_EINVAL;
+}
+
 // With `bytes`, a call's work arguments are: where `work` is null, a question for the
 // bytes (asked() is true after the allocations: the call ends there); else memory of so many
 // bytes. Without `bytes` the memory comes from the library's temporaries, and not on a

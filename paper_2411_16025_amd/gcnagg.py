@@ -23,6 +23,8 @@ GCN_DT_BF16 = 1
 GCN_Q8_USE_CSC = 1
 GCN_Q_CODES_2BIT = 2
 GCN_LAYERNORM = 1
+GCN_ACCUMULATE = 1
+GCN_ROUTE_NORMALIZE = 1
 
 STATUS = {0: "GCN_OK", 1: "GCN_EINVAL", 2: "GCN_ERANGE", 3: "GCN_ENOMEM", 4: "GCN_EHIP",
           5: "GCN_ESTATE"}
@@ -37,6 +39,8 @@ EXPORTS = ("gcn_build_csr", "gcn_normalize", "gcn_normalize_rc", "gcn_normalize_
            "gcn_aggregate_fwd_q8halo", "gcn_quantize_rows_u8", "gcn_layernorm_quantize",
            "gcn_gemm_f32", "gcn_relu", "gcn_gemm_grouped", "gcn_dropout",
            "gcn_layernorm_affine_fwd", "gcn_layernorm_affine_bwd",
+           "gcn_group_ids", "gcn_embed_fwd", "gcn_embed_bwd", "gcn_route_fwd", "gcn_route_bwd",
+           "gcn_combine_fwd", "gcn_combine_bwd", "gcn_pack8", "gcn_unpack8", "gcn_gemm_grouped_q8",
            "gcn_relu_bwd", "gcn_softmax_xent", "gcn_gcn2_step", "gcn_graph_free",
            "gcn_graph_info", "gcn_graph_export", "gcn_graph_bins", "gcn_profile_enable",
            "gcn_profile_read", "gcn_last_error")
@@ -94,6 +98,18 @@ def lib():
                                                i64, P]
         L.gcn_layernorm_affine_bwd.argtypes = [i64, i64, P, i64, i32, P, ctypes.c_double, P, P, i64,
                                                P, i64, P, P, P, P, P]
+        f64 = ctypes.c_double
+        L.gcn_group_ids.argtypes = [i64, P, i64, P, P, P, P, P, P]
+        L.gcn_embed_fwd.argtypes = [i64, i64, i64, P, i64, P, i64, i32, f64, P, i64, i32, P]
+        L.gcn_embed_bwd.argtypes = [i64, i64, i64, P, P, P, i64, i32, f64, P, i64, i32, u32, P, P, P]
+        L.gcn_route_fwd.argtypes = [i64, i64, P, i64, i32, i64, u32, P, f64, P, P, P, P, P, P, P]
+        L.gcn_route_bwd.argtypes = [i64, i64, P, i64, i32, i64, u32, P, P, P, f64, P, P, P, i64, P]
+        L.gcn_combine_fwd.argtypes = [i64, i64, i64, P, i64, i64, i32, P, P, P, i64, P]
+        L.gcn_combine_bwd.argtypes = [i64, i64, i64, P, i64, i64, i32, P, P, P, i64, P, i64, P, P]
+        L.gcn_pack8.argtypes = [i64, i64, P, i64, i32, P, i64, P, i64, P]
+        L.gcn_unpack8.argtypes = [i64, i64, P, i64, P, i64, P, i64, i32, P]
+        L.gcn_gemm_grouped_q8.argtypes = [i64, P, i64, i64, i64, P, i64, P, i64, P, i64, i32, P, i64,
+                                          i64, P, P, P]
         L.gcn_graph_free.argtypes = [P]
         L.gcn_graph_free.restype = None
         L.gcn_graph_info.argtypes = [P, P, P, P]
@@ -823,6 +839,242 @@ def gcn_layernorm_affine_bwd(X: torch.Tensor, dY: torch.Tensor, gamma=None, eps:
         n, F, X.data_ptr(), ldx, code, g, eps, spec, dY.data_ptr(), lddy, ptr(dX), lddx,
         ptr(dgamma), ptr(dbeta), work, size, s), X.device, stream)
     return dX, dgamma, dbeta
+
+
+def _flat(t, dtype, count, name):
+    """A contiguous tensor of `count` values (any shape)."""
+    _dev(t, dtype, name)
+    if t.numel() != count or not t.is_contiguous():
+        raise ValueError("%s must hold %d contiguous values" % (name, count))
+    return t.data_ptr()
+
+
+def _out(t, shape, dtype, device, name, stream):
+    """t, or a new one."""
+    if t is None:
+        return _new(shape, dtype, device, stream)
+    _dev(t, dtype, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s" % (name, tuple(shape)))
+    return t
+
+
+def gcn_group_ids(ids: torch.Tensor, n_groups: int, slots: bool = True, stream=None):
+    """(offsets int64 [n_groups + 1], order int32 [n], slot int32 [n] or None): the positions
+    of ids (int32) sorted by group, stable; ids outside [0, n_groups) get slot -1, and the
+    places behind the last group hold -1 in order."""
+    _dev(ids, torch.int32, "ids")
+    if ids.dim() != 1 or not ids.is_contiguous():
+        raise ValueError("ids must be 1-D and contiguous")
+    _on_current_device(ids)
+    n = ids.numel()
+    offsets = _new((n_groups + 1 if n_groups > 0 else 0,), torch.int64, ids.device, stream)
+    order = _new((n,), torch.int32, ids.device, stream)
+    slot = _new((n,), torch.int32, ids.device, stream) if slots else None
+    _with_work(lambda work, size, s: lib().gcn_group_ids(
+        n, ids.data_ptr(), n_groups, offsets.data_ptr(), order.data_ptr(),
+        slot.data_ptr() if slots else None, work, size, s), ids.device, stream)
+    return offsets, order, slot
+
+
+def gcn_embed_fwd(T: torch.Tensor, ids: torch.Tensor, per: int = 1, scale: float = 1.0,
+                  out_dtype: torch.dtype | None = None, Y: torch.Tensor | None = None, stream=None):
+    """Y[i] = scale * T[ids[i] / per] (ids int32); rows of ids outside [0, rows of T * per) are 0."""
+    code = _dtype_code(_dev(T, None, "T"))
+    ldt = _ld(T, "T")
+    V, F = T.shape
+    p = _flat(ids, torch.int32, ids.numel(), "ids")
+    if ids.dim() != 1:
+        raise ValueError("ids must be 1-D")
+    n = ids.numel()
+    dt = out_dtype if out_dtype is not None else (Y.dtype if Y is not None else T.dtype)
+    Y = _out(Y, (n, F), dt, T.device, "Y", stream)
+    _on_current_device(T, ids, Y)
+    _check(lib().gcn_embed_fwd(n, F, V, p, per, T.data_ptr(), ldt, code, scale, Y.data_ptr(),
+                               _ld(Y, "Y"), _dtype_code(Y), _stream(stream)))
+    return Y
+
+
+def gcn_embed_bwd(dY: torch.Tensor, offsets: torch.Tensor, order: torch.Tensor, scale: float = 1.0,
+                  out_dtype: torch.dtype | None = None, dT: torch.Tensor | None = None,
+                  accumulate: bool = False, stream=None):
+    """dT[v] = scale * the sum of dY[order[j]] over offsets[v] <= j < offsets[v + 1], from
+    gcn_group_ids(ids, V); with accumulate added to the dT that is given. Type: out_dtype, else
+    dT's, else fp32."""
+    code = _dtype_code(_dev(dY, None, "dY"))
+    lddy = _ld(dY, "dY")
+    n, F = dY.shape
+    _dev(offsets, torch.int64, "offsets")
+    if offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+        raise ValueError("offsets must be contiguous with V + 1 entries")
+    V = offsets.numel() - 1
+    po = _flat(order, torch.int32, n, "order")
+    if accumulate and dT is None:
+        raise ValueError("accumulate needs dT")
+    dt = out_dtype if out_dtype is not None else (dT.dtype if dT is not None else torch.float32)
+    dT = _out(dT, (V, F), dt, dY.device, "dT", stream)
+    _on_current_device(dY, offsets, order, dT)
+    code_t, lddt = _dtype_code(dT), _ld(dT, "dT")
+    _with_work(lambda work, size, s: lib().gcn_embed_bwd(
+        n, F, V, offsets.data_ptr(), po, dY.data_ptr(), lddy, code, scale, dT.data_ptr(), lddt,
+        code_t, GCN_ACCUMULATE if accumulate else 0, work, size, s), dY.device, stream)
+    return dT
+
+
+def gcn_route_fwd(logits: torch.Tensor, k: int, mask: torch.Tensor | None = None,
+                  coef: float | None = None, normalize: bool = False, stream=None):
+    """(experts int32 [n, k], weights fp32 [n, k], counts int64 [E + 1], loss fp32 or None): the k
+    largest logits of each row, their softmax weights (normalize: divided by their sum), how often
+    each expert was chosen and, last, by how many rows; with coef the balance loss."""
+    code = _dtype_code(_dev(logits, None, "logits"))
+    ldz = _ld(logits, "logits")
+    n, E = logits.shape
+    pm = _flat(mask, torch.uint8, n, "mask") if mask is not None else None
+    _on_current_device(logits, mask)
+    rows = (n, max(k, 0))
+    experts = _new(rows, torch.int32, logits.device, stream)
+    weights = _new(rows, torch.float32, logits.device, stream)
+    counts = _new((E + 1,), torch.int64, logits.device, stream)
+    loss = _new((), torch.float32, logits.device, stream) if coef is not None else None
+    _with_work(lambda work, size, s: lib().gcn_route_fwd(
+        n, E, logits.data_ptr(), ldz, code, k, GCN_ROUTE_NORMALIZE if normalize else 0, pm,
+        coef if coef is not None else 0.0, experts.data_ptr(), weights.data_ptr(), counts.data_ptr(),
+        loss.data_ptr() if loss is not None else None, work, size, s), logits.device, stream)
+    return experts, weights, counts, loss
+
+
+def gcn_route_bwd(logits: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor,
+                  counts: torch.Tensor | None = None, dweights: torch.Tensor | None = None,
+                  coef: float | None = None, normalize: bool = False,
+                  dloss: torch.Tensor | None = None, dlogits: torch.Tensor | None = None,
+                  stream=None):
+    """dlogits (which may be the logits themselves) of gcn_route_fwd, from its outputs and the
+    gradients dweights (fp32 [n, k], None: 0) and dloss (fp32 on the GPU, None: 1; with coef)."""
+    code = _dtype_code(_dev(logits, None, "logits"))
+    ldz = _ld(logits, "logits")
+    n, E = logits.shape
+    if experts.dim() != 2 or experts.shape[0] != n:
+        raise ValueError("experts must be [n, k]")
+    k = experts.shape[1]
+    ptr = lambda t, dt, count, nm: _flat(t, dt, count, nm) if t is not None else None  # noqa: E731
+    pe = _flat(experts, torch.int32, n * k, "experts")
+    pw = _flat(weights, torch.float32, n * k, "weights")
+    pc = ptr(counts, torch.int64, E + 1, "counts")
+    pd = ptr(dweights, torch.float32, n * k, "dweights")
+    pl = ptr(dloss, torch.float32, 1, "dloss")
+    dlogits = _rows_out(logits, dlogits, "dlogits", stream)
+    _on_current_device(logits, experts, weights, counts, dweights, dloss, dlogits)
+    _check(lib().gcn_route_bwd(n, E, logits.data_ptr(), ldz, code, k,
+                               GCN_ROUTE_NORMALIZE if normalize else 0, pe, pw, pc,
+                               coef if coef is not None else 0.0, pd, pl, dlogits.data_ptr(),
+                               _ld(dlogits, "dlogits"), _stream(stream)))
+    return dlogits
+
+
+def _slots(slot, weights):
+    _dev(slot, torch.int32, "slot")
+    if slot.dim() != 2 or not slot.is_contiguous():
+        raise ValueError("slot must be [n, k] and contiguous")
+    n, k = slot.shape
+    return n, k, _flat(weights, torch.float32, n * k, "weights") if weights is not None else None
+
+
+def gcn_combine_fwd(Z: torch.Tensor, slot: torch.Tensor, weights: torch.Tensor | None = None,
+                    Y: torch.Tensor | None = None, stream=None):
+    """Y[t] = sum_i weights[t, i] Z[slot[t, i]] (weights None: 1); slots outside the rows of Z take
+    no part. Without weights it is the gradient of gcn_embed_fwd(X, order, per=k)."""
+    code = _dtype_code(_dev(Z, None, "Z"))
+    ldz = _ld(Z, "Z")
+    n, k, pw = _slots(slot, weights)
+    Y = _out(Y, (n, Z.shape[1]), Z.dtype, Z.device, "Y", stream)
+    _on_current_device(Z, slot, weights, Y)
+    _check(lib().gcn_combine_fwd(n, k, Z.shape[1], Z.data_ptr(), Z.shape[0], ldz, code,
+                                 slot.data_ptr(), pw, Y.data_ptr(), _ld(Y, "Y"), _stream(stream)))
+    return Y
+
+
+def gcn_combine_bwd(Z: torch.Tensor, slot: torch.Tensor, weights: torch.Tensor | None,
+                    dY: torch.Tensor, dZ: torch.Tensor | None = None, input_grad: bool = True,
+                    weight_grad: bool = True, stream=None):
+    """(dZ, dweights) of gcn_combine_fwd; no slot may occur twice. dZ (which may be Z itself) keeps
+    what it holds in rows that are no slot's: a dZ that is made here holds nothing defined in them.
+    None without input_grad or weight_grad."""
+    code = _dtype_code(_dev(Z, None, "Z"))
+    _dev(dY, Z.dtype, "dY")
+    ldz, lddy = _ld(Z, "Z"), _ld(dY, "dY")
+    n, k, pw = _slots(slot, weights)
+    F = Z.shape[1]
+    if tuple(dY.shape) != (n, F):
+        raise ValueError("dY must be %s" % ((n, F),))
+    dZ = _rows_out(Z, dZ, "dZ", stream) if input_grad else None
+    dw = _new((n, k), torch.float32, Z.device, stream) if weight_grad else None
+    _on_current_device(Z, slot, weights, dY, dZ)
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    _check(lib().gcn_combine_bwd(n, k, F, Z.data_ptr(), Z.shape[0], ldz, code, slot.data_ptr(), pw,
+                                 dY.data_ptr(), lddy, ptr(dZ), _ld(dZ, "dZ") if input_grad else 0,
+                                 ptr(dw), _stream(stream)))
+    return dZ, dw
+
+
+def gcn_pack8(X: torch.Tensor, stream=None):
+    """(Q int8 [n, F], S uint8 [n, (F + 31) / 32]): rows in 8 bits, 32 columns under one power of two."""
+    code = _dtype_code(_dev(X, None, "X"))
+    ldx = _ld(X, "X")
+    n, F = X.shape
+    Q = _new((n, F), torch.int8, X.device, stream)
+    S = _new((n, (F + 31) // 32), torch.uint8, X.device, stream)
+    _on_current_device(X)
+    _check(lib().gcn_pack8(n, F, X.data_ptr(), ldx, code, Q.data_ptr(), F, S.data_ptr(), S.shape[1],
+                           _stream(stream)))
+    return Q, S
+
+
+def _packed(Q, S):
+    """(row strides of the codes and of the scale bytes)"""
+    _dev(Q, torch.int8, "Q")
+    _dev(S, torch.uint8, "S")
+    ldq, lds = _ld(Q, "Q"), _ld(S, "S")
+    if tuple(S.shape) != (Q.shape[0], (Q.shape[1] + 31) // 32):
+        raise ValueError("S must hold one byte per 32 columns of Q")
+    return ldq, lds
+
+
+def gcn_unpack8(Q: torch.Tensor, S: torch.Tensor, out_dtype: torch.dtype | None = None,
+                Y: torch.Tensor | None = None, stream=None):
+    """The values of gcn_pack8's codes (type: out_dtype, else Y's, else fp32)."""
+    ldq, lds = _packed(Q, S)
+    dt = out_dtype if out_dtype is not None else (Y.dtype if Y is not None else torch.float32)
+    Y = _out(Y, tuple(Q.shape), dt, Q.device, "Y", stream)
+    _on_current_device(Q, S, Y)
+    _check(lib().gcn_unpack8(Q.shape[0], Q.shape[1], Q.data_ptr(), ldq, S.data_ptr(), lds,
+                             Y.data_ptr(), _ld(Y, "Y"), _dtype_code(Y), _stream(stream)))
+    return Y
+
+
+def gcn_gemm_grouped_q8(offsets: torch.Tensor, Q: torch.Tensor, S: torch.Tensor, B: torch.Tensor,
+                        C: torch.Tensor | None = None, stream=None):
+    """C[g] = X_g^T B_g (fp32 [groups, K, N]) over the rows [offsets[g], offsets[g + 1]), X [rows, K]
+    the values of gcn_pack8's codes, B [rows, N] fp32 or bf16."""
+    _dev(offsets, torch.int64, "offsets")
+    if offsets.dim() != 1 or offsets.numel() < 2 or not offsets.is_contiguous():
+        raise ValueError("offsets must be contiguous with groups + 1 entries")
+    G = offsets.numel() - 1
+    ldq, lds = _packed(Q, S)
+    code = _dtype_code(_dev(B, None, "B"))
+    ldb = _ld(B, "B")
+    rows, K = Q.shape
+    if B.shape[0] != rows:
+        raise ValueError("Q and B must have the same rows")
+    N = B.shape[1]
+    C = _out(C, (G, K, N), torch.float32, B.device, "C", stream)
+    if C.stride(2) != 1 and N > 1:
+        raise ValueError("C must have unit column stride")
+    ldc = max(C.stride(1), N) if K <= 1 else C.stride(1)
+    _on_current_device(offsets, Q, S, B, C)
+    _with_work(lambda work, size, s: lib().gcn_gemm_grouped_q8(
+        G, offsets.data_ptr(), rows, N, K, Q.data_ptr(), ldq, S.data_ptr(), lds, B.data_ptr(), ldb,
+        code, C.data_ptr(), ldc, C.stride(0), work, size, s), B.device, stream)
+    return C
 
 
 def gcn_graph_info(g: Graph):

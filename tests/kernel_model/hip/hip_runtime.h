@@ -84,6 +84,19 @@ inline long long __double_as_longlong(double v) { return __builtin_bit_cast(long
 inline double __longlong_as_double(long long v) { return __builtin_bit_cast(double, v); }
 inline int __clzll(long long v) { return v ? __builtin_clzll((unsigned long long)v) : 64; }
 
+inline int __popcll(unsigned long long v) { return __builtin_popcountll(v); }
+template <class T>
+T atomicAdd(T* p, T v) {  // (of a workgroup's own memory: threads run one at a time)
+  const T old = *p;
+  *p += v;
+  return old;
+}
+// the lanes of a wavefront do what stands before it before any does what stands behind it
+inline void __builtin_amdgcn_fence(int, const char*) {
+  const char c = 0;
+  model::give("fence", &c, 1);
+}
+
 inline uint64_t __ballot(bool p) {
   const model::Given& g = model::give("ballot", &p, sizeof p);
   uint64_t m = 0;
@@ -95,6 +108,11 @@ inline bool __any(bool p) { return __ballot(p) != 0; }
 template <class T>
 T __shfl_xor(T v, int off, int) {
   return model::from_lane("shfl_xor", v, model::lane() ^ off);
+}
+template <class T>
+T __shfl_up(T v, unsigned off, int) {
+  const int from = model::lane() - (int)off;
+  return model::from_lane("shfl_up", v, from < 0 ? model::lane() : from);
 }
 inline int __builtin_amdgcn_readlane(int v, int l) { return model::from_lane("readlane", v, l); }
 inline int __builtin_amdgcn_readfirstlane(int v) {
