@@ -90,6 +90,8 @@ class Engine:
             conv = lambda v: np.asarray(v, NUMPY[kind])  # noqa: E731
         ld = F + pad
         flat = np.empty(max((n - 1) * ld + F, 0) if n else 0, NUMPY[kind])
+        if kind not in ("f32", "bf16") and fill != fill:
+            fill = 77
         flat[:] = conv(np.full(1, fill, np.float32 if kind in ("f32", "bf16") else NUMPY[kind]))[0]
         for i in range(n):
             flat[i * ld:i * ld + F] = conv(np.ascontiguousarray(x[i]))

@@ -406,3 +406,43 @@ def check_grad8(e, sizes, K, N, kind="f32", before=0, after=0, pad=0, memory=0, 
             bound = (min(sizes[g], 65536) + 8) * U * (np.abs(x).T @ np.abs(y))
             assert (np.abs(got[g] - want) <= bound).all(), (what, g)
     c.check_margins()
+
+
+def check_grad8_special(e, rows, K, N, kind="f32", seed=0):
+    """Rows of B with infinities, NaN, the largest and the smallest numbers, and rows of X that stand for NaN:
+    in whole columns, so that sums have one value whatever their order."""
+    r = np.random.default_rng(seed)
+    q, s = pack8(r.standard_normal((rows, K)))
+    b = rounded(r.standard_normal((rows, N)), kind)
+    one = np.zeros((rows, N), np.float32)
+    one[rows // 2] = 1
+    b[:, 0] = np.where(one[:, 0] > 0, np.inf, 0)  # sums are infinite, or NaN where q is 0
+    b[rows // 3, 1] = np.nan
+    b[:, 2] = one[:, 2] * rounded(3.3e38, kind)
+    b[:, 3] *= np.float32(2.0 ** -120)     # (and their lower parts denormal numbers)
+    b[:, 4] = rounded(b[:, 4] * np.float32(2.0 ** 100), kind)
+    b[:, 5] = 0
+    s[rows - 1, 0] = 255
+    q[rows - 1, :32] = 0
+    qd, sd, bd = e.rows(q, "i8", 0), e.rows(s, "u8", 0), e.rows(b, kind, 0)
+    c, o = e.rows(np.full((K, N), 7.0), "f32", 0), e.put(np.array([0, rows], np.int64))
+    Call(e, 0)(e.lib.gcn_gemm_grouped_q8, 1, o.ptr, rows, N, K, qd.ptr, qd.ld, sd.ptr, sd.ld, bd.ptr, bd.ld,
+               CODE[kind], c.ptr, c.ld, K * N)
+    got, x = c.get(), unpack8(q, s)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = x.T @ b.astype(np.float64)
+        mag = np.abs(x).T @ np.abs(b.astype(np.float64))
+    what = (rows, K, N, kind)
+    assert np.isnan(got[:32]).all() and np.isnan(got[:, 1]).all(), what
+    rest = slice(32, K)
+    # bf16 multiplies denormal numbers' lower parts by nothing: its products are exact, but those below 2^-126
+    # and their sums may be lost (8-bit values times 2^-120 normal ones are above 2^-133 times 127)
+    tiny = rows * 2.0 ** -126 if kind == "bf16" else rows * 2.0 ** -149
+    with np.errstate(invalid="ignore", over="ignore"):
+        near = np.abs(got - want) <= (rows + 8) * U * mag + tiny
+        big = np.abs(want) > 3.4e38
+    assert np.array_equal(np.isnan(got[rest, 0]), x[rows // 2, rest] == 0), what
+    assert np.array_equal(np.isinf(got[rest, 0]), x[rows // 2, rest] != 0), what
+    ok = near | (big & np.isinf(got) & (np.sign(got) == np.sign(want)))
+    assert ok[rest, 2:].all(), (what, np.argwhere(~ok[rest, 2:])[:4])
+    assert (got[rest, 5] == 0).all() and not np.signbit(got[rest, 5]).any(), what

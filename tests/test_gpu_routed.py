@@ -81,7 +81,7 @@ class Engine:
         n, F = x.shape
         t = self.types[kind]
         if kind not in KINDS:
-            fill = int(fill)
+            fill = 77 if fill != fill else int(fill)
         flat = self.torch.full((shift + n * (F + pad) + 8,), fill, dtype=t, device="cuda:0")
         v = flat[shift:shift + n * (F + pad)].view(n, F + pad)[:, :F] if n else flat[:0].view(0, F)
         if n:
@@ -252,11 +252,19 @@ def test_pack8(E, n, F, kind, how):
                                        ([130, 700], 64, 64), ([20] * 30, 40, 24), ([0, 0], 5, 5),
                                        ([900, 0, 1], 130, 129), ([513], 256, 264), ([5000, 300], 512, 1000),
                                        ([3000, 0, 2500], 264, 520), ([20000], 8, 8), ([9], 2000, 600),
-                                       ([10] * 1100, 32, 16), ([4000, 1], 100, 2048)])
+                                       ([10] * 1100, 32, 16), ([4000, 1], 100, 2048), ([700, 0, 90], 136, 520),
+                                       ([33, 1] * 3, 16, 8), ([257], 300, 140), ([70, 3], 17, 257),
+                                       ([30000, 5000], 100, 256), ([3000] * 9, 260, 130)])
 def test_grad8(E, sizes, K, N, kind, memory):
     for pad, whole in ((0, True), (8, False), (3, True)):
         run(E, "check_grad8", sizes, K, N, kind=kind, before=pad, after=memory, pad=pad, memory=memory, whole=whole,
             seed=K + N)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,K,N", [(40, 64, 8), (100, 150, 20), (300, 260, 264), (9, 40, 7), (5000, 300, 520)])
+def test_grad8_special(E, rows, K, N, kind):
+    run(E, "check_grad8_special", rows, K, N, kind=kind, seed=K)
 
 
 # ---- a layer --------------------------------------------------------------------------

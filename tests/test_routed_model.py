@@ -123,9 +123,16 @@ def test_pack8(model):
 def test_grad8(model):
     cases = []
     for sizes, K, N in (([1], 1, 1), ([5], 3, 7), ([40, 0, 3], 33, 65), ([300], 100, 47), ([130, 700], 64, 64),
-                        ([20] * 30, 40, 24), ([0, 0], 5, 5), ([900, 0, 1], 130, 129), ([513], 256, 264)):
+                        ([20] * 30, 40, 24), ([0, 0], 5, 5), ([900, 0, 1], 130, 129), ([513], 256, 264),
+                    ([700, 0, 90], 136, 520), ([33, 1] * 3, 16, 8), ([257], 300, 140), ([70, 3], 17, 257),
+                    ([5] * 1030, 20, 9)):
         for i, kind in enumerate(("f32", "bf16")):
             for memory in (0, 1):
                 cases.append(["check_grad8", [sizes, K, N], dict(kind=kind, before=3 * i, after=2 * memory, pad=5 * memory,
                                                                  memory=memory, whole=i == memory, seed=K)])
     model(cases)
+
+
+def test_grad8_special(model):
+    model([["check_grad8_special", [rows, K, N], dict(kind=kind, seed=K)] for kind in ("f32", "bf16")
+           for rows, K, N in ((40, 64, 8), (100, 150, 20), (300, 260, 264), (9, 40, 7))])
