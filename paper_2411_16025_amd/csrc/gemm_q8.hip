@@ -2,6 +2,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "groups.h"
 #include "mul_tile.h"
@@ -217,22 +218,126 @@ struct PartLoader {
 };
 
 // bf16 rows: as in gemm_grouped.hip.
-template <class TB, int X, int BK, int NT, bool DIRECT>
-struct RowLoader : Loader<false, X, BK, NT, DIRECT> {
+template <class TB, int X, int BK, int NT>
+struct RowLoader : Loader<false, X, BK, NT, false> {
   static constexpr int kParts = 1;
 };
-template <int X, int BK, int NT, bool DIRECT>
-struct RowLoader<float, X, BK, NT, DIRECT> : PartLoader<X, BK, NT> {
+template <int X, int BK, int NT>
+struct RowLoader<float, X, BK, NT> : PartLoader<X, BK, NT> {
   static constexpr int kParts = 3;
 };
 
-// A workgroup of WR x WC wavefronts, RB x CB blocks of 32 x 32 of C each. DIRECT: bf16 rows
-// that direct loads take to LDS.
-template <class TB, bool DIRECT, int BK, int WR, int WC, int RB, int CB>
+// A workgroup's part of C and its chunk of a group's rows.
+struct Place {
+  bool any;
+  int m0, n0, g;
+  int64_t first, beg, end, chunk;
+};
+
+// Chunk `slot` of at most 64 groups, the long groups first: lane l has group l's chunks, those of
+// the groups before it are counted by their sizes.
+__device__ inline GroupTile long_first(const Groups& by, const TileCount& c, int slot, int R) {
+  const int lane = threadIdx.x & 63;
+  const int size = lane < by.n ? (int)std::max<int64_t>(0, c.end - c.first) : -1;
+  const int mine = lane < by.n ? tiles_of(size, R, 1) : 0;
+  int before = 0;
+  for (int o = 0; o < by.n; ++o) {
+    const int so = __builtin_amdgcn_readlane(size, o), to = __builtin_amdgcn_readlane(mine, o);
+    before += so > size || (so == size && o < lane) ? to : 0;
+  }
+  const uint64_t at = __ballot(lane < by.n && before <= slot && slot < before + mine);
+  const int l = at ? 63 - __clzll((long long)at) : 0;
+  GroupTile r;
+  r.g = l;
+  r.first = lane_value(c.first, l);
+  r.end = lane_value(c.end, l);
+  r.beg = r.first + (int64_t)(slot - __builtin_amdgcn_readlane(before, l)) * R;
+  return r;
+}
+
+// The XCDs share every chunk's tiles (of fewer than eight, the chunks), and long groups come first:
+// groups of 100 to 5,000 rows, 2048 x 4096: 1128 us where each XCD had an eighth of all tiles in the
+// groups' order, the XCDs of the long ones the most work.
+__device__ inline Place place(const Q8Args& a, int BM, int BN) {
+  Place r{};
+  const int R = (int)a.split;
+  const bool counted = a.by.n <= kCountedGroups;
+  TileCount count{};
+  if (counted) count = count_tiles(a.by, R, 1);
+  const uint32_t slots = counted ? count.total : a.slots;
+  const uint32_t per = a.col_tiles * a.row_tiles, share = (per + 7) / 8, xcd = blockIdx.x & 7;
+  uint32_t slot, t;
+  if (per >= 8) {
+    slot = (blockIdx.x >> 3) / share;
+    const uint32_t x = (xcd + slot) & 7;  // (which XCD has one tile less than others changes)
+    t = per * x / 8 + (blockIdx.x >> 3) % share;
+    if (t >= per * (x + 1) / 8) return r;
+  } else {
+    slot = blockIdx.x / (8 * per) * 8 + xcd;
+    t = (blockIdx.x >> 3) % per;
+  }
+  if (slot >= slots) return r;
+  const GroupTile gt = a.by.n <= 64 ? long_first(a.by, count, (int)slot, R)
+                       : counted    ? counted_tile(a.by, count, (int)slot, R, 1)
+                                    : group_tile(a.by, slot, R);
+  if (gt.beg >= gt.end && gt.beg != gt.first) return r;  // an empty group's first chunk: zeros
+  r.any = true;
+  r.m0 = (int)t / a.col_tiles * BM;
+  r.n0 = (int)t % a.col_tiles * BN;
+  r.g = gt.g;
+  r.first = gt.first;
+  r.beg = gt.beg;
+  r.end = std::max(gt.beg, std::min(gt.beg + a.split, gt.end));
+  r.chunk = (gt.beg - gt.first) / a.split;
+  return r;
+}
+
+// A wavefront's sums, times `down`, to C or to the chunk's partial sums (with 0 added to the
+// product: -0 becomes +0).
+template <int RB, int CB>
+__device__ inline void write_sums(const Q8Args& a, const Place& pl, int m0, int n0,
+                                  const f16 (*acc)[CB], float down) {
+  float* C = a.c + pl.g * a.stride_c;
+  int64_t ldc = a.ldc;
+  if (pl.chunk > 0) {
+    C = a.part + (pl.first / a.split + pl.chunk - 1) * a.K * a.N;
+    ldc = a.N;
+  }
+  const int lane = threadIdx.x & 63;
+  // (addresses: a uniform row, and the lane's part in 32 bits)
+  const uint32_t lane_at = (uint32_t)(4 * (lane >> 5)) * (uint32_t)ldc + (lane & 31);
+  auto write = [&](auto past) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int r = m0 + i * 32 + (e & 3) + 8 * (e >> 2);
+        float* row = C + r * ldc + n0;
+        if (r + 4 * (lane >> 5) >= a.K) continue;
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+          if (n0 + j * 32 + (lane & 31) >= a.N) continue;
+          const float v = __builtin_fmaf(acc[i][j][e], down, 0.f);
+          if constexpr (decltype(past)::value)
+            __builtin_nontemporal_store(v, row + lane_at + j * 32);
+          else
+            row[lane_at + j * 32] = v;
+        }
+      }
+  };
+  // past the caches where rows are whole lines, as in gemm_grouped.hip
+  if (((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(4 * ldc)) & 127) == 0)
+    write(std::true_type{});
+  else
+    write(std::false_type{});
+}
+
+// A workgroup of WR x WC wavefronts, RB x CB blocks of 32 x 32 of C each.
+template <class TB, int BK, int WR, int WC, int RB, int CB>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
   constexpr int NT = 64 * WR * WC, BM = 32 * WR * RB, BN = 32 * WC * CB;
   using LA = CodeLoader<BM, BK, NT>;
-  using LB = RowLoader<TB, BN, BK, NT, DIRECT>;
+  using LB = RowLoader<TB, BN, BK, NT>;
   using TA = Tile<false, BM, BK>;
   using TN = Tile<false, BN, BK>;
   constexpr int NP = LB::kParts;
@@ -240,28 +345,16 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
       b1[NP * TN::kBytes];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = w / WC, wc = w % WC;
-  // the chunks' tiles divide evenly among the XCDs, those of a chunk beside each other
-  const int R = (int)a.split;
-  const bool counted = a.by.n <= kCountedGroups;
-  TileCount count{};
-  if (counted) count = count_tiles(a.by, R, 1);
-  const uint32_t rows = counted ? count.total : a.slots;
-  const uint32_t per = a.col_tiles * a.row_tiles, units = rows * per, xcd = blockIdx.x & 7;
-  const uint32_t u = (uint32_t)((uint64_t)units * xcd / 8) + (blockIdx.x >> 3);
-  if (u >= (uint32_t)((uint64_t)units * (xcd + 1) / 8)) return;
-  const uint32_t slot = u / per;
-  const int m0 = (int)(u % per) / a.col_tiles * BM, n0 = (int)(u % per) % a.col_tiles * BN;
-  const GroupTile gt = counted ? counted_tile(a.by, count, (int)slot, R, 1)
-                               : group_tile(a.by, slot, R);
-  if (gt.beg >= gt.end && gt.beg != gt.first) return;  // an empty group's first chunk: zeros
-  const int64_t k_beg = gt.beg, k_end = std::max(gt.beg, std::min(gt.beg + a.split, gt.end));
-  const int64_t chunk = (gt.beg - gt.first) / a.split;
+  const Place pl = place(a, BM, BN);
+  if (!pl.any) return;
+  const int m0 = pl.m0, n0 = pl.n0;
+  const int64_t k_beg = pl.beg, k_end = pl.end;
   LA la;
   LB lb;
   la.init(a.q + m0, a.ldq, a.s + m0 / 32, a.lds, a.K - m0);
   lb.init(static_cast<const TB*>(a.b) + n0, a.ldb, a.N - n0);
   // (the matrix core's rounding has one sign: every other chunk's sums are of negated products)
-  const uint32_t sign = chunk & 1 ? 0x80000000u : 0;
+  const uint32_t sign = pl.chunk & 1 ? 0x80000000u : 0;
 
   f16 acc[RB][CB];
 #pragma unroll
@@ -322,7 +415,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
     la.store(a0, sign);
     lb.store(b0);
     load(1, b1);
-    wait_loads<DIRECT ? TN::kPieces / NT : 63>();  // stage 0's; the direct loads of stage 1 are the last ones
+    wait_loads<63>();
     read(0, 0, a0, b0);
     for (int64_t s = 0; s < stages; s += 2) {
       stage(s, a0, b0, a1, b1);
@@ -332,14 +425,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
     wait_loads();  // those past the last stage
   }
 
-  float* C = a.c + gt.g * a.stride_c;
-  int64_t ldc = a.ldc;
-  if (chunk > 0) {
-    C = a.part + (gt.first / a.split + chunk - 1) * a.K * a.N;
-    ldc = a.N;
-  }
   float down = NP == 3 ? 1.f / kUp : 1.f;
-  if (chunk & 1) down = -down;
+  if (pl.chunk & 1) down = -down;
   if constexpr (NP == 3) {
     if (not_finite<RB, CB>(acc)) {
       down = 1.f;
@@ -364,38 +451,180 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
       mul_again<RB, CB>(k_beg, k_end, again, acc);
     }
   }
+  write_sums<RB, CB>(a, pl, m0 + wr * RB * 32, n0 + wc * CB * 32, acc, down);
+}
+
+// bf16 rows that start on 16 bytes and hold whole pieces. The codes' way to LDS is through
+// registers, three stages long, so that decoding them (22 vector instructions for 8) stands between
+// the products of the stage before theirs: their loads are issued with the direct loads of the
+// other operand, waited for with them one stage later, and decoded during the next one. No branch
+// divides a stage: past the last one its loads are repeated, rows past the chunk's end have a unit of
+// 0 and a piece of zeros. ODD: rows of codes that do not end with a unit of 16.
+template <bool ODD, int BK, int WR, int WC, int RB, int CB>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8_direct(Q8Args a) {
+  constexpr int NT = 64 * WR * WC, BM = 32 * WR * RB, BN = 32 * WC * CB;
+  using TA = Tile<false, BM, BK>;
+  using TN = Tile<false, BN, BK>;
+  constexpr int UA = BM * BK / 16 / NT, PB = TN::kPieces / NT;  // units, pieces of a thread
+  static_assert(BM * BK / 16 % NT == 0 && TN::kPieces % NT == 0, "every thread has as many");
+  __shared__ __align__(16) char a0[TA::kBytes], a1[TA::kBytes], b0[TN::kBytes], b1[TN::kBytes];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = w / WC, wc = w % WC;
+  const Place pl = place(a, BM, BN);
+  if (!pl.any) return;
+  const int m0 = pl.m0, n0 = pl.n0;
+
+  // Where a thread's first unit and piece are in memory, from the stage's first row on, and in LDS.
+  // Its others are whole rows further on, in the same columns.
+  constexpr int LA = NT / (BM / 16), LB = NT / (BN / 8);  // rows between them
+  static_assert(NT % (BM / 16) == 0 && NT % (BN / 8) == 0 && LA % 4 == 0 && LB % 4 == 0,
+                "the same columns and places in their lines");
+  const int line_a = threadIdx.x / (BM / 16), line_b = threadIdx.x / (BN / 8);
+  const int e_a = 16 * (threadIdx.x % (BM / 16)), have = a.K - m0;
+  const uint32_t qo = line_a * (uint32_t)a.ldq + (uint32_t)(std::min(e_a, have - 16) + 16);
+  const uint32_t so = line_a * (uint32_t)a.lds + (uint32_t)std::min(e_a, have - 1) / 32;
+  const uint32_t ao = line_a * (BM * 2) + ((e_a / 8) ^ TA::swz(line_a)) * 16;
+  const int down_a = std::min(16, std::max(0, e_a + 16 - have));
+  const int e_b = 8 * ((threadIdx.x % (BN / 8)) ^ TN::swz(line_b));
+  const uint32_t bo = 2 * (line_b * (uint32_t)a.ldb + (e_b < a.N - n0 ? e_b : 0));
+  // (from 16 codes before the tile on, where a unit at a row's end may begin)
+  const int8_t* q = a.q + pl.beg * a.ldq + m0 - 16;
+  const uint8_t* sc = a.s + pl.beg * a.lds + m0 / 32;
+  const bf16* b = static_cast<const bf16*>(a.b) + pl.beg * a.ldb + n0;
+  const int rows = (int)(pl.end - pl.beg), stages = (rows + BK - 1) / BK;
+  const uint32_t sign = pl.chunk & 1 ? 0x80000000u : 0;
+
+  f16 acc[RB][CB];
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
-    for (int j = 0; j < CB; ++j) {
-      const int r0 = m0 + (wr * RB + i) * 32 + 4 * (lane >> 5);
-      const int c = n0 + (wc * CB + j) * 32 + (lane & 31);
+    for (int j = 0; j < CB; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int r = r0 + (e & 3) + 8 * (e >> 2);
-        if (r < a.K && c < a.N) C[r * ldc + c] = __builtin_fmaf(acc[i][j][e], down, 0.f);
-      }
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  struct Raw {
+    u4 v[UA];
+    uint32_t scale[UA];
+  } r0, r1;
+  // the codes of a stage (in the last one of the rows that there are)
+  auto load_a = [&](Raw& r, int s) {
+    s = std::min(s, stages - 1);
+    const int8_t* qs = q + (int64_t)(s * BK) * a.ldq;
+    const uint8_t* ss = sc + (int64_t)(s * BK) * a.lds;
+    const int over = s * BK + BK - rows;  // rows past the chunk's end
+#pragma unroll
+    for (int p = 0; p < UA; ++p) {
+      const uint32_t on = p * LA - std::max(0, line_a + p * LA + over - (BK - 1));
+      r.v[p] = *reinterpret_cast<const u4b*>(qs + (uint32_t)(qo + on * (uint32_t)a.ldq));
+      r.scale[p] = ss[(uint32_t)(so + on * (uint32_t)a.lds)];
     }
+  };
+  auto decode = [&](char* to, const Raw& r, int s, int piece) {  // piece: of the thread's 2 UA
+    const int p = piece / 2, h = piece & 1;
+    u4 x = r.v[p];
+    if constexpr (ODD) x = bytes_down(x, down_a);
+    const float unit =
+        line_a + p * LA + s * BK < rows ? __uint_as_float(r.scale[p] << 23 ^ sign) : 0.f;
+    *reinterpret_cast<u4*>(to + (ao + p * LA * BM * 2 + 16 * h)) =
+        decode8(x[2 * h], x[2 * h + 1], unit);
+  };
+  auto load_b = [&](char* to, int s) {
+    s = std::min(s, stages - 1);
+    const char* bs = reinterpret_cast<const char*>(b + (int64_t)(s * BK) * a.ldb);
+    const int left = rows - s * BK;
+#pragma unroll
+    for (int p = 0; p < PB; ++p) {
+      const char* at = bs + 2 * p * LB * a.ldb + bo;
+      if (line_b + p * LB >= left) at = reinterpret_cast<const char*>(&g_zeros);
+      __builtin_amdgcn_global_load_lds((const GCN_GLOBAL void*)at,
+                                       (GCN_LDS void*)(to + (w * 64 + p * NT) * 16), 16, 0, 0);
+    }
+  };
+  constexpr int STEPS = BK / 16;
+  static_assert(STEPS % 2 == 0, "the fragments' buffers alternate over the stages");
+  bf8 fa[2][RB], fb[2][CB];
+  auto read = [&](int to, int step, const char* ca, const char* cb) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i) fa[to][i] = TA::read(ca, wr * RB + i, step, lane);
+#pragma unroll
+    for (int j = 0; j < CB; ++j) fb[to][j] = TN::read(cb, wc * CB + j, step, lane);
+  };
+  auto multiply = [&](int from) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+        acc[i][j] =
+            __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[from][i], fb[from][j], acc[i][j], 0, 0, 0);
+  };
+  // Between two products: one or two LDS reads, and some of the decoding.
+  constexpr int READS = 2 * (RB + CB), MULS = RB * CB;
+  auto order = [&](bool decodes) {
+#pragma unroll
+    for (int p = 0; p < MULS; ++p) {
+      __builtin_amdgcn_sched_group_barrier(0x100, (READS + MULS - 1) / MULS, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      if (decodes) __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
+    }
+  };
+  // Stage s, in (ca, cb): the codes of stage s + 1 go from r to na, then those of stage s + 3 to r.
+  auto stage = [&](int s, char* ca, char* cb, char* na, char* nb, Raw& r) {
+    constexpr int PER = (2 * UA + STEPS - 2) / (STEPS - 1);  // pieces to decode in a step
+#pragma unroll
+    for (int st = 0; st + 1 < STEPS; ++st) {
+      read((st + 1) & 1, st + 1, ca, cb);
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (st * PER + i < 2 * UA) decode(na, r, s + 1, st * PER + i);
+      multiply(st & 1);
+      order(true);
+    }
+    wait_loads();
+    load_b(cb, s + 2);
+    load_a(r, s + 3);
+    read(0, 0, na, nb);
+    multiply((STEPS - 1) & 1);
+    order(false);
+  };
+  if (stages > 0) {
+    load_b(b0, 0);
+    load_a(r0, 0);
+    load_a(r1, 1);
+    load_b(b1, 1);
+#pragma unroll
+    for (int i = 0; i < 2 * UA; ++i) decode(a0, r0, 0, i);
+    load_a(r0, 2);
+    wait_loads();
+    read(0, 0, a0, b0);
+    for (int s = 0; s < stages; s += 2) {
+      stage(s, a0, b0, a1, b1, r1);
+      if (s + 1 >= stages) break;
+      stage(s + 1, a1, b1, a0, b0, r0);
+    }
+    wait_loads();  // those past the last stage
+  }
+  write_sums<RB, CB>(a, pl, m0 + wr * RB * 32, n0 + wc * CB * 32, acc, pl.chunk & 1 ? -1.f : 1.f);
 }
 
-template <class TB, bool DIRECT, int BK, int WR, int WC, int RB, int CB>
-gcn_status launch(Q8Args a, hipStream_t s) {
+template <int WR, int WC, int RB, int CB, class Kernel>
+gcn_status launch(Kernel kernel, Q8Args a, hipStream_t s) {
   constexpr int BM = 32 * WR * RB, BN = 32 * WC * CB;
   a.col_tiles = (int)ceil_div((int64_t)a.N, (int64_t)BN);
   a.row_tiles = (int)ceil_div((int64_t)a.K, (int64_t)BM);
   const int64_t slots = group_slots(a.by, a.split);
-  const int64_t blocks = ceil_div(slots * a.col_tiles * a.row_tiles, (int64_t)8) * 8;
+  const int64_t per = (int64_t)a.col_tiles * a.row_tiles;
+  const int64_t blocks = 8 * (per >= 8 ? slots * ceil_div(per, (int64_t)8) : ceil_div(slots, (int64_t)8) * per);
   GCN_CHECK(launch_fits(blocks, 64 * WR * WC));
   a.slots = (uint32_t)slots;
-  hipLaunchKernelGGL((k_mul8<TB, DIRECT, BK, WR, WC, RB, CB>), dim3((unsigned)blocks),
-                     dim3(64 * WR * WC), 0, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WR * WC), 0, s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }
 
 // Rows of sixteen codes, and strides whose offsets over a stage's rows are 32 bits.
 bool mul8_takes(const Q8Args& a) {
-  return a.N >= 8 && a.K >= 16 && a.ldb < (int64_t(1) << 22);
+  return a.N >= 8 && a.K >= 16 && a.ldb < (int64_t(1) << 22) && a.ldq < (int64_t(1) << 24) &&
+         a.lds < (int64_t(1) << 24) && a.ldc < (int64_t(1) << 26);
 }
 
 gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
@@ -416,14 +645,18 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * K * N, "grouped GEMM partials"));
   if (scratch->asked()) return GCN_OK;
   ProfScope ps("grouped_q8", s);
+  const bool odd = K % 16 != 0;
   if (dtype == GCN_DT_F32)
-    GCN_CHECK((tn == 256 ? launch<float, false, 32, 2, 4, 2, 2>(a, s)
-                         : launch<float, false, 32, 2, 2, 2, 2>(a, s)));
+    GCN_CHECK((tn == 256 ? launch<2, 4, 2, 2>(k_mul8<float, 32, 2, 4, 2, 2>, a, s)
+                         : launch<2, 2, 2, 2>(k_mul8<float, 32, 2, 2, 2, 2>, a, s)));
   else if (wide)
-    GCN_CHECK((launch<bf16, true, 64, 4, 2, 2, 4>(a, s)));
+    GCN_CHECK((odd ? launch<4, 2, 2, 4>(k_mul8_direct<true, 64, 4, 2, 2, 4>, a, s)
+                   : launch<4, 2, 2, 4>(k_mul8_direct<false, 64, 4, 2, 2, 4>, a, s)));
+  else if (direct)
+    GCN_CHECK((odd ? launch<2, 2, 2, 2>(k_mul8_direct<true, 64, 2, 2, 2, 2>, a, s)
+                   : launch<2, 2, 2, 2>(k_mul8_direct<false, 64, 2, 2, 2, 2>, a, s)));
   else
-    GCN_CHECK((direct ? launch<bf16, true, 64, 2, 2, 2, 2>(a, s)
-                      : launch<bf16, false, 64, 2, 2, 2, 2>(a, s)));
+    GCN_CHECK((launch<2, 2, 2, 2>(k_mul8<bf16, 64, 2, 2, 2, 2>, a, s)));
   return parts > 0 ? sum_group_partials(a.by, a.split, K, N, a.part, a.c, a.ldc, a.stride_c, s)
                    : GCN_OK;
 }
