@@ -27,6 +27,7 @@ struct Q8Args {
   float* part;    // of the others here
   int col_tiles, row_tiles;
   uint32_t slots;
+  bool by_chunk;  // each chunk's tiles on one XCD
 };
 
 // The general kernel: 64 x 64 of C per workgroup, fp32 products, any size.
@@ -229,7 +230,7 @@ struct RowLoader<float, X, BK, NT> : PartLoader<X, BK, NT> {
 
 // A workgroup's part of C and its chunk of a group's rows.
 struct Place {
-  bool any;
+  bool any, whole;  // whether there is one; whether the chunk is the whole group
   int m0, n0, g;
   int64_t first, beg, end, chunk;
 };
@@ -255,9 +256,10 @@ __device__ inline GroupTile long_first(const Groups& by, const TileCount& c, int
   return r;
 }
 
-// The XCDs share every chunk's tiles (of fewer than eight, the chunks), and long groups come first:
-// groups of 100 to 5,000 rows, 2048 x 4096: 1128 us where each XCD had an eighth of all tiles in the
-// groups' order, the XCDs of the long ones the most work.
+// Of few chunks the XCDs share every one's tiles, of many (or with fewer than eight tiles) each has
+// whole chunks, which it reads once; long groups come first. 16 groups of 100 to 5,000 rows, 2048 x 4096:
+// 1128 us where each XCD had an eighth of all tiles in the groups' order, the XCDs of the long ones the
+// most work.
 __device__ inline Place place(const Q8Args& a, int BM, int BN) {
   Place r{};
   const int R = (int)a.split;
@@ -267,13 +269,14 @@ __device__ inline Place place(const Q8Args& a, int BM, int BN) {
   const uint32_t slots = counted ? count.total : a.slots;
   const uint32_t per = a.col_tiles * a.row_tiles, share = (per + 7) / 8, xcd = blockIdx.x & 7;
   uint32_t slot, t;
-  if (per >= 8) {
+  if (!a.by_chunk) {
     slot = (blockIdx.x >> 3) / share;
     const uint32_t x = (xcd + slot) & 7;  // (which XCD has one tile less than others changes)
     t = per * x / 8 + (blockIdx.x >> 3) % share;
     if (t >= per * (x + 1) / 8) return r;
   } else {
-    slot = blockIdx.x / (8 * per) * 8 + xcd;
+    const uint32_t turn = blockIdx.x / (8 * per);  // there and back, as the chunks get shorter
+    slot = turn * 8 + (turn & 1 ? 7 - xcd : xcd);
     t = (blockIdx.x >> 3) % per;
   }
   if (slot >= slots) return r;
@@ -282,6 +285,7 @@ __device__ inline Place place(const Q8Args& a, int BM, int BN) {
                                     : group_tile(a.by, slot, R);
   if (gt.beg >= gt.end && gt.beg != gt.first) return r;  // an empty group's first chunk: zeros
   r.any = true;
+  r.whole = gt.end - gt.first <= R;
   r.m0 = (int)t / a.col_tiles * BM;
   r.n0 = (int)t % a.col_tiles * BN;
   r.g = gt.g;
@@ -325,8 +329,9 @@ __device__ inline void write_sums(const Q8Args& a, const Place& pl, int m0, int 
         }
       }
   };
-  // past the caches where rows are whole lines, as in gemm_grouped.hip
-  if (((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(4 * ldc)) & 127) == 0)
+  // past the caches where rows are whole lines, as in gemm_grouped.hip, and no partial sums are added
+  // (32,768 rows of 8 groups in 16 chunks, 1024 x 1024: 139 us with those past the caches, 128)
+  if (pl.whole && ((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(4 * ldc)) & 127) == 0)
     write(std::true_type{});
   else
     write(std::false_type{});
@@ -613,7 +618,9 @@ gcn_status launch(Kernel kernel, Q8Args a, hipStream_t s) {
   a.row_tiles = (int)ceil_div((int64_t)a.K, (int64_t)BM);
   const int64_t slots = group_slots(a.by, a.split);
   const int64_t per = (int64_t)a.col_tiles * a.row_tiles;
-  const int64_t blocks = 8 * (per >= 8 ? slots * ceil_div(per, (int64_t)8) : ceil_div(slots, (int64_t)8) * per);
+  a.by_chunk = per < 8 || slots >= 32;
+  const int64_t blocks =
+      8 * (a.by_chunk ? ceil_div(slots, (int64_t)8) * per : slots * ceil_div(per, (int64_t)8));
   GCN_CHECK(launch_fits(blocks, 64 * WR * WC));
   a.slots = (uint32_t)slots;
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * WR * WC), 0, s, a);
@@ -695,7 +702,7 @@ extern "C" gcn_status gcn_gemm_grouped_q8(int64_t n_groups, const int64_t* offse
     return GCN_EINVAL;
   }
   Q8Args a{Groups{(int)n_groups, offsets, rows}, (int)N, (int)K, Q, ldq, S, lds, B, ldb, C, ldc,
-           stride_w, 0, nullptr, 0, 0, 0};
+           stride_w, 0, nullptr, 0, 0, 0, false};
   if (mul8_takes(a)) return mul8(a, dtype, &scratch, s);
   // four workgroups to a CU, chunks of 128 to 4096 rows (4096 where the groups' tiles are enough, longer
   // for more than a launch would take)
