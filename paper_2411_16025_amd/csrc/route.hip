@@ -1,10 +1,12 @@
 // A router's choice, the balance loss and their gradient (gcn_route_fwd, gcn_route_bwd).
 //
 // G neighbouring lanes hold a row, V logits each in registers, so it is read once: the largest
-// logit, the exponentials and their sum, then k times the largest of those left. Ties go to the
-// lowest index: the largest value first, then the least index that has it.
+// logit, the exponentials and their sum, then k times the largest of those left, whose index lane
+// i % G keeps. Ties go to the lowest index. What each lane adds up of p over its rows, and the
+// choices counted in LDS, are a workgroup's sums; one workgroup adds those.
 
 #include <cmath>
+#include <type_traits>
 
 #include "groups.h"
 #include "lanes.h"
@@ -13,7 +15,6 @@
 namespace gcn {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxExperts = 1024;
 
 struct RouteArgs {
@@ -49,6 +50,11 @@ __device__ inline float slot_max(float v) {
   return v;
 }
 template <int G, int OFF = 1>
+__device__ inline uint32_t slot_max(uint32_t v) {
+  if constexpr (OFF < G) return slot_max<G, 2 * OFF>(max(v, (uint32_t)slot_partner<OFF>((int)v)));
+  return v;
+}
+template <int G, int OFF = 1>
 __device__ inline int slot_min(int v) {
   if constexpr (OFF < G) return slot_min<G, 2 * OFF>(min(v, slot_partner<OFF>(v)));
   return v;
@@ -68,7 +74,7 @@ __device__ inline void load_logits(const T* row, int f, int E, float (&z)[V]) {
 
 // p of the row: e / sum. A row of -inf alone: zeros, and false.
 template <int G, int V>
-__device__ inline bool softmax(const float (&z)[V], float (&p)[V], float* top) {
+__device__ inline bool softmax(const float (&z)[V], float (&p)[V], float* top, float* inverse) {
   float m = -INFINITY, s = 0.f;
   bool nan = false;
 #pragma unroll
@@ -86,142 +92,201 @@ __device__ inline bool softmax(const float (&z)[V], float (&p)[V], float* top) {
   }
   s = slot_sum<G>(s);
   const float inv = s == 0.f ? 0.f : 1.f / s;
+  *inverse = inv;
 #pragma unroll
   for (int i = 0; i < V; ++i) p[i] *= inv;
   return any;
 }
 
-template <int V>
-__device__ inline float element(const float (&v)[V], int i) {
-  float r = v[0];
+// The logits that are left to choose from. fp32: the largest one, then the least index that has it.
+template <class T, int G, int V>
+struct Left {
+  float z[V];
+  __device__ inline Left(const float (&v)[V], int) {
 #pragma unroll
-  for (int e = 1; e < V; ++e) r = i == e ? v[e] : r;
-  return r;
-}
+    for (int e = 0; e < V; ++e) z[e] = v[e];
+  }
+  // the next one's value and index, and whether there is one
+  __device__ inline bool next(int f, float* top, int* at) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < V; ++e) m = fmaxf(m, z[e]);
+    m = slot_max<G>(m);
+    int i = G * V;
+#pragma unroll
+    for (int e = V - 1; e >= 0; --e) i = z[e] == m ? f + e : i;
+    i = slot_min<G>(i);
+#pragma unroll
+    for (int e = 0; e < V; ++e) z[e] = f + e == i ? -INFINITY : z[e];
+    *top = m;
+    *at = i;
+    return m > -INFINITY;
+  }
+};
 
-// counts, their number of rows and the loss from the workgroups' sums, by one workgroup.
-__device__ inline void finish(const RouteArgs& a, int threads) {
-  __shared__ double sums[2][16];
+// bf16: value and index in one whole number, the value's bits in an order that grows with it (-0 as
+// +0), below them the index from the end; 0 for a logit that cannot be chosen.
+template <int G, int V>
+struct Left<bf16, G, V> {
+  uint32_t key[V];
+  __device__ inline Left(const float (&v)[V], int f) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const uint32_t b = __float_as_uint(v[e] + 0.f);
+      const uint32_t up = (b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) & 0xFFFF0000u;
+      key[e] = v[e] > -INFINITY ? up | (0xFFFFu - (uint32_t)(f + e)) : 0;
+    }
+  }
+  __device__ inline bool next(int, float* top, int* at) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < V; ++e) m = max(m, key[e]);
+    m = slot_max<G>(m);
+#pragma unroll
+    for (int e = 0; e < V; ++e) key[e] = key[e] == m ? 0 : key[e];
+    const uint32_t b = m & 0xFFFF0000u;
+    *top = __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b & 0xFFFF0000u);
+    *at = (int)(0xFFFFu - (m & 0xFFFFu));
+    return m > 0;
+  }
+};
+
+// counts, their number of rows and the loss from the workgroups' sums, by one workgroup: each
+// thread adds the sums of every groups-th workgroup for a column, the first ones those of a column.
+template <int NT>
+__device__ inline void finish(const RouteArgs& a) {
+  __shared__ uint32_t part_c[NT];
+  __shared__ double part_p[NT], sums[2][NT / 64];
+  __shared__ uint32_t rows;
+  const int t = threadIdx.x;
+  int cols = 1;
+  while (cols < a.E + 1 && cols < NT) cols *= 2;
   double cp = 0.0, c = 0.0;
-  int64_t rows = 0;
-  for (int e = threadIdx.x; e <= a.E; e += threads) {
-    int64_t n = 0;
-    for (int b = 0; b < a.blocks; ++b) n += a.part_counts[(int64_t)b * (a.E + 1) + e];
-    a.counts[e] = n;
-    if (e == a.E || !a.loss) continue;
+  for (int e0 = 0; e0 <= a.E; e0 += cols) {
+    const int e = e0 + t % cols;
+    uint32_t n = 0;
     double p = 0.0;
-    for (int b = 0; b < a.blocks; ++b) p += (double)a.part_p[(int64_t)b * a.E + e];
-    cp += (double)n * p;
-    c += (double)n;
+    if (e <= a.E)
+#pragma unroll 8
+      for (int b = t / cols; b < a.blocks; b += NT / cols) {
+        n += a.part_counts[(int64_t)b * (a.E + 1) + e];
+        if (a.loss && e < a.E) p += (double)a.part_p[(int64_t)b * a.E + e];
+      }
+    part_c[t] = n;
+    part_p[t] = p;
+    __syncthreads();
+    if (t < cols && e <= a.E) {
+      for (int q = t + cols; q < NT; q += cols) {
+        n += part_c[q];
+        p += part_p[q];
+      }
+      a.counts[e] = n;
+      if (e == a.E) {
+        rows = n;
+      } else {
+        cp += (double)n * p;
+        c += (double)n;
+      }
+    }
+    __syncthreads();
   }
   if (!a.loss) return;
-  const int w = threadIdx.x >> 6;
   cp = slot_sum<64>(cp);
   c = slot_sum<64>(c);
-  if ((threadIdx.x & 63) == 0) {
-    sums[0][w] = cp;
-    sums[1][w] = c;
+  if ((t & 63) == 0) {
+    sums[0][t >> 6] = cp;
+    sums[1][t >> 6] = c;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int q = 1; q < threads / 64; ++q) {
+  if (t == 0) {
+    for (int q = 1; q < NT / 64; ++q) {
       cp += sums[0][q];
       c += sums[1][q];
     }
-    for (int b = 0; b < a.blocks; ++b) rows += a.part_counts[(int64_t)b * (a.E + 1) + a.E];
     // (without a choice p is 0 or, of rows that hold a NaN alone, NaN)
     const double all = c * (double)rows;
     *a.loss = (float)(a.coef * a.E * (all > 0.0 ? cp / all : cp));
   }
 }
 
-template <class T, int G, int V>
-__global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
-  constexpr int kSlots = kThreads / G;  // rows at a time
+template <class T, int NT, int G, int V>
+__global__ __launch_bounds__(NT) void k_route(RouteArgs a) {
+  constexpr int kSlots = NT / G;  // rows at a time
+  constexpr int kKept = 64 / G < 8 ? (64 / G > 0 ? 64 / G : 1) : 8;  // choices of a lane: k <= min(64, 8 G)
   __shared__ uint32_t cnt[kMaxExperts + 1];
-  __shared__ float sums[kWaves][G * V];
-  // a row's choices, until their sum is known (k <= min(E, 64) <= 8 G)
-  constexpr int kMost = V * G < 64 ? V * G : 64;
-  __shared__ int32_t found_at[kSlots][kMost];
-  __shared__ float found_p[kSlots][kMost];
+  __shared__ float sums[NT / 64][G * V];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, in = threadIdx.x % G, f = in * V;
-  for (int e = threadIdx.x; e <= a.E; e += kThreads) cnt[e] = 0;
+  for (int e = threadIdx.x; e <= a.E; e += NT) cnt[e] = 0;
   __syncthreads();
   float acc[V] = {};
   for (int64_t t0 = (int64_t)blockIdx.x * kSlots; t0 < a.n; t0 += (int64_t)gridDim.x * kSlots) {
     const int64_t t = t0 + threadIdx.x / G;
     const bool row = t < a.n && (!a.mask || a.mask[t] != 0);
-    float z[V], p[V], top;
+    float z[V], p[V], top, inv;
     load_logits(static_cast<const T*>(a.z) + (row ? t : 0) * a.ldz, f, row ? a.E : 0, z);
-    const bool any = softmax<G>(z, p, &top);
+    const bool any = softmax<G>(z, p, &top, &inv);
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] += p[i];
     if (any && in == 0) atomicAdd(&cnt[a.E], 1u);
-    const int slot = threadIdx.x / G;
-    float sum = 0.f;
-    for (int i = 0; i < a.k; ++i) {
-      if (i > 0) {
-        top = -INFINITY;
+    Left<T, G, V> left(z, f);
+    int at[kKept];
+    float weight[kKept], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) top = fmaxf(top, z[e]);
-        top = slot_max<G>(top);
-      }
-      int at = G * V;
-#pragma unroll
-      for (int e = V - 1; e >= 0; --e) at = z[e] == top ? f + e : at;
-      at = slot_min<G>(at);
-      const bool found = top > -INFINITY && at < a.E;
-      if (found ? at / V == in : in == 0) {
-        float pi = 0.f;
-        if (found) {
-          pi = element(p, at - f);
-#pragma unroll
-          for (int e = 0; e < V; ++e) z[e] = e == at - f ? -INFINITY : z[e];
-          atomicAdd(&cnt[at], 1u);
+    for (int c = 0; c < kKept; ++c) {
+      at[c] = -1;
+      float of = top;
+      for (int i = c * G; i < min(a.k, c * G + G); ++i) {
+        float v;
+        int j;
+        const bool found = left.next(f, &v, &j);
+        if (i % G == in) {
+          at[c] = found ? j : -1;
+          of = v;
         }
-        sum += pi;
-        found_at[slot][i] = found ? at : -1;
-        found_p[slot][i] = pi;
       }
+      weight[c] = at[c] >= 0 ? expf(of - top) * inv : 0.f;
+      sum += weight[c];
     }
-    sum = slot_sum<G>(sum);
-    // (a row's lanes are of one wavefront, whose LDS operations take effect in order; the fence
-    // keeps the compiler from moving the loads before the stores)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (t < a.n)
-      for (int i = in; i < a.k; i += G) {
-        const int at = found_at[slot][i];
-        const float w = found_p[slot][i];
-        a.experts[t * a.k + i] = at;
-        a.weights[t * a.k + i] = a.normalize && at >= 0 ? w / sum : w;
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (a.normalize) sum = slot_sum<G>(sum);
+#pragma unroll
+    for (int c = 0; c < kKept; ++c) {
+      const int i = c * G + in;
+      if (t >= a.n || i >= a.k) continue;
+      a.experts[t * a.k + i] = at[c];
+      a.weights[t * a.k + i] = a.normalize && at[c] >= 0 ? weight[c] / sum : weight[c];
+      if (at[c] >= 0) atomicAdd(&cnt[at[c]], 1u);
+    }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e <= a.E; e += kThreads)
+  for (int e = threadIdx.x; e <= a.E; e += NT)
     a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = cnt[e];
-  if (!a.loss) return;
-  // the slots of a wavefront, then the wavefronts, in their order
+  if (a.loss) {
+    // the slots of a wavefront, then the wavefronts, in their order
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
+    for (int i = 0; i < V; ++i) {
 #pragma unroll
-    for (int off = G; off < 64; off *= 2) acc[i] += __shfl_xor(acc[i], off, 64);
-    if (lane < G) sums[w][f + i] = acc[i];
+      for (int off = G; off < 64; off *= 2) acc[i] += __shfl_xor(acc[i], off, 64);
+      if (lane < G) sums[w][f + i] = acc[i];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.E; e += NT) {
+      float s = 0.f;
+#pragma unroll
+      for (int q = 0; q < NT / 64; ++q) s += sums[q][e];
+      a.part_p[(int64_t)blockIdx.x * a.E + e] = s;
+    }
   }
-  __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += kThreads) {
-    float s = 0.f;
-#pragma unroll
-    for (int q = 0; q < kWaves; ++q) s += sums[q][e];
-    a.part_p[(int64_t)blockIdx.x * a.E + e] = s;
+  if (gridDim.x == 1) {  // no other workgroup: its sums are all
+    __syncthreads();
+    finish<NT>(a);
   }
 }
 
-__global__ __launch_bounds__(1024) void k_finish(RouteArgs a) { finish(a, 1024); }
+__global__ __launch_bounds__(1024) void k_finish(RouteArgs a) { finish<1024>(a); }
 
-template <class T, int G, int V>
-__global__ __launch_bounds__(kThreads) void k_route_bwd(RouteArgs a) {
-  constexpr int kSlots = kThreads / G;
+template <class T, int NT, int G, int V>
+__global__ __launch_bounds__(NT) void k_route_bwd(RouteArgs a) {
+  constexpr int kSlots = NT / G;
   const int in = threadIdx.x % G, f = in * V;
   // a_e of the balance loss
   float bal[V] = {};
@@ -241,9 +306,9 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(RouteArgs a) {
     const int64_t t = t0 + threadIdx.x / G;
     const bool in_rows = t < a.n;
     const bool row = in_rows && a.chosen[t * a.k] >= 0;
-    float z[V], p[V], d[V] = {}, top;
+    float z[V], p[V], d[V] = {}, top, inv;
     load_logits(static_cast<const T*>(a.z) + (row ? t : 0) * a.ldz, f, row ? a.E : 0, z);
-    softmax<G>(z, p, &top);
+    softmax<G>(z, p, &top, &inv);
     float inner = 0.f;  // sum of g w over the chosen
     if (row && a.dw)
       for (int i = 0; i < a.k; ++i)
@@ -274,24 +339,28 @@ __global__ __launch_bounds__(kThreads) void k_route_bwd(RouteArgs a) {
   }
 }
 
-// Rows at a time of a workgroup.
 inline int route_lanes(int64_t E) {
   int g = 1;
   while (g < 64 && g * 8 < E) g *= 2;
   return g;
 }
-int route_blocks(int64_t n, int64_t E) {
-  return (int)std::min<int64_t>(512, ceil_div(n, (int64_t)(kThreads / route_lanes(E))));
+
+// Workgroups of 16 wavefronts for many rows: two to a CU keep it busy, and their sums are few.
+constexpr int kFew = 256, kMany = 1024;
+bool many_rows(int64_t n, int64_t E) { return n > 256 * (int64_t)(kFew / route_lanes(E)); }
+int route_blocks(int64_t n, int64_t E, int64_t most) {
+  return (int)std::min<int64_t>(
+      most, ceil_div(n, (int64_t)((many_rows(n, E) ? kMany : kFew) / route_lanes(E))));
 }
 
-template <class T, bool BWD>
+template <class T, int NT, bool BWD>
 gcn_status launch(const RouteArgs& a, int blocks, hipStream_t s) {
   auto go = [&](auto lanes, auto values) {
     constexpr int G = decltype(lanes)::value, V = decltype(values)::value;
     if constexpr (BWD)
-      hipLaunchKernelGGL((k_route_bwd<T, G, V>), dim3(blocks), dim3(kThreads), 0, s, a);
+      hipLaunchKernelGGL((k_route_bwd<T, NT, G, V>), dim3(blocks), dim3(NT), 0, s, a);
     else
-      hipLaunchKernelGGL((k_route<T, G, V>), dim3(blocks), dim3(kThreads), 0, s, a);
+      hipLaunchKernelGGL((k_route<T, NT, G, V>), dim3(blocks), dim3(NT), 0, s, a);
   };
   std::integral_constant<int, 8> v8;
   switch (route_lanes(a.E)) {
@@ -309,6 +378,16 @@ gcn_status launch(const RouteArgs& a, int blocks, hipStream_t s) {
   }
   GCN_HIP(hipGetLastError());
   return GCN_OK;
+}
+
+template <bool BWD>
+gcn_status launch(const RouteArgs& a, int dtype, int blocks, hipStream_t s) {
+  if constexpr (!BWD)
+    if (many_rows(a.n, a.E))
+      return dtype == GCN_DT_F32 ? launch<float, kMany, BWD>(a, blocks, s)
+                                 : launch<bf16, kMany, BWD>(a, blocks, s);
+  return dtype == GCN_DT_F32 ? launch<float, kFew, BWD>(a, blocks, s)
+                             : launch<bf16, kFew, BWD>(a, blocks, s);
 }
 
 gcn_status check_route(int64_t n, int64_t E, int dtype, int64_t k, uint32_t flags, double coef) {
@@ -357,16 +436,15 @@ extern "C" gcn_status gcn_route_fwd(int64_t n, int64_t E, const void* logits, in
   a.coef = coef;
   a.counts = counts;
   a.loss = loss;
-  a.blocks = route_blocks(n, E);
+  a.blocks = route_blocks(n, E, 512);
   if (a.blocks > 0) {
     GCN_CHECK(scratch.alloc(&a.part_counts, a.blocks * (E + 1), "counts of workgroups"));
     if (loss) GCN_CHECK(scratch.alloc(&a.part_p, a.blocks * E, "sums of workgroups"));
   }
   if (scratch.asked()) return GCN_OK;
   ProfScope ps("route_fwd", s);
-  if (a.blocks > 0)
-    GCN_CHECK((dtype == GCN_DT_F32 ? launch<float, false>(a, a.blocks, s)
-                                   : launch<bf16, false>(a, a.blocks, s)));
+  if (a.blocks > 0) GCN_CHECK(launch<false>(a, dtype, a.blocks, s));
+  if (a.blocks == 1) return GCN_OK;
   hipLaunchKernelGGL(k_finish, dim3(1), dim3(1024), 0, s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
@@ -403,6 +481,6 @@ extern "C" gcn_status gcn_route_bwd(int64_t n, int64_t E, const void* logits, in
   a.ldd = ldd;
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps("route_bwd", s);
-  const int blocks = (int)std::min<int64_t>(2048, ceil_div(n, (int64_t)(kThreads / route_lanes(E))));
-  return dtype == GCN_DT_F32 ? launch<float, true>(a, blocks, s) : launch<bf16, true>(a, blocks, s);
+  const int blocks = (int)std::min<int64_t>(2048, ceil_div(n, (int64_t)(kFew / route_lanes(E))));
+  return launch<true>(a, dtype, blocks, s);
 }
