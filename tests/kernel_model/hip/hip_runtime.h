@@ -140,6 +140,7 @@ inline uint32_t __builtin_amdgcn_perm(uint32_t hi, uint32_t lo, uint32_t sel) {
   for (int i = 0; i < 4; ++i) r |= (uint32_t)(v >> 8 * (sel >> 8 * i & 7) & 255) << 8 * i;
   return r;
 }
+inline float __builtin_amdgcn_exp2f(float v) { return std::exp2(v); }
 inline double __builtin_amdgcn_rsq(double v) { return 1.0 / std::sqrt(v); }
 inline void __builtin_amdgcn_s_waitcnt(int) {}
 inline void __builtin_amdgcn_sched_group_barrier(int, int, int) {}
