@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kThreads) void k_combine(CombineArgs a) {
   for (int i = 0; i < a.k; i += kAhead) {
     uint32_t at[kAhead];
     float by[kAhead];
-    Raw8<T> raw[kAhead];
+    Raw<T, 8> raw[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       at[j] = i + j < a.k ? (uint32_t)slot[i + j] : 0xFFFFFFFFu;
@@ -48,18 +48,18 @@ __global__ __launch_bounds__(kThreads) void k_combine(CombineArgs a) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const bool in = at[j] < a.rows;
-      raw[j] = load8(static_cast<const T*>(a.z) + (in ? at[j] : 0) * a.ldz, f, in ? (int)a.F : 0);
+      raw[j] = load_raw<T, 8>(static_cast<const T*>(a.z) + (in ? at[j] : 0) * a.ldz, f, in ? (int)a.F : 0);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (at[j] >= a.rows) continue;
       float x[8];
-      unpack8(raw[j], x);
+      unpack_raw(raw[j], x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(by[j], x[e], v[e]);
     }
   }
-  store8(static_cast<T*>(a.y) + (int64_t)t * a.ldy, f, (int)a.F, v);
+  store_raw(static_cast<T*>(a.y) + (int64_t)t * a.ldy, f, (int)a.F, v);
 }
 
 // G lanes have a token.
@@ -77,16 +77,16 @@ __global__ __launch_bounds__(kThreads) void k_combine_bwd(CombineArgs a) {
     if (real)
       for (int64_t f = 8 * in; f < a.F; f += 8 * G) {
         float g[8], x[8];
-        unpack8(load8(dy, (int)f, (int)a.F), g);
+        unpack_raw(load_raw<T, 8>(dy, (int)f, (int)a.F), g);
         if (a.dw) {
-          unpack8(load8(static_cast<const T*>(a.z) + at * a.ldz, (int)f, (int)a.F), x);
+          unpack_raw(load_raw<T, 8>(static_cast<const T*>(a.z) + at * a.ldz, (int)f, (int)a.F), x);
 #pragma unroll
           for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(g[e], x[e], dot);
         }
         if (a.dz) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) g[e] *= w;
-          store8(static_cast<T*>(a.dz) + at * a.lddz, (int)f, (int)a.F, g);
+          store_raw(static_cast<T*>(a.dz) + at * a.lddz, (int)f, (int)a.F, g);
         }
       }
     if (a.dw) {

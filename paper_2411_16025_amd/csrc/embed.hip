@@ -23,12 +23,13 @@ struct TakeArgs {
   int64_t ldy;
 };
 
-// A thread has PER pieces, whose ids, then whose rows, are on their way together.
+// A thread has PER pieces of 16 bytes of Y, whose ids, then whose rows, are on their way together.
 template <class T, class TY, int PER>
 __global__ __launch_bounds__(kThreads) void k_take(TakeArgs a) {
+  constexpr int N = kPiece<TY>;
   uint32_t row[PER], piece[PER], from[PER];
   bool real[PER];
-  Raw8<T> raw[PER];
+  Raw<T, N> raw[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     if (!locate(a.tiles, kThreads * PER, threadIdx.x + k * kThreads, &row[k], &piece[k])) {
@@ -42,24 +43,24 @@ __global__ __launch_bounds__(kThreads) void k_take(TakeArgs a) {
     real[k] = (int32_t)from[k] >= 0;
     if (a.per != 1) from[k] /= a.per;
     real[k] = real[k] && from[k] < a.V && piece[k] < a.tiles.pieces;
-    raw[k] = load8(static_cast<const T*>(a.t) + (real[k] ? from[k] : 0) * a.ldt,
-                   (int)(8 * piece[k]), real[k] ? (int)a.F : 0);
+    raw[k] = load_raw<T, N>(static_cast<const T*>(a.t) + (real[k] ? from[k] : 0) * a.ldt,
+                   (int)(N * piece[k]), real[k] ? (int)a.F : 0);
   }
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     if (piece[k] >= a.tiles.pieces) continue;
-    float v[8];
-    unpack8(raw[k], v);
+    float v[N];
+    unpack_raw(raw[k], v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = real[k] ? a.scale * v[e] : 0.f;
-    store8(static_cast<TY*>(a.y) + row[k] * a.ldy, (int)(8 * piece[k]), (int)a.F, v);
+    for (int e = 0; e < N; ++e) v[e] = real[k] ? a.scale * v[e] : 0.f;
+    store_raw(static_cast<TY*>(a.y) + row[k] * a.ldy, (int)(N * piece[k]), (int)a.F, v);
   }
 }
 
 template <class T, class TY>
 gcn_status take(TakeArgs a, int64_t n, int64_t F, hipStream_t s) {
   ProfScope ps("embed_fwd", s);
-  const int64_t pieces = ceil_div(F, (int64_t)8);
+  const int64_t pieces = ceil_div(F, (int64_t)kPiece<TY>);
   const bool few = n * pieces < 512 * 4 * kThreads;
   a.tiles = row_tiles(n, pieces, kThreads * (few ? 1 : 4));
   GCN_CHECK(launch_fits(a.tiles.blocks(), kThreads));
@@ -97,53 +98,68 @@ struct SumArgs {
 };
 
 // v += the rows at places [beg, end), in their order.
-template <class T>
-__device__ inline void add_rows(const SumArgs& a, int64_t beg, int64_t end, int f, float (&v)[8]) {
+template <class T, int N>
+__device__ inline void add_rows(const SumArgs& a, int64_t beg, int64_t end, int f, float (&v)[N]) {
   constexpr int kAhead = 4;
   for (int64_t j = beg; j < end; j += kAhead) {
     int32_t at[kAhead];
-    Raw8<T> raw[kAhead];
+    Raw<T, N> raw[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) at[i] = j + i < end ? a.order[j + i] : -1;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const bool in = at[i] >= 0 && at[i] < a.n;
-      raw[i] = load8(static_cast<const T*>(a.dy) + (in ? at[i] : 0) * a.lddy, f, in ? (int)a.F : 0);
+      raw[i] = load_raw<T, N>(static_cast<const T*>(a.dy) + (in ? at[i] : 0) * a.lddy, f, in ? (int)a.F : 0);
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      float x[8];
-      unpack8(raw[i], x);
+      float x[N];
+      unpack_raw(raw[i], x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += x[e];
+      for (int e = 0; e < N; ++e) v[e] += x[e];
     }
   }
 }
 
 // Scaled, added to the row's piece where wanted, and stored.
-template <class TT>
-__device__ inline void write_piece(const SumArgs& a, int64_t row, int f, float (&v)[8]) {
+template <class TT, int N>
+__device__ inline void write_piece(const SumArgs& a, int64_t row, int f, float (&v)[N]) {
   TT* to = static_cast<TT*>(a.dt) + row * a.lddt;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+  for (int e = 0; e < N; ++e) v[e] *= a.scale;
   if (a.add) {
-    float old[8];
-    unpack8(load8(to, f, (int)a.F), old);
+    float old[N];
+    unpack_raw(load_raw<TT, N>(to, f, (int)a.F), old);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += old[e];
+    for (int e = 0; e < N; ++e) v[e] += old[e];
   }
-  store8(to, f, (int)a.F, v);
+  store_raw(to, f, (int)a.F, v);
 }
 
-template <class T, class TT>
+// PER pieces of 16 bytes of dT to a thread: most rows of a large table have no place, and what
+// bounds the pass then is writing their zeros.
+template <class T, class TT, int PER>
 __global__ __launch_bounds__(kThreads) void k_sum_rows(SumArgs a) {
-  uint32_t row, piece;
-  if (!locate(a.tiles, kThreads, threadIdx.x, &row, &piece)) return;
-  const int64_t beg = group_offset(a.by, (int)row), end = group_offset(a.by, (int)row + 1);
-  if (end - beg > a.chunk || (a.add && end <= beg)) return;
-  float v[8] = {};
-  add_rows<T>(a, beg, end, (int)(8 * piece), v);
-  write_piece<TT>(a, row, (int)(8 * piece), v);
+  constexpr int N = kPiece<TT>;
+  uint32_t row[PER], piece[PER];
+  int64_t beg[PER], end[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const bool in =
+        locate(a.tiles, kThreads * PER, threadIdx.x + k * kThreads, &row[k], &piece[k]);
+    if (!in) row[k] = 0;
+    beg[k] = group_offset(a.by, (int)row[k]);
+    end[k] = group_offset(a.by, (int)row[k] + 1);
+    if (!in) end[k] = beg[k] + a.chunk + 1;  // not here
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (end[k] - beg[k] > a.chunk || (a.add && end[k] <= beg[k])) continue;
+    const int f = (int)(N * piece[k]);
+    float v[N] = {};
+    add_rows<T>(a, beg[k], end[k], f, v);
+    write_piece<TT>(a, row[k], f, v);
+  }
 }
 
 // The long row that partial sum p belongs to: whether there is one.
@@ -163,10 +179,10 @@ __global__ __launch_bounds__(kThreads) void k_sum_chunks(SumArgs a, int64_t p) {
   if (!long_row(a, p, &t, &p0, &more)) return;
   const int64_t beg = t.first + (p - p0 + 1) * a.chunk, end = min(beg + a.chunk, t.end);
   const uint32_t piece = blockIdx.x * kThreads + threadIdx.x;
-  if (piece >= a.tiles.pieces) return;
+  if (8 * piece >= a.F) return;
   float v[8] = {};
   add_rows<T>(a, beg, end, (int)(8 * piece), v);
-  store8(a.part + p * a.ldp, (int)(8 * piece), (int)a.F, v);
+  store_raw(a.part + p * a.ldp, (int)(8 * piece), (int)a.F, v);
 }
 
 // The pieces of a long row, shared by the workgroups of its partial sums.
@@ -177,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void k_join_chunks(SumArgs a, int64_t p) 
   int64_t p0, more;
   if (!long_row(a, p, &t, &p0, &more)) return;
   for (int64_t piece = ((p - p0) * gridDim.x + blockIdx.x) * kThreads + threadIdx.x;
-       piece < a.tiles.pieces; piece += more * gridDim.x * kThreads) {
+       8 * piece < a.F; piece += more * gridDim.x * kThreads) {
     const int f = (int)(8 * piece);
     float v[8] = {};
     add_rows<T>(a, t.first, t.first + a.chunk, f, v);
@@ -186,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void k_join_chunks(SumArgs a, int64_t p) 
     for (int e = 0; e < 8; ++e) s[e] = (double)v[e];
     for (int64_t q = p0; q < p0 + more; ++q) {
       float x[8];
-      unpack8(load8(a.part + q * a.ldp, f, (int)a.F), x);
+      unpack_raw(load_raw<float, 8>(a.part + q * a.ldp, f, (int)a.F), x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[e] += (double)x[e];
     }
@@ -198,18 +214,23 @@ __global__ __launch_bounds__(kThreads) void k_join_chunks(SumArgs a, int64_t p) 
 
 template <class T, class TT>
 gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
-  const int64_t pieces = ceil_div((int64_t)a.F, (int64_t)8);
-  a.tiles = row_tiles(a.by.n, pieces, kThreads);
+  const int64_t pieces = ceil_div((int64_t)a.F, (int64_t)kPiece<TT>);
+  const bool few = a.by.n * pieces < 2048 * kThreads;
+  a.tiles = row_tiles(a.by.n, pieces, kThreads * (few ? 1 : 4));
   a.chunk = 32;
   GCN_CHECK(launch_fits(a.tiles.blocks(), kThreads));
   const int64_t parts = a.by.rows / a.chunk;
-  a.ldp = 8 * pieces;
+  a.ldp = ceil_div((int64_t)a.F, (int64_t)8) * 8;
   if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * a.ldp, "sums of repeated ids"));
   if (scratch->asked()) return GCN_OK;
   ProfScope ps("embed_bwd", s);
-  hipLaunchKernelGGL((k_sum_rows<T, TT>), dim3((unsigned)a.tiles.blocks()), dim3(kThreads), 0, s, a);
+  const dim3 rows((unsigned)a.tiles.blocks());
+  if (few)
+    hipLaunchKernelGGL((k_sum_rows<T, TT, 1>), rows, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_sum_rows<T, TT, 4>), rows, dim3(kThreads), 0, s, a);
   GCN_HIP(hipGetLastError());
-  const unsigned wide = (unsigned)ceil_div(pieces, (int64_t)kThreads);
+  const unsigned wide = (unsigned)ceil_div(a.ldp, (int64_t)8 * kThreads);
   for (int64_t p = 0; p < parts; p += 65535) {  // (a grid's second axis)
     const dim3 grid(wide, (unsigned)std::min<int64_t>(parts - p, 65535));
     hipLaunchKernelGGL(k_sum_chunks<T>, grid, dim3(kThreads), 0, s, a, p);

@@ -65,65 +65,51 @@ __global__ __launch_bounds__(kThreads) void k_count(SortArgs a) {
     a.hist[(uint64_t)blockIdx.x * a.digits + d] = cnt[d];
 }
 
-// 64 digits to a workgroup; its sixteen wavefronts share the tiles.
+// 64 digits to a workgroup; its sixteen wavefronts share the tiles, eight at a time.
 __global__ __launch_bounds__(1024) void k_sum_tiles(SortArgs a) {
   __shared__ uint32_t sums[16][64];
   const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
   const uint32_t per = (a.tiles + 15) / 16, beg = min(w * per, a.tiles), end = min(beg + per, a.tiles);
   const bool in = d < a.digits;
-  uint32_t s = 0;
-  for (uint32_t t = beg; t < end; ++t) s += in ? a.hist[(uint64_t)t * a.digits + d] : 0;
+  uint32_t* h = a.hist + (in ? d : 0);
+  uint32_t v[8], s = 0;
+  auto load = [&](uint32_t t) {
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      v[i] = in && t + i < end ? h[(uint64_t)(t + i) * a.digits] : 0;
+  };
+  for (uint32_t t = beg; t < end; t += 8) {
+    load(t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += v[i];
+  }
   sums[w][lane] = s;
   __syncthreads();
   uint32_t run = 0, all = 0;
+#pragma unroll
   for (uint32_t q = 0; q < 16; ++q) {
     run += q < w ? sums[q][lane] : 0;
     all += sums[q][lane];
   }
   if (!in) return;
   if (w == 0) a.total[d] = all;
-  for (uint32_t t = beg; t < end; ++t) {
-    uint32_t* h = &a.hist[(uint64_t)t * a.digits + d];
-    const uint32_t v = *h;
-    *h = run;
-    run += v;
+  for (uint32_t t = beg; t < end; t += 8) {
+    if (per > 8) load(t);
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (t + i < end) {
+        h[(uint64_t)(t + i) * a.digits] = run;
+        run += v[i];
+      }
   }
 }
 
-template <bool FIRST, bool LAST, int ITEMS>
-__global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
-  __shared__ uint32_t first[kMaxDigits];         // the place of the tile's first id of a digit
-  __shared__ uint32_t cnt[kWaves][kMaxDigits];   // ids of a wavefront, then of those before it
-  __shared__ uint32_t wave_sum[kWaves];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  for (uint32_t d = t; d < kWaves * a.digits; d += kThreads) cnt[d / a.digits][d % a.digits] = 0;
-  // each thread sums a run of digits
-  const uint32_t per = (a.digits + kThreads - 1) / kThreads;
-  uint32_t mine = 0;
-  for (uint32_t i = 0; i < per; ++i) {
-    const uint32_t d = t * per + i;
-    if (d < a.digits) mine += a.total[d];
-  }
-  uint32_t upto = mine;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t v = __shfl_up(upto, off, 64);
-    if (lane >= off) upto += v;
-  }
-  if (lane == 63) wave_sum[w] = upto;
-  __syncthreads();
-  uint32_t run = upto - mine;
-  for (int q = 0; q < w; ++q) run += wave_sum[q];
-  for (uint32_t i = 0; i < per; ++i) {
-    const uint32_t d = t * per + i;
-    if (d >= a.digits) break;
-    if (FIRST && LAST && blockIdx.x == 0) a.offsets[d] = run;
-    first[d] = run + a.hist[(uint64_t)blockIdx.x * a.digits + d];
-    run += a.total[d];
-  }
-  uint64_t key[ITEMS];
-  uint32_t rank[ITEMS];
-  const uint32_t base = blockIdx.x * (kThreads * ITEMS) + w * (64 * ITEMS) + lane;
+// A wavefront's ITEMS times 64 keys from `base` (the lane's first) on, and each one's number among
+// those of its digit, which cnt [digits], all 0 before, then holds.
+template <bool FIRST, int ITEMS>
+__device__ inline void rank_keys(const SortArgs& a, uint32_t base, uint32_t* cnt,
+                                 uint64_t (&key)[ITEMS], uint32_t (&rank)[ITEMS]) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int j = 0; j < ITEMS; ++j)
     key[j] = base + j * 64 < a.n ? load_key<FIRST>(a, base + j * 64) : ~0ull;
@@ -139,14 +125,74 @@ __global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
       peers &= b ? m : ~m;
     }
     const uint32_t before = (uint32_t)__popcll(peers & below);
-    const uint32_t have = valid ? cnt[w][d] : 0;
+    const uint32_t have = valid ? cnt[d] : 0;
     // (LDS operations of one wavefront take effect in order; the fence keeps
     // the compiler from moving the store before the other lanes' loads)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (valid && before == 0) cnt[w][d] = have + (uint32_t)__popcll(peers);
+    if (valid && before == 0) cnt[d] = have + (uint32_t)__popcll(peers);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     rank[j] = have + before;
   }
+}
+
+// The sum of v over the threads before this one; sums [threads / 64] in LDS.
+__device__ inline uint32_t before_thread(uint32_t v, uint32_t* sums) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t upto = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(upto, off, 64);
+    if (lane >= off) upto += o;
+  }
+  if (lane == 63) sums[w] = upto;
+  __syncthreads();
+  uint32_t run = upto - v;
+  for (int q = 0; q < w; ++q) run += sums[q];
+  return run;
+}
+
+__device__ inline void put(const SortArgs& a, uint64_t key, uint32_t place) {
+  const uint32_t at = (uint32_t)key;
+  const bool in = (uint32_t)(key >> 32) < a.groups;
+  if (a.order) a.order[place] = in ? (int32_t)at : -1;
+  if (a.slot) a.slot[at] = in ? (int32_t)place : -1;
+}
+
+template <bool FIRST, bool LAST, int ITEMS>
+__global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
+  __shared__ uint32_t first[kMaxDigits];        // the place of the tile's first id of a digit
+  __shared__ uint32_t cnt[kWaves][kMaxDigits];  // ids of a wavefront, then of those before it
+  __shared__ uint32_t sums[kWaves];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+#pragma unroll
+  for (int q = 0; q < kWaves; ++q)
+    for (uint32_t d = t; d < a.digits; d += kThreads) cnt[q][d] = 0;
+  // each thread has a run of digits
+  constexpr int kRun = kMaxDigits / kThreads;
+  const uint32_t per = (a.digits + kThreads - 1) / kThreads;
+  uint32_t total[kRun], here[kRun], mine = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kRun; ++i) {
+    const uint32_t d = t * per + i;
+    const bool in = i < per && d < a.digits;
+    total[i] = in ? a.total[d] : 0;
+    here[i] = in ? a.hist[(uint64_t)blockIdx.x * a.digits + d] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) mine += total[i];
+  uint32_t run = before_thread(mine, sums);
+#pragma unroll
+  for (uint32_t i = 0; i < kRun; ++i) {
+    const uint32_t d = t * per + i;
+    if (i >= per || d >= a.digits) break;
+    if (FIRST && LAST && blockIdx.x == 0) a.offsets[d] = run;
+    first[d] = run + here[i];
+    run += total[i];
+  }
+  uint64_t key[ITEMS];
+  uint32_t rank[ITEMS];
+  const uint32_t base = blockIdx.x * (kThreads * ITEMS) + w * (64 * ITEMS) + lane;
+  rank_keys<FIRST>(a, base, cnt[w], key, rank);
   __syncthreads();
   for (uint32_t d = t; d < a.digits; d += kThreads) {
     uint32_t s = first[d];
@@ -163,18 +209,66 @@ __global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
     if (base + j * 64 >= a.n) continue;
     const uint32_t place = cnt[w][digit(a, key[j])] + rank[j];
     if constexpr (LAST) {
-      const uint32_t id = (uint32_t)(key[j] >> 32), at = (uint32_t)key[j];
-      const bool in = id < a.groups;
-      if (a.order) a.order[place] = in ? (int32_t)at : -1;
-      if (a.slot) a.slot[at] = in ? (int32_t)place : -1;
-      if constexpr (!FIRST) a.sorted[place] = id;
+      put(a, key[j], place);
+      if constexpr (!FIRST) a.sorted[place] = (uint32_t)(key[j] >> 32);
     } else {
       a.out[place] = key[j];
     }
   }
 }
 
-// The first place of a key that is at least v, in [lo, hi].
+// Few ids and groups: all of it by one workgroup, in one launch (48 ids: .. us).
+constexpr int kOneThreads = 1024, kOneItems = 4, kOneMost = kOneThreads * kOneItems;
+constexpr uint32_t kOneDigits = 1024;
+
+__global__ __launch_bounds__(kOneThreads) void k_sort_one(SortArgs a) {
+  constexpr int kOneWaves = kOneThreads / 64;
+  __shared__ uint32_t cnt[kOneWaves][kOneDigits];
+  __shared__ uint32_t sums[kOneWaves];
+  const uint32_t t = threadIdx.x, w = t >> 6;
+  if (t < a.digits)
+#pragma unroll
+    for (int q = 0; q < kOneWaves; ++q) cnt[q][t] = 0;
+  __syncthreads();
+  uint64_t key[kOneItems];
+  uint32_t rank[kOneItems];
+  const uint32_t base = w * (64 * kOneItems) + (t & 63);
+  rank_keys<true>(a, base, cnt[w], key, rank);
+  __syncthreads();
+  uint32_t mine = 0;
+  if (t < a.digits)
+#pragma unroll
+    for (int q = 0; q < kOneWaves; ++q) mine += cnt[q][t];
+  uint32_t run = before_thread(mine, sums);
+  if (t < a.digits) {
+    a.offsets[t] = run;
+#pragma unroll
+    for (int q = 0; q < kOneWaves; ++q) {
+      const uint32_t c = cnt[q][t];
+      cnt[q][t] = run;
+      run += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kOneItems; ++j)
+    if (base + j * 64 < a.n) put(a, key[j], cnt[w][digit(a, key[j])] + rank[j]);
+}
+
+// The first place of a key that is at least v: the wavefront's lanes look at 64 places at a time.
+__device__ inline uint32_t wave_lower_bound(const uint32_t* keys, uint32_t n, uint32_t v) {
+  uint32_t lo = 0, len = n;  // the keys before lo are below v, the one at lo + len is not
+  while (len > 0) {
+    const uint32_t step = (len + 63) / 64, at = lo + (threadIdx.x & 63) * step + step - 1;
+    const bool below = at < lo + len && keys[at] < v;
+    const uint32_t steps = (uint32_t)__popcll(__ballot(below));
+    const uint32_t end = lo + len;
+    lo += steps * step;
+    len = lo < end ? min(step - 1, end - lo) : 0;
+  }
+  return lo;
+}
+
 __device__ inline uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t v) {
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo) / 2;
@@ -186,13 +280,25 @@ __device__ inline uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32
   return lo;
 }
 
-// Offsets from the sorted keys: a workgroup's groups are found in the range between its own ends.
+// Offsets from the sorted keys, 1024 groups to a workgroup: the keys between its ends are found by
+// two wavefronts, and brought to LDS where they fit there.
+constexpr uint32_t kPerBlock = 1024, kStaged = 2048;
 __global__ __launch_bounds__(kThreads) void k_offsets(const uint32_t* sorted, uint32_t n,
                                                       uint32_t groups, int64_t* offsets) {
-  const uint32_t v0 = blockIdx.x * kThreads, v = v0 + threadIdx.x;
-  const uint32_t lo = lower_bound(sorted, 0, n, v0);
-  const uint32_t hi = lower_bound(sorted, lo, n, min(v0 + kThreads, groups));
-  if (v <= groups) offsets[v] = lower_bound(sorted, lo, hi, v);
+  __shared__ uint32_t ends[2], keys[kStaged];
+  const uint32_t v0 = blockIdx.x * kPerBlock, w = threadIdx.x >> 6;
+  if (w < 2) {
+    const uint32_t p = wave_lower_bound(sorted, n, w == 0 ? v0 : min(v0 + kPerBlock, groups));
+    if ((threadIdx.x & 63) == 0) ends[w] = p;
+  }
+  __syncthreads();
+  const uint32_t lo = ends[0], len = ends[1] - lo;
+  if (len <= kStaged)
+    for (uint32_t i = threadIdx.x; i < len; i += kThreads) keys[i] = sorted[lo + i];
+  __syncthreads();
+  for (uint32_t v = v0 + threadIdx.x; v < v0 + kPerBlock && v <= groups; v += kThreads)
+    offsets[v] = len <= kStaged ? lo + lower_bound(keys, 0, len, v)
+                                : lower_bound(sorted, lo, lo + len, v);
 }
 
 __global__ __launch_bounds__(kThreads) void k_zero_offsets(int64_t* offsets, int64_t count) {
@@ -224,7 +330,7 @@ gcn_status sort_ids(SortArgs a, int bits, int passes, uint64_t* pairs[2], hipStr
                : p + 1 == passes ? pass<false, true, ITEMS>(a, s)
                                  : pass<false, false, ITEMS>(a, s)));
   }
-  hipLaunchKernelGGL(k_offsets, dim3((unsigned)ceil_div((int64_t)a.groups + 1, (int64_t)kThreads)),
+  hipLaunchKernelGGL(k_offsets, dim3((unsigned)ceil_div((int64_t)a.groups + 1, (int64_t)kPerBlock)),
                      dim3(kThreads), 0, s, a.sorted, a.n, a.groups, a.offsets);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
@@ -272,6 +378,13 @@ extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_gro
   a.offsets = offsets;
   a.bits = bits;
   a.digits = (uint32_t)n_groups + 1;
+  if (n <= kOneMost && a.digits <= kOneDigits) {
+    if (scratch.asked()) return GCN_OK;
+    ProfScope ps("group_ids", s);
+    hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(kOneThreads), 0, s, a);
+    GCN_HIP(hipGetLastError());
+    return GCN_OK;
+  }
   a.tiles = (uint32_t)ceil_div(n, (int64_t)kThreads * (small ? 4 : 16));
   const int64_t digits = passes == 1 ? n_groups + 1 : int64_t(1) << ((bits + passes - 1) / passes);
   GCN_CHECK(scratch.alloc(&a.hist, (int64_t)a.tiles * digits, "digit counts"));

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kThreads) void k_pack(PackArgs a) {
   const bool in = locate(a.tiles, kThreads, threadIdx.x, &row, &piece);
   const int f = (int)(8 * piece);
   float v[8];
-  unpack8(load8(static_cast<const T*>(a.x) + (in ? (int64_t)row * a.ldx : 0), f, in ? (int)a.F : 0), v);
+  unpack_raw(load_raw<T, 8>(static_cast<const T*>(a.x) + (in ? (int64_t)row * a.ldx : 0), f, in ? (int)a.F : 0), v);
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void k_unpack(PackArgs a) {
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = unit * (float)((int32_t)(c[e / 4] << (24 - 8 * (e & 3))) >> 24);
-  store8(static_cast<T*>(a.y) + (int64_t)row * a.ldy, f, (int)a.F, v);
+  store_raw(static_cast<T*>(a.y) + (int64_t)row * a.ldy, f, (int)a.F, v);
 }
 
 gcn_status check_pack(int64_t n, int64_t F, int dtype, const void* x, int64_t ldx, const int8_t* Q,

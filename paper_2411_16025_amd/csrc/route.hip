@@ -70,7 +70,7 @@ __device__ inline void load_logits(const T* row, int f, int E, float (&z)[V]) {
 #pragma unroll
   for (int i = 0; i < V; i += 8) {
     float v[8];
-    unpack8(load8(row, f + i, E), v);
+    unpack_raw(load_raw<T, 8>(row, f + i, E), v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[i + e] = f + i + e < E ? v[e] : -INFINITY;
   }
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(NT) void k_route_bwd(RouteArgs a) {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = row ? d[i + e] : 0.f;
-        store8(static_cast<T*>(a.dz) + t * a.ldd, f + i, a.E, v);
+        store_raw(static_cast<T*>(a.dz) + t * a.ldd, f + i, a.E, v);
       }
   }
 }

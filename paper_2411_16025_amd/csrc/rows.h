@@ -1,4 +1,4 @@
-// Rows as pieces of eight elements, spread over the threads of a launch.
+// Rows as pieces of four or eight elements, spread over the threads of a launch.
 #pragma once
 
 #include <algorithm>
@@ -7,39 +7,55 @@
 
 namespace gcn {
 
-// Eight elements, as they lie in memory.
-template <class T>
-struct Raw8 {
-  static constexpr int kParts = 8 / kPiece<T>;
-  u4 part[kParts];
+// N elements (4 or 8), as they lie in memory.
+template <class T, int N>
+struct Raw {
+  static constexpr int kBytes = N * (int)sizeof(T);  // 8, 16 or 32
+  u4 part[(kBytes + 15) / 16];
 };
 
 // Those at column f of a row of F (any alignment); zeros behind its end, and nothing read where
 // F is at most f.
-template <class T>
-__device__ inline Raw8<T> load8(const T* row, int f, int F) {
-  Raw8<T> r;
+template <class T, int N>
+__device__ inline Raw<T, N> load_raw(const T* row, int f, int F) {
+  Raw<T, N> r;
+  if constexpr (Raw<T, N>::kBytes == 8) {
+    typedef uint32_t half __attribute__((ext_vector_type(2), aligned(2)));
+    r.part[0] = u4{0, 0, 0, 0};
+    if (f + 4 <= F) {
+      const half h = *reinterpret_cast<const half*>(row + f);
+      r.part[0][0] = h[0];
+      r.part[0][1] = h[1];
+    } else {
 #pragma unroll
-  for (int i = 0; i < Raw8<T>::kParts; ++i) r.part[i] = load_piece(row, f + i * kPiece<T>, F);
+      for (int e = 0; e < 3; ++e)
+        if (f + e < F)
+          r.part[0][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[f + e] << (16 * (e & 1));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / kPiece<T>; ++i) r.part[i] = load_piece(row, f + i * kPiece<T>, F);
+  }
   return r;
 }
 
-template <class T>
-__device__ inline void unpack8(const Raw8<T>& r, float (&v)[8]) {
+template <class T, int N>
+__device__ inline void unpack_raw(const Raw<T, N>& r, float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < Raw8<T>::kParts; ++i) {
+  for (int i = 0; i < (N + kPiece<T> - 1) / kPiece<T>; ++i) {
     float p[kPiece<T>];
     unpack<T>(r.part[i], p);
 #pragma unroll
-    for (int e = 0; e < kPiece<T>; ++e) v[i * kPiece<T> + e] = p[e];
+    for (int e = 0; e < kPiece<T>; ++e)
+      if (i * kPiece<T> + e < N) v[i * kPiece<T> + e] = p[e];
   }
 }
 
-// The part inside the row, each value rounded to nearest even.
-template <class T>
-__device__ inline void store8(T* row, int f, int F, const float (&v)[8]) {
+// The part inside the row, each value rounded to nearest even; N elements are 16 or 32 bytes.
+template <class T, int N>
+__device__ inline void store_raw(T* row, int f, int F, const float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < Raw8<T>::kParts; ++i) {
+  for (int i = 0; i < N / kPiece<T>; ++i) {
     float p[kPiece<T>];
 #pragma unroll
     for (int e = 0; e < kPiece<T>; ++e) p[e] = v[i * kPiece<T> + e];

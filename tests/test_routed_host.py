@@ -33,7 +33,7 @@ def test_group_ids_refusals(L):
     ask = dict(size=ctypes.byref(size))
     # two lists of ids with their positions and one of ids, 20 bytes an id; 2048 counts of 4 bytes for every
     # 4096 ids (1024 of few), 2 bytes an id
-    for n, groups, most in ((1000, 3, 1 << 14), (1 << 20, 16, 1 << 16), (1 << 20, 1 << 22, 22 << 20),
+    for n, groups, most in ((5000, 3, 1 << 14), (1 << 20, 16, 1 << 16), (1 << 20, 1 << 22, 22 << 20),
                             ((1 << 31) - 1, 1 << 30, (22 << 31) + (1 << 20))):
         assert L.gcn_group_ids(*{**d, **ask, "n": n, "groups": groups}.values()) == 0
         assert 0 < size.value <= most, (n, groups, size.value)

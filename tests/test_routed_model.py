@@ -51,7 +51,7 @@ def model(tmp_path_factory):
 def test_group_ids(model):
     cases = []
     for n, G in ((0, 5), (1, 1), (1, 7), (63, 3), (300, 16), (1023, 1), (1025, 64), (5000, 300), (2500, 2047),
-                 (2500, 2048), (3000, 5000), (700, 70000), (400, 1 << 20)):
+                 (2500, 2048), (3000, 5000), (700, 70000), (400, 1 << 20), (4096, 1023), (4097, 1023), (4096, 1024)):
         for i, how in enumerate(("spread", "skew", "one", "none")):
             cases.append(["check_group_ids", [n, G, how], dict(memory=i & 1, seed=n + G)])
     cases += [["check_group_ids", [900, G, "none"], dict(only=v, memory=1)] for G in (9, 3000)
@@ -84,6 +84,8 @@ def test_embed_bwd(model):
             cases.append(["check_embed_bwd", [n, F, V], dict(how=("spread", "skew", "one", "none")[i], kd=kd, kt=kt,
                                                              pad=(0, 3, 8, 1)[i], add=bool(i & 1),
                                                              memory=i >> 1, seed=n + F)])
+    # a large table, pieces of four rows to a thread
+    cases.append(["check_embed_bwd", [60, 1, 530000], dict(how="skew", seed=1)])
     model(cases)
 
 
