@@ -75,17 +75,19 @@ gcn_status take(TakeArgs a, int64_t n, int64_t F, hipStream_t s) {
 // ---- the gradient ----------------------------------------------------------------
 //
 // Rows of the table with up to `chunk` places are summed by the threads that own their pieces.
-// Longer ones in chunks: a workgroup per chunk behind a row's first one writes its sum, and those
-// workgroups then share the row's columns, each adding the first chunk's rows and the sums. Two
-// long rows never begin in one run of `chunk` places, so the sum of chunk i of a row that begins at
-// place b has the number b / chunk + i - 1 (groups.h counts the partial sums of products so).
+// Longer ones in chunks: the sum of each chunk behind the first is a partial sum, and the row's
+// pieces are then shared by the workgroups of those, which add the first chunk's rows and the partial
+// sums. Two long rows never begin in one run of `chunk` places, so the sum of chunk i of a row that
+// begins at place b has the number b / chunk + i - 1 (groups.h counts the partial sums of products
+// so). The pass over the rows writes a number's row beside it; whoever has a number takes that row
+// only if its offsets say so too, so numbers of no long row need no value there.
 
 struct SumArgs {
   RowTiles tiles;
   Groups by;            // the table's rows; by.rows places
   int32_t n;            // rows of dY
   uint32_t F;
-  int chunk;
+  int shift;            // chunk = 1 << shift
   const int32_t* order;
   const void* dy;
   int64_t lddy;
@@ -93,7 +95,9 @@ struct SumArgs {
   void* dt;
   int64_t lddt;
   bool add;
-  float* part;          // [places / chunk][F]
+  uint32_t parts;       // places / chunk
+  int32_t* owner;       // [parts]
+  float* part;          // [parts][ldp]
   int64_t ldp;
 };
 
@@ -109,7 +113,8 @@ __device__ inline void add_rows(const SumArgs& a, int64_t beg, int64_t end, int 
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const bool in = at[i] >= 0 && at[i] < a.n;
-      raw[i] = load_raw<T, N>(static_cast<const T*>(a.dy) + (in ? at[i] : 0) * a.lddy, f, in ? (int)a.F : 0);
+      raw[i] = load_raw<T, N>(static_cast<const T*>(a.dy) + (in ? at[i] : 0) * a.lddy, f,
+                              in ? (int)a.F : 0);
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
@@ -136,111 +141,197 @@ __device__ inline void write_piece(const SumArgs& a, int64_t row, int f, float (
   store_raw(to, f, (int)a.F, v);
 }
 
-// PER pieces of 16 bytes of dT to a thread: most rows of a large table have no place, and what
-// bounds the pass then is writing their zeros.
-template <class T, class TT, int PER>
+// A workgroup has up to kRows rows, or a part of a long one, in pieces of 16 bytes of dT. Most rows of
+// a large table have no place, and writing their zeros bounds the pass: they are written first,
+// without a look at anything but the offsets in LDS; then the rows that have some, which were
+// listed, so that all lanes gather (2,449,029 x 100 fp32, 250,000 places: 318 us where each piece
+// looked for its row's places, .. so).
+constexpr int kRows = 1024;
+
+template <class T, class TT, int kRowTile>
 __global__ __launch_bounds__(kThreads) void k_sum_rows(SumArgs a) {
   constexpr int N = kPiece<TT>;
-  uint32_t row[PER], piece[PER];
-  int64_t beg[PER], end[PER];
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const bool in =
-        locate(a.tiles, kThreads * PER, threadIdx.x + k * kThreads, &row[k], &piece[k]);
-    if (!in) row[k] = 0;
-    beg[k] = group_offset(a.by, (int)row[k]);
-    end[k] = group_offset(a.by, (int)row[k] + 1);
-    if (!in) end[k] = beg[k] + a.chunk + 1;  // not here
-  }
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    if (end[k] - beg[k] > a.chunk || (a.add && end[k] <= beg[k])) continue;
-    const int f = (int)(N * piece[k]);
-    float v[N] = {};
-    add_rows<T>(a, beg[k], end[k], f, v);
-    write_piece<TT>(a, row[k], f, v);
-  }
-}
-
-// The long row that partial sum p belongs to: whether there is one.
-__device__ inline bool long_row(const SumArgs& a, int64_t p, GroupTile* t, int64_t* p0,
-                                int64_t* more) {
-  *t = group_tile_from(a.by, [&](int, int64_t o) { return o / a.chunk <= p; });
-  *p0 = t->first / a.chunk;
-  *more = (t->end - t->first + a.chunk - 1) / a.chunk - 1;
-  return p >= *p0 && p < *p0 + *more;
-}
-
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_sum_chunks(SumArgs a, int64_t p) {
-  p += blockIdx.y;
-  GroupTile t;
-  int64_t p0, more;
-  if (!long_row(a, p, &t, &p0, &more)) return;
-  const int64_t beg = t.first + (p - p0 + 1) * a.chunk, end = min(beg + a.chunk, t.end);
-  const uint32_t piece = blockIdx.x * kThreads + threadIdx.x;
-  if (8 * piece >= a.F) return;
-  float v[8] = {};
-  add_rows<T>(a, beg, end, (int)(8 * piece), v);
-  store_raw(a.part + p * a.ldp, (int)(8 * piece), (int)a.F, v);
-}
-
-// The pieces of a long row, shared by the workgroups of its partial sums.
-template <class T, class TT>
-__global__ __launch_bounds__(kThreads) void k_join_chunks(SumArgs a, int64_t p) {
-  p += blockIdx.y;
-  GroupTile t;
-  int64_t p0, more;
-  if (!long_row(a, p, &t, &p0, &more)) return;
-  for (int64_t piece = ((p - p0) * gridDim.x + blockIdx.x) * kThreads + threadIdx.x;
-       8 * piece < a.F; piece += more * gridDim.x * kThreads) {
-    const int f = (int)(8 * piece);
-    float v[8] = {};
-    add_rows<T>(a, t.first, t.first + a.chunk, f, v);
-    double s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = (double)v[e];
-    for (int64_t q = p0; q < p0 + more; ++q) {
-      float x[8];
-      unpack_raw(load_raw<float, 8>(a.part + q * a.ldp, f, (int)a.F), x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] += (double)x[e];
+  __shared__ int32_t first[kRows + 1];  // the rows' first places
+  __shared__ uint16_t list[kRows];      // rows of 1 .. chunk places
+  __shared__ uint32_t listed;
+  const RowTiles& t = a.tiles;
+  const uint32_t row0 = blockIdx.x / t.parts * t.rows, rows = min(t.rows, t.n - row0);
+  const uint32_t piece0 = blockIdx.x % t.parts * kRowTile;
+  const uint32_t pieces = min(t.pieces - piece0, t.parts > 1 ? (uint32_t)kRowTile : t.pieces);  // of a row, here
+  for (uint32_t r = threadIdx.x; r <= rows; r += kThreads)
+    first[r] = (int32_t)group_offset(a.by, (int)(row0 + r));
+  if (threadIdx.x == 0) listed = 0;
+  __syncthreads();
+  const int32_t chunk = 1 << a.shift;
+  // the first wavefront lists the rows, in their order
+  if (threadIdx.x < 64) {
+    uint32_t n = 0;
+    for (uint32_t r0 = 0; r0 < rows; r0 += 64) {
+      const uint32_t r = r0 + threadIdx.x;
+      const int32_t len = r < rows ? first[r + 1] - first[r] : 0;
+      const bool some = len > 0 && len <= chunk;
+      const uint64_t m = __ballot(some);
+      if (some) list[n + (uint32_t)__popcll(m & ((1ull << threadIdx.x) - 1))] = (uint16_t)r;
+      n += (uint32_t)__popcll(m);
     }
+    if (threadIdx.x == 0) listed = n;
+  }
+  if (!a.add) {
+    const float zero[N] = {};
+    for (uint32_t q = threadIdx.x; q < rows * pieces; q += kThreads) {
+      const uint32_t r = pieces == 1 ? q : (rows > 1 ? (uint32_t)((uint64_t)q * t.magic >> 32) : 0);
+      if (first[r + 1] <= first[r])
+        store_raw(static_cast<TT*>(a.dt) + (int64_t)(row0 + r) * a.lddt,
+                  (int)(N * (piece0 + q - r * pieces)), (int)a.F, zero);
+    }
+  }
+  // the numbers of long rows' partial sums
+  if (blockIdx.x % t.parts == 0)
+    for (uint32_t r = threadIdx.x; r < rows; r += kThreads) {
+      const int32_t len = first[r + 1] - first[r];
+      if (len <= chunk) continue;
+      const uint32_t p0 = (uint32_t)first[r] >> a.shift, more = (uint32_t)(len - 1) >> a.shift;
+      for (uint32_t p = p0; p < p0 + more; ++p) a.owner[p] = (int32_t)(row0 + r);
+    }
+  __syncthreads();
+  for (uint32_t q = threadIdx.x; q < listed * pieces; q += kThreads) {
+    const uint32_t i = pieces == 1 ? q : (rows > 1 ? (uint32_t)((uint64_t)q * t.magic >> 32) : 0);
+    const uint32_t r = list[i];
+    const int f = (int)(N * (piece0 + q - i * pieces));
+    float v[N] = {};
+    add_rows<T>(a, first[r], first[r + 1], f, v);
+    write_piece<TT>(a, row0 + r, f, v);
+  }
+}
+
+// The long row that partial sum p belongs to.
+struct LongRow {
+  bool any;
+  int v;
+  int64_t first, end;
+  uint32_t p0, more;  // its partial sums
+};
+__device__ inline LongRow long_row(const SumArgs& a, uint32_t p) {
+  LongRow r{};
+  if (p >= a.parts) return r;
+  r.v = a.owner[p];
+  if (r.v < 0 || r.v >= a.by.n) return r;
+  r.first = group_offset(a.by, r.v);
+  r.end = group_offset(a.by, r.v + 1);
+  const int64_t len = r.end - r.first;
+  r.p0 = (uint32_t)(r.first >> a.shift);
+  r.more = len > (1 << a.shift) ? (uint32_t)((len - 1) >> a.shift) : 0;
+  r.any = p >= r.p0 && p - r.p0 < r.more;
+  return r;
+}
+
+// `lanes` neighbouring threads (a power of two) have a chunk.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_sum_chunks(SumArgs a, int lanes) {
+  const uint32_t p = blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
+  const LongRow r = long_row(a, p);
+  if (!r.any) return;
+  const int64_t beg = r.first + ((int64_t)(p - r.p0 + 1) << a.shift);
+  const int64_t end = min(beg + (1 << a.shift), r.end);
+  for (int64_t f = 8 * (threadIdx.x % lanes); f < a.F; f += 8 * lanes) {
+    float v[8] = {};
+    add_rows<T>(a, beg, end, (int)f, v);
+    store_raw(a.part + p * a.ldp, (int)f, (int)a.F, v);
+  }
+}
+
+// A share of a long row's pieces: the threads divide the first chunk's rows and the partial sums
+// among them, and the sums of a piece meet in LDS. kInTurn numbers to a workgroup, as most are of no
+// long row.
+constexpr int kInTurn = 2;
+
+template <class T, class TT>
+__global__ __launch_bounds__(kThreads) void k_join_chunks(SumArgs a) {
+  __shared__ double sums[kThreads][9];  // (9: the rows fall on different banks)
+  const int64_t pieces = ((int64_t)a.F + 7) / 8;
+  for (int i = 0; i < kInTurn; ++i) {
+    const uint32_t p = blockIdx.x * kInTurn + i;
+    const LongRow r = long_row(a, p);  // (the same for all threads)
+    if (!r.any) continue;
+    int share = 8;  // pieces of a workgroup
+    while (share < kThreads && (int64_t)share * r.more < pieces) share *= 2;
+    const int groups = kThreads / share, g = threadIdx.x / share;
+    const int part = max(1, (1 << a.shift) / groups);  // of the first chunk's places
+    for (int64_t s0 = (int64_t)(p - r.p0) * share; s0 < pieces; s0 += (int64_t)r.more * share) {
+      const int64_t piece = s0 + threadIdx.x % share;
+      const int f = (int)(8 * piece);
+      double s[8] = {};
+      float v[8] = {};
+      if (piece < pieces) {
+        if (g * part < (1 << a.shift))
+          add_rows<T>(a, r.first + g * part, r.first + (g + 1) * part, f, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)s[e];
-    write_piece<TT>(a, t.g, f, v);
+        for (int e = 0; e < 8; ++e) s[e] = (double)v[e];
+        constexpr int kAhead = 4;
+        for (uint32_t q = r.p0 + g; q < r.p0 + r.more; q += kAhead * groups) {
+          Raw<float, 8> raw[kAhead];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+            raw[j] = load_raw<float, 8>(a.part + min(q + j * groups, r.p0 + r.more - 1) * a.ldp, f,
+                                        (int)a.F);
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            float x[8];
+            unpack_raw(raw[j], x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += q + j * groups < r.p0 + r.more ? (double)x[e] : 0.0;
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums[threadIdx.x][e] = s[e];
+      __syncthreads();
+      if (g == 0 && piece < pieces) {
+        for (int o = 1; o < groups; ++o)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[e] += sums[threadIdx.x + o * share][e];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)s[e];
+        write_piece<TT>(a, r.v, f, v);
+      }
+      __syncthreads();
+    }
   }
 }
 
 template <class T, class TT>
 gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
-  const int64_t pieces = ceil_div((int64_t)a.F, (int64_t)kPiece<TT>);
-  const bool few = a.by.n * pieces < 2048 * kThreads;
-  a.tiles = row_tiles(a.by.n, pieces, kThreads * (few ? 1 : 4));
-  a.chunk = 32;
+  // small tiles where most rows have places to gather (131,072 places of 50,000 rows of 1024 bf16: 182 us
+  // in tiles of 4096 pieces, .. in 1024)
+  const bool sparse = a.by.n > a.by.rows;
+  a.tiles = row_tiles(a.by.n, ceil_div((int64_t)a.F, (int64_t)kPiece<TT>), sparse ? 4096 : 1024);
+  a.tiles.rows = std::min<uint32_t>(a.tiles.rows, kRows);
+  a.shift = a.by.rows <= (1 << 18) ? 5 : 7;
   GCN_CHECK(launch_fits(a.tiles.blocks(), kThreads));
-  const int64_t parts = a.by.rows / a.chunk;
+  a.parts = (uint32_t)(a.by.rows >> a.shift);
   a.ldp = ceil_div((int64_t)a.F, (int64_t)8) * 8;
-  if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * a.ldp, "sums of repeated ids"));
+  if (a.parts > 0) {
+    GCN_CHECK(scratch->alloc(&a.part, a.parts * a.ldp, "sums of repeated ids"));
+    GCN_CHECK(scratch->alloc(&a.owner, a.parts, "rows of repeated ids"));
+  }
   if (scratch->asked()) return GCN_OK;
   ProfScope ps("embed_bwd", s);
   const dim3 rows((unsigned)a.tiles.blocks());
-  if (few)
-    hipLaunchKernelGGL((k_sum_rows<T, TT, 1>), rows, dim3(kThreads), 0, s, a);
+  if (sparse)
+    hipLaunchKernelGGL((k_sum_rows<T, TT, 4096>), rows, dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((k_sum_rows<T, TT, 4>), rows, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_sum_rows<T, TT, 1024>), rows, dim3(kThreads), 0, s, a);
   GCN_HIP(hipGetLastError());
-  const unsigned wide = (unsigned)ceil_div(a.ldp, (int64_t)8 * kThreads);
-  for (int64_t p = 0; p < parts; p += 65535) {  // (a grid's second axis)
-    const dim3 grid(wide, (unsigned)std::min<int64_t>(parts - p, 65535));
-    hipLaunchKernelGGL(k_sum_chunks<T>, grid, dim3(kThreads), 0, s, a, p);
-    GCN_HIP(hipGetLastError());
-  }
-  for (int64_t p = 0; p < parts; p += 65535) {
-    const dim3 grid(wide, (unsigned)std::min<int64_t>(parts - p, 65535));
-    hipLaunchKernelGGL((k_join_chunks<T, TT>), grid, dim3(kThreads), 0, s, a, p);
-    GCN_HIP(hipGetLastError());
-  }
+  if (a.parts == 0) return GCN_OK;
+  int lanes = 8;
+  while (lanes < kThreads && 8 * (int64_t)lanes < a.F) lanes *= 2;
+  hipLaunchKernelGGL(k_sum_chunks<T>,
+                     dim3((unsigned)ceil_div(a.parts, (int64_t)kThreads / lanes)),
+                     dim3(kThreads), 0, s, a, lanes);
+  GCN_HIP(hipGetLastError());
+  hipLaunchKernelGGL((k_join_chunks<T, TT>), dim3((unsigned)ceil_div(a.parts, (int64_t)kInTurn)),
+                     dim3(kThreads), 0, s, a);
+  GCN_HIP(hipGetLastError());
   return GCN_OK;
 }
 

@@ -104,15 +104,20 @@ __global__ __launch_bounds__(1024) void k_sum_tiles(SortArgs a) {
   }
 }
 
-// A wavefront's ITEMS times 64 keys from `base` (the lane's first) on, and each one's number among
-// those of its digit, which cnt [digits], all 0 before, then holds.
+// A wavefront's ITEMS times 64 keys from `base` (the lane's first) on.
 template <bool FIRST, int ITEMS>
-__device__ inline void rank_keys(const SortArgs& a, uint32_t base, uint32_t* cnt,
-                                 uint64_t (&key)[ITEMS], uint32_t (&rank)[ITEMS]) {
-  const int lane = threadIdx.x & 63;
+__device__ inline void load_keys(const SortArgs& a, uint32_t base, uint64_t (&key)[ITEMS]) {
 #pragma unroll
   for (int j = 0; j < ITEMS; ++j)
     key[j] = base + j * 64 < a.n ? load_key<FIRST>(a, base + j * 64) : ~0ull;
+}
+
+// Each one's number among the wavefront's of its digit, whose counts cnt [digits], all 0 before, then
+// holds.
+template <int ITEMS>
+__device__ inline void rank_keys(const SortArgs& a, uint32_t base, uint32_t* cnt,
+                                 const uint64_t (&key)[ITEMS], uint32_t (&rank)[ITEMS]) {
+  const int lane = threadIdx.x & 63;
   const uint64_t below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
 #pragma unroll
   for (int j = 0; j < ITEMS; ++j) {
@@ -164,6 +169,10 @@ __global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
   __shared__ uint32_t cnt[kWaves][kMaxDigits];  // ids of a wavefront, then of those before it
   __shared__ uint32_t sums[kWaves];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  uint64_t key[ITEMS];
+  uint32_t rank[ITEMS];
+  const uint32_t base = blockIdx.x * (kThreads * ITEMS) + w * (64 * ITEMS) + lane;
+  load_keys<FIRST>(a, base, key);
 #pragma unroll
   for (int q = 0; q < kWaves; ++q)
     for (uint32_t d = t; d < a.digits; d += kThreads) cnt[q][d] = 0;
@@ -189,10 +198,7 @@ __global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
     first[d] = run + here[i];
     run += total[i];
   }
-  uint64_t key[ITEMS];
-  uint32_t rank[ITEMS];
-  const uint32_t base = blockIdx.x * (kThreads * ITEMS) + w * (64 * ITEMS) + lane;
-  rank_keys<FIRST>(a, base, cnt[w], key, rank);
+  rank_keys(a, base, cnt[w], key, rank);
   __syncthreads();
   for (uint32_t d = t; d < a.digits; d += kThreads) {
     uint32_t s = first[d];
@@ -226,14 +232,15 @@ __global__ __launch_bounds__(kOneThreads) void k_sort_one(SortArgs a) {
   __shared__ uint32_t cnt[kOneWaves][kOneDigits];
   __shared__ uint32_t sums[kOneWaves];
   const uint32_t t = threadIdx.x, w = t >> 6;
+  uint64_t key[kOneItems];
+  uint32_t rank[kOneItems];
+  const uint32_t base = w * (64 * kOneItems) + (t & 63);
+  load_keys<true>(a, base, key);
   if (t < a.digits)
 #pragma unroll
     for (int q = 0; q < kOneWaves; ++q) cnt[q][t] = 0;
   __syncthreads();
-  uint64_t key[kOneItems];
-  uint32_t rank[kOneItems];
-  const uint32_t base = w * (64 * kOneItems) + (t & 63);
-  rank_keys<true>(a, base, cnt[w], key, rank);
+  rank_keys(a, base, cnt[w], key, rank);
   __syncthreads();
   uint32_t mine = 0;
   if (t < a.digits)
@@ -281,7 +288,7 @@ __device__ inline uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32
 }
 
 // Offsets from the sorted keys, 1024 groups to a workgroup: the keys between its ends are found by
-// two wavefronts, and brought to LDS where they fit there.
+// two wavefronts; all of them, or every some, are brought to LDS, where most of a search is.
 constexpr uint32_t kPerBlock = 1024, kStaged = 2048;
 __global__ __launch_bounds__(kThreads) void k_offsets(const uint32_t* sorted, uint32_t n,
                                                       uint32_t groups, int64_t* offsets) {
@@ -292,13 +299,14 @@ __global__ __launch_bounds__(kThreads) void k_offsets(const uint32_t* sorted, ui
     if ((threadIdx.x & 63) == 0) ends[w] = p;
   }
   __syncthreads();
-  const uint32_t lo = ends[0], len = ends[1] - lo;
-  if (len <= kStaged)
-    for (uint32_t i = threadIdx.x; i < len; i += kThreads) keys[i] = sorted[lo + i];
+  const uint32_t lo = ends[0], len = ends[1] - lo, step = len / kStaged + 1;
+  const uint32_t staged = len / step;  // the last key of every `step`
+  for (uint32_t i = threadIdx.x; i < staged; i += kThreads) keys[i] = sorted[lo + i * step + step - 1];
   __syncthreads();
-  for (uint32_t v = v0 + threadIdx.x; v < v0 + kPerBlock && v <= groups; v += kThreads)
-    offsets[v] = len <= kStaged ? lo + lower_bound(keys, 0, len, v)
-                                : lower_bound(sorted, lo, lo + len, v);
+  for (uint32_t v = v0 + threadIdx.x; v < v0 + kPerBlock && v <= groups; v += kThreads) {
+    const uint32_t at = lower_bound(keys, 0, staged, v) * step;
+    offsets[v] = lower_bound(sorted, lo + at, lo + min(at + step - 1, len), v);
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void k_zero_offsets(int64_t* offsets, int64_t count) {
