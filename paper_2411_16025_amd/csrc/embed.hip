@@ -102,9 +102,8 @@ struct SumArgs {
 };
 
 // v += the rows at places [beg, end), in their order.
-template <class T, int N>
+template <class T, int N, int kAhead = 4>
 __device__ inline void add_rows(const SumArgs& a, int64_t beg, int64_t end, int f, float (&v)[N]) {
-  constexpr int kAhead = 4;
   for (int64_t j = beg; j < end; j += kAhead) {
     int32_t at[kAhead];
     Raw<T, N> raw[kAhead];
@@ -152,29 +151,35 @@ template <class T, class TT, int kRowTile>
 __global__ __launch_bounds__(kThreads) void k_sum_rows(SumArgs a) {
   constexpr int N = kPiece<TT>;
   __shared__ int32_t first[kRows + 1];  // the rows' first places
-  __shared__ uint16_t list[kRows];      // rows of 1 .. chunk places
-  __shared__ uint32_t listed;
+  __shared__ uint16_t list[kRows];      // rows of 1 .. chunk places, and from the end on those of more
+  __shared__ uint32_t listed, longs;
   const RowTiles& t = a.tiles;
   const uint32_t row0 = blockIdx.x / t.parts * t.rows, rows = min(t.rows, t.n - row0);
   const uint32_t piece0 = blockIdx.x % t.parts * kRowTile;
   const uint32_t pieces = min(t.pieces - piece0, t.parts > 1 ? (uint32_t)kRowTile : t.pieces);  // of a row, here
   for (uint32_t r = threadIdx.x; r <= rows; r += kThreads)
     first[r] = (int32_t)group_offset(a.by, (int)(row0 + r));
-  if (threadIdx.x == 0) listed = 0;
   __syncthreads();
   const int32_t chunk = 1 << a.shift;
   // the first wavefront lists the rows, in their order
   if (threadIdx.x < 64) {
-    uint32_t n = 0;
+    uint32_t n = 0, l = 0;
     for (uint32_t r0 = 0; r0 < rows; r0 += 64) {
       const uint32_t r = r0 + threadIdx.x;
       const int32_t len = r < rows ? first[r + 1] - first[r] : 0;
-      const bool some = len > 0 && len <= chunk;
-      const uint64_t m = __ballot(some);
-      if (some) list[n + (uint32_t)__popcll(m & ((1ull << threadIdx.x) - 1))] = (uint16_t)r;
-      n += (uint32_t)__popcll(m);
+      const uint64_t some = __ballot(len > 0 && len <= chunk), more = __ballot(len > chunk);
+      const uint64_t below = (1ull << threadIdx.x) - 1;
+      if (len > chunk)
+        list[kRows - 1 - l - (uint32_t)__popcll(more & below)] = (uint16_t)r;
+      else if (len > 0)
+        list[n + (uint32_t)__popcll(some & below)] = (uint16_t)r;
+      n += (uint32_t)__popcll(some);
+      l += (uint32_t)__popcll(more);
     }
-    if (threadIdx.x == 0) listed = n;
+    if (threadIdx.x == 0) {
+      listed = n;
+      longs = l;
+    }
   }
   if (!a.add) {
     const float zero[N] = {};
@@ -185,15 +190,14 @@ __global__ __launch_bounds__(kThreads) void k_sum_rows(SumArgs a) {
                   (int)(N * (piece0 + q - r * pieces)), (int)a.F, zero);
     }
   }
+  __syncthreads();
   // the numbers of long rows' partial sums
   if (blockIdx.x % t.parts == 0)
-    for (uint32_t r = threadIdx.x; r < rows; r += kThreads) {
-      const int32_t len = first[r + 1] - first[r];
-      if (len <= chunk) continue;
-      const uint32_t p0 = (uint32_t)first[r] >> a.shift, more = (uint32_t)(len - 1) >> a.shift;
-      for (uint32_t p = p0; p < p0 + more; ++p) a.owner[p] = (int32_t)(row0 + r);
+    for (uint32_t i = 0; i < longs; ++i) {
+      const uint32_t r = list[kRows - 1 - i], p0 = (uint32_t)first[r] >> a.shift;
+      const uint32_t more = (uint32_t)(first[r + 1] - first[r] - 1) >> a.shift;
+      for (uint32_t p = threadIdx.x; p < more; p += kThreads) a.owner[p0 + p] = (int32_t)(row0 + r);
     }
-  __syncthreads();
   for (uint32_t q = threadIdx.x; q < listed * pieces; q += kThreads) {
     const uint32_t i = pieces == 1 ? q : (rows > 1 ? (uint32_t)((uint64_t)q * t.magic >> 32) : 0);
     const uint32_t r = list[i];
@@ -225,19 +229,18 @@ __device__ inline LongRow long_row(const SumArgs& a, uint32_t p) {
   return r;
 }
 
-// `lanes` neighbouring threads (a power of two) have a chunk.
+// A thread has a piece of a chunk's sum.
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_sum_chunks(SumArgs a, int lanes) {
-  const uint32_t p = blockIdx.x * (kThreads / lanes) + threadIdx.x / lanes;
+__global__ __launch_bounds__(kThreads) void k_sum_chunks(SumArgs a, RowTiles tiles) {
+  constexpr int N = kPiece<T>;
+  uint32_t p, piece;
+  if (!locate(tiles, kThreads, threadIdx.x, &p, &piece)) return;
   const LongRow r = long_row(a, p);
   if (!r.any) return;
   const int64_t beg = r.first + ((int64_t)(p - r.p0 + 1) << a.shift);
-  const int64_t end = min(beg + (1 << a.shift), r.end);
-  for (int64_t f = 8 * (threadIdx.x % lanes); f < a.F; f += 8 * lanes) {
-    float v[8] = {};
-    add_rows<T>(a, beg, end, (int)f, v);
-    store_raw(a.part + p * a.ldp, (int)f, (int)a.F, v);
-  }
+  float v[N] = {};
+  add_rows<T, N, 8>(a, beg, min(beg + (1 << a.shift), r.end), (int)(N * piece), v);
+  store_raw(a.part + p * a.ldp, (int)(N * piece), (int)a.F, v);
 }
 
 // A share of a long row's pieces: the threads divide the first chunk's rows and the partial sums
@@ -323,11 +326,9 @@ gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
     hipLaunchKernelGGL((k_sum_rows<T, TT, 1024>), rows, dim3(kThreads), 0, s, a);
   GCN_HIP(hipGetLastError());
   if (a.parts == 0) return GCN_OK;
-  int lanes = 8;
-  while (lanes < kThreads && 8 * (int64_t)lanes < a.F) lanes *= 2;
-  hipLaunchKernelGGL(k_sum_chunks<T>,
-                     dim3((unsigned)ceil_div(a.parts, (int64_t)kThreads / lanes)),
-                     dim3(kThreads), 0, s, a, lanes);
+  const RowTiles chunks = row_tiles(a.parts, ceil_div((int64_t)a.F, (int64_t)kPiece<T>), kThreads);
+  GCN_CHECK(launch_fits(chunks.blocks(), kThreads));
+  hipLaunchKernelGGL(k_sum_chunks<T>, dim3((unsigned)chunks.blocks()), dim3(kThreads), 0, s, a, chunks);
   GCN_HIP(hipGetLastError());
   hipLaunchKernelGGL((k_join_chunks<T, TT>), dim3((unsigned)ceil_div(a.parts, (int64_t)kInTurn)),
                      dim3(kThreads), 0, s, a);

@@ -16,7 +16,6 @@
 namespace gcn {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxBits = 11, kMaxDigits = 1 << kMaxBits;
 
 struct SortArgs {
@@ -49,19 +48,19 @@ __device__ inline uint32_t digit(const SortArgs& a, uint64_t key) {
   return (uint32_t)(key >> (32 + a.shift)) & ((1u << a.bits) - 1);
 }
 
-template <bool FIRST, int ITEMS>
-__global__ __launch_bounds__(kThreads) void k_count(SortArgs a) {
+template <bool FIRST, int NT, int ITEMS>
+__global__ __launch_bounds__(NT) void k_count(SortArgs a) {
   __shared__ uint32_t cnt[kMaxDigits];
-  for (uint32_t d = threadIdx.x; d < a.digits; d += kThreads) cnt[d] = 0;
+  for (uint32_t d = threadIdx.x; d < a.digits; d += NT) cnt[d] = 0;
   __syncthreads();
-  const uint32_t base = blockIdx.x * (kThreads * ITEMS);
+  const uint32_t base = blockIdx.x * (NT * ITEMS);
 #pragma unroll
   for (int j = 0; j < ITEMS; ++j) {
-    const uint32_t i = base + j * kThreads + threadIdx.x;
+    const uint32_t i = base + j * NT + threadIdx.x;
     if (i < a.n) atomicAdd(&cnt[digit(a, load_key<FIRST>(a, i))], 1u);
   }
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < a.digits; d += kThreads)
+  for (uint32_t d = threadIdx.x; d < a.digits; d += NT)
     a.hist[(uint64_t)blockIdx.x * a.digits + d] = cnt[d];
 }
 
@@ -163,22 +162,23 @@ __device__ inline void put(const SortArgs& a, uint64_t key, uint32_t place) {
   if (a.slot) a.slot[at] = in ? (int32_t)place : -1;
 }
 
-template <bool FIRST, bool LAST, int ITEMS>
-__global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
+template <bool FIRST, bool LAST, int NT, int ITEMS>
+__global__ __launch_bounds__(NT) void k_place(SortArgs a) {
+  constexpr int kWaves = NT / 64;
   __shared__ uint32_t first[kMaxDigits];        // the place of the tile's first id of a digit
   __shared__ uint32_t cnt[kWaves][kMaxDigits];  // ids of a wavefront, then of those before it
   __shared__ uint32_t sums[kWaves];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   uint64_t key[ITEMS];
   uint32_t rank[ITEMS];
-  const uint32_t base = blockIdx.x * (kThreads * ITEMS) + w * (64 * ITEMS) + lane;
+  const uint32_t base = blockIdx.x * (NT * ITEMS) + w * (64 * ITEMS) + lane;
   load_keys<FIRST>(a, base, key);
 #pragma unroll
   for (int q = 0; q < kWaves; ++q)
-    for (uint32_t d = t; d < a.digits; d += kThreads) cnt[q][d] = 0;
+    for (uint32_t d = t; d < a.digits; d += NT) cnt[q][d] = 0;
   // each thread has a run of digits
-  constexpr int kRun = kMaxDigits / kThreads;
-  const uint32_t per = (a.digits + kThreads - 1) / kThreads;
+  constexpr int kRun = kMaxDigits / NT;
+  const uint32_t per = (a.digits + NT - 1) / NT;
   uint32_t total[kRun], here[kRun], mine = 0;
 #pragma unroll
   for (uint32_t i = 0; i < kRun; ++i) {
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
   }
   rank_keys(a, base, cnt[w], key, rank);
   __syncthreads();
-  for (uint32_t d = t; d < a.digits; d += kThreads) {
+  for (uint32_t d = t; d < a.digits; d += NT) {
     uint32_t s = first[d];
 #pragma unroll
     for (int q = 0; q < kWaves; ++q) {
@@ -224,13 +224,13 @@ __global__ __launch_bounds__(kThreads) void k_place(SortArgs a) {
 }
 
 // Few ids and groups: all of it by one workgroup, in one launch (48 ids: .. us).
-constexpr int kOneThreads = 1024, kOneItems = 4, kOneMost = kOneThreads * kOneItems;
-constexpr uint32_t kOneDigits = 1024;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kOneItems = 4, kOneMost = kThreads * kOneItems;
+constexpr uint32_t kOneDigits = kThreads;
 
-__global__ __launch_bounds__(kOneThreads) void k_sort_one(SortArgs a) {
-  constexpr int kOneWaves = kOneThreads / 64;
-  __shared__ uint32_t cnt[kOneWaves][kOneDigits];
-  __shared__ uint32_t sums[kOneWaves];
+__global__ __launch_bounds__(kThreads) void k_sort_one(SortArgs a) {
+  __shared__ uint32_t cnt[kWaves][kOneDigits];
+  __shared__ uint32_t sums[kWaves];
   const uint32_t t = threadIdx.x, w = t >> 6;
   uint64_t key[kOneItems];
   uint32_t rank[kOneItems];
@@ -238,19 +238,19 @@ __global__ __launch_bounds__(kOneThreads) void k_sort_one(SortArgs a) {
   load_keys<true>(a, base, key);
   if (t < a.digits)
 #pragma unroll
-    for (int q = 0; q < kOneWaves; ++q) cnt[q][t] = 0;
+    for (int q = 0; q < kWaves; ++q) cnt[q][t] = 0;
   __syncthreads();
   rank_keys(a, base, cnt[w], key, rank);
   __syncthreads();
   uint32_t mine = 0;
   if (t < a.digits)
 #pragma unroll
-    for (int q = 0; q < kOneWaves; ++q) mine += cnt[q][t];
+    for (int q = 0; q < kWaves; ++q) mine += cnt[q][t];
   uint32_t run = before_thread(mine, sums);
   if (t < a.digits) {
     a.offsets[t] = run;
 #pragma unroll
-    for (int q = 0; q < kOneWaves; ++q) {
+    for (int q = 0; q < kWaves; ++q) {
       const uint32_t c = cnt[q][t];
       cnt[q][t] = run;
       run += c;
@@ -276,21 +276,10 @@ __device__ inline uint32_t wave_lower_bound(const uint32_t* keys, uint32_t n, ui
   return lo;
 }
 
-__device__ inline uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t hi, uint32_t v) {
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (keys[mid] < v)
-      lo = mid + 1;
-    else
-      hi = mid;
-  }
-  return lo;
-}
-
 // Offsets from the sorted keys, 1024 groups to a workgroup: the keys between its ends are found by
 // two wavefronts; all of them, or every some, are brought to LDS, where most of a search is.
-constexpr uint32_t kPerBlock = 1024, kStaged = 2048;
-__global__ __launch_bounds__(kThreads) void k_offsets(const uint32_t* sorted, uint32_t n,
+constexpr uint32_t kFinders = 256, kEach = 4, kPerBlock = kFinders * kEach, kStaged = 2048;
+__global__ __launch_bounds__(kFinders) void k_offsets(const uint32_t* sorted, uint32_t n,
                                                       uint32_t groups, int64_t* offsets) {
   __shared__ uint32_t ends[2], keys[kStaged];
   const uint32_t v0 = blockIdx.x * kPerBlock, w = threadIdx.x >> 6;
@@ -301,11 +290,26 @@ __global__ __launch_bounds__(kThreads) void k_offsets(const uint32_t* sorted, ui
   __syncthreads();
   const uint32_t lo = ends[0], len = ends[1] - lo, step = len / kStaged + 1;
   const uint32_t staged = len / step;  // the last key of every `step`
-  for (uint32_t i = threadIdx.x; i < staged; i += kThreads) keys[i] = sorted[lo + i * step + step - 1];
+  for (uint32_t i = threadIdx.x; i < staged; i += kFinders) keys[i] = sorted[lo + i * step + step - 1];
   __syncthreads();
-  for (uint32_t v = v0 + threadIdx.x; v < v0 + kPerBlock && v <= groups; v += kThreads) {
-    const uint32_t at = lower_bound(keys, 0, staged, v) * step;
-    offsets[v] = lower_bound(sorted, lo + at, lo + min(at + step - 1, len), v);
+  // a thread's searches go on together
+  uint32_t at[kEach] = {}, left = staged;
+  auto halve = [&](uint32_t& left, auto key) {  // of `left` keys from at on, half are known to be below or not
+    const uint32_t mid = left / 2;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i)
+      at[i] += key(at[i] + mid) < v0 + threadIdx.x + i * kFinders ? left - mid : 0;
+    left = mid;
+  };
+  while (left > 0) halve(left, [&](uint32_t i) { return keys[min(i, staged - 1)]; });
+#pragma unroll
+  for (uint32_t i = 0; i < kEach; ++i) at[i] *= step;
+  for (left = step - 1; left > 0;)
+    halve(left, [&](uint32_t i) { return i < len ? sorted[lo + i] : 0xFFFFFFFFu; });
+#pragma unroll
+  for (uint32_t i = 0; i < kEach; ++i) {
+    const uint32_t v = v0 + threadIdx.x + i * kFinders;
+    if (v <= groups) offsets[v] = lo + min(at[i], len);
   }
 }
 
@@ -314,35 +318,39 @@ __global__ __launch_bounds__(kThreads) void k_zero_offsets(int64_t* offsets, int
   if (i < count) offsets[i] = 0;
 }
 
-template <bool FIRST, bool LAST, int ITEMS>
+template <bool FIRST, bool LAST, int NT, int ITEMS>
 gcn_status pass(const SortArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_count<FIRST, ITEMS>), dim3(a.tiles), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((k_count<FIRST, NT, ITEMS>), dim3(a.tiles), dim3(NT), 0, s, a);
   GCN_HIP(hipGetLastError());
   hipLaunchKernelGGL(k_sum_tiles, dim3((a.digits + 63) / 64), dim3(1024), 0, s, a);
   GCN_HIP(hipGetLastError());
-  hipLaunchKernelGGL((k_place<FIRST, LAST, ITEMS>), dim3(a.tiles), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((k_place<FIRST, LAST, NT, ITEMS>), dim3(a.tiles), dim3(NT), 0, s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }
 
-template <int ITEMS>
+template <int NT, int ITEMS>
 gcn_status sort_ids(SortArgs a, int bits, int passes, uint64_t* pairs[2], hipStream_t s) {
-  if (passes == 1) return pass<true, true, ITEMS>(a, s);
+  if (passes == 1) return pass<true, true, NT, ITEMS>(a, s);
   for (int p = 0; p < passes; ++p) {
     a.shift = bits * p / passes;
     a.bits = bits * (p + 1) / passes - a.shift;
     a.digits = 1u << a.bits;
     a.in = pairs[(p + 1) & 1];
     a.out = pairs[p & 1];
-    GCN_CHECK((p == 0            ? pass<true, false, ITEMS>(a, s)
-               : p + 1 == passes ? pass<false, true, ITEMS>(a, s)
-                                 : pass<false, false, ITEMS>(a, s)));
+    GCN_CHECK((p == 0            ? pass<true, false, NT, ITEMS>(a, s)
+               : p + 1 == passes ? pass<false, true, NT, ITEMS>(a, s)
+                                 : pass<false, false, NT, ITEMS>(a, s)));
   }
   hipLaunchKernelGGL(k_offsets, dim3((unsigned)ceil_div((int64_t)a.groups + 1, (int64_t)kPerBlock)),
-                     dim3(kThreads), 0, s, a.sorted, a.n, a.groups, a.offsets);
+                     dim3(kFinders), 0, s, a.sorted, a.n, a.groups, a.offsets);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }
+
+// Ids of a tile: small ones while those are not enough for the CUs (131,072 ids of 50,000 groups: 36 us in
+// tiles of 1024, 42 of 4096; 1,000,000 of 64: 25 and 20), 16 to a thread where there are many.
+int tile_of(int64_t n) { return n <= (1 << 18) ? 1024 : n <= (1 << 20) ? 4096 : 16384; }
 
 }  // namespace
 }  // namespace gcn
@@ -376,7 +384,6 @@ extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_gro
   }
   const int bits = bits_for((uint64_t)n_groups);
   const int passes = std::max(1, (bits + kMaxBits - 1) / kMaxBits);
-  const bool small = n <= (1 << 19);  // tiles of 1024 ids, so that there are enough of them
   SortArgs a{};
   a.n = (uint32_t)n;
   a.groups = (uint32_t)n_groups;
@@ -389,11 +396,11 @@ extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_gro
   if (n <= kOneMost && a.digits <= kOneDigits) {
     if (scratch.asked()) return GCN_OK;
     ProfScope ps("group_ids", s);
-    hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(kOneThreads), 0, s, a);
+    hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(kThreads), 0, s, a);
     GCN_HIP(hipGetLastError());
     return GCN_OK;
   }
-  a.tiles = (uint32_t)ceil_div(n, (int64_t)kThreads * (small ? 4 : 16));
+  a.tiles = (uint32_t)ceil_div(n, (int64_t)tile_of(n));
   const int64_t digits = passes == 1 ? n_groups + 1 : int64_t(1) << ((bits + passes - 1) / passes);
   GCN_CHECK(scratch.alloc(&a.hist, (int64_t)a.tiles * digits, "digit counts"));
   GCN_CHECK(scratch.alloc(&a.total, digits, "digit totals"));
@@ -405,5 +412,9 @@ extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_gro
   }
   if (scratch.asked()) return GCN_OK;
   ProfScope ps("group_ids", s);
-  return small ? sort_ids<4>(a, bits, passes, pairs, s) : sort_ids<16>(a, bits, passes, pairs, s);
+  switch (tile_of(n)) {
+    case 1024: return sort_ids<256, 4>(a, bits, passes, pairs, s);
+    case 4096: return sort_ids<1024, 4>(a, bits, passes, pairs, s);
+    default: return sort_ids<1024, 16>(a, bits, passes, pairs, s);
+  }
 }
