@@ -144,7 +144,7 @@ __device__ inline void write_piece(const SumArgs& a, int64_t row, int f, float (
 // a large table have no place, and writing their zeros bounds the pass: they are written first,
 // without a look at anything but the offsets in LDS; then the rows that have some, which were
 // listed, so that all lanes gather (2,449,029 x 100 fp32, 250,000 places: 318 us where each piece
-// looked for its row's places, .. so).
+// looked for its row's places, 245 so; with stores past the caches 282, and rows of 47 258 instead of 128).
 constexpr int kRows = 1024;
 
 template <class T, class TT, int kRowTile>
@@ -304,9 +304,9 @@ __global__ __launch_bounds__(kThreads) void k_join_chunks(SumArgs a) {
 
 template <class T, class TT>
 gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
-  // small tiles where most rows have places to gather (131,072 places of 50,000 rows of 1024 bf16: 182 us
-  // in tiles of 4096 pieces, .. in 1024)
-  const bool sparse = a.by.n > a.by.rows;
+  // small tiles where many rows have places to gather (131,072 places of 50,000 rows of 1024 bf16: 182 us
+  // in tiles of 4096 pieces, 85 in 1024; 16,384 of 32,000 x 4096: 134 and 50)
+  const bool sparse = a.by.n > 4 * a.by.rows;
   a.tiles = row_tiles(a.by.n, ceil_div((int64_t)a.F, (int64_t)kPiece<TT>), sparse ? 4096 : 1024);
   a.tiles.rows = std::min<uint32_t>(a.tiles.rows, kRows);
   a.shift = a.by.rows <= (1 << 18) ? 5 : 7;

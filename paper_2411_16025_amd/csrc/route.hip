@@ -187,13 +187,36 @@ struct Left<bf16, G, V> {
   }
 };
 
+// The loss, from every thread's part of sum_e c_e P_e and of sum_e c_e, and the rows with a choice.
+template <int NT>
+__device__ inline void write_loss(const RouteArgs& a, double cp, double c, const uint32_t& rows) {
+  __shared__ double sums[2][NT / 64];
+  const int t = threadIdx.x;
+  cp = slot_sum<64>(cp);
+  c = slot_sum<64>(c);
+  if ((t & 63) == 0) {
+    sums[0][t >> 6] = cp;
+    sums[1][t >> 6] = c;
+  }
+  __syncthreads();
+  if (t == 0) {
+    for (int q = 1; q < NT / 64; ++q) {
+      cp += sums[0][q];
+      c += sums[1][q];
+    }
+    // (without a choice p is 0 or, of rows that hold a NaN alone, NaN)
+    const double all = c * (double)rows;
+    *a.loss = (float)(a.coef * a.E * (all > 0.0 ? cp / all : cp));
+  }
+}
+
 // counts, their number of rows and the loss from the workgroups' sums, by one workgroup: each
 // thread adds those of every groups-th workgroup for a column, sixteen loads at a time (they come from
 // the other XCDs), the first ones then the sums of a column.
-template <int NT>
-__device__ inline void finish(const RouteArgs& a) {
+__global__ __launch_bounds__(1024) void k_finish(RouteArgs a) {
+  constexpr int NT = 1024;
   __shared__ uint32_t part_c[NT];
-  __shared__ double part_p[NT], sums[2][NT / 64];
+  __shared__ double part_p[NT];
   __shared__ uint32_t rows;
   const int t = threadIdx.x, cols = min(a.E + 1, NT), groups = NT / cols, col = t % cols;
   double cp = 0.0, c = 0.0;
@@ -231,23 +254,7 @@ __device__ inline void finish(const RouteArgs& a) {
     }
     __syncthreads();
   }
-  if (!a.loss) return;
-  cp = slot_sum<64>(cp);
-  c = slot_sum<64>(c);
-  if ((t & 63) == 0) {
-    sums[0][t >> 6] = cp;
-    sums[1][t >> 6] = c;
-  }
-  __syncthreads();
-  if (t == 0) {
-    for (int q = 1; q < NT / 64; ++q) {
-      cp += sums[0][q];
-      c += sums[1][q];
-    }
-    // (without a choice p is 0 or, of rows that hold a NaN alone, NaN)
-    const double all = c * (double)rows;
-    *a.loss = (float)(a.coef * a.E * (all > 0.0 ? cp / all : cp));
-  }
+  if (a.loss) write_loss<NT>(a, cp, c, rows);
 }
 
 template <class T, int NT, int G, int V>
@@ -303,21 +310,24 @@ __global__ __launch_bounds__(NT, NT == kMany && V == 8 ? 8 : 1) void k_route(Rou
     }
   }
   __syncthreads();
+  const bool only = NT == kFew && gridDim.x == 1;  // no other workgroup: its sums are all
+  double cp = 0.0, c = 0.0;
   for (int e = threadIdx.x; e <= a.E; e += NT) {
     float s = 0.f;
     if (a.loss && e < a.E)
 #pragma unroll
       for (int q = 0; q < NT / 64; ++q) s += sums[q][e];
-    a.part[(int64_t)blockIdx.x * (a.E + 1) + e] = RouteArgs::Part{cnt[e], s};
+    if (only) {
+      a.counts[e] = cnt[e];
+      cp += e < a.E ? (double)cnt[e] * (double)s : 0.0;
+      c += e < a.E ? (double)cnt[e] : 0.0;
+    } else {
+      a.part[(int64_t)blockIdx.x * (a.E + 1) + e] = RouteArgs::Part{cnt[e], s};
+    }
   }
   if constexpr (NT == kFew)
-    if (gridDim.x == 1) {  // no other workgroup: its sums are all
-      __syncthreads();
-      finish<NT>(a);
-    }
+    if (only && a.loss) write_loss<NT>(a, cp, c, cnt[a.E]);
 }
-
-__global__ __launch_bounds__(1024) void k_finish(RouteArgs a) { finish<1024>(a); }
 
 template <class T, int NT, int G, int V>
 __global__ __launch_bounds__(NT) void k_route_bwd(RouteArgs a) {
@@ -344,19 +354,38 @@ __global__ __launch_bounds__(NT) void k_route_bwd(RouteArgs a) {
     float z[V], p[V], d[V] = {}, top, inv;
     load_logits(static_cast<const T*>(a.z) + (row ? t : 0) * a.ldz, f, row ? a.E : 0, z);
     softmax<G>(z, p, &top, &inv);
-    float inner = 0.f;  // sum of g w over the chosen
-    if (row && a.dw)
-      for (int i = 0; i < a.k; ++i)
-        if (a.chosen[t * a.k + i] >= 0) inner += a.dw[t * a.k + i] * a.w[t * a.k + i];
-    if (row && a.dw)
-      for (int i = 0; i < a.k; ++i) {
-        const int at = a.chosen[t * a.k + i];
-        if (at < 0 || at >= a.E) continue;
-        const float g = a.dw[t * a.k + i];
-        const float x = a.w[t * a.k + i] * (a.normalize ? g - inner : g);
+    // the chosen ones, four at a time; all lanes of the slot load them
+    float inner = 0.f;  // sum of g w over them
+    int at[4];
+    float g[4], cw[4];
+    auto chosen = [&](int i) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) d[e] += f + e == at ? x : 0.f;
+      for (int j = 0; j < 4; ++j) {
+        const int64_t q = t * a.k + min(i + j, a.k - 1);
+        at[j] = a.chosen[q];
+        g[j] = a.dw[q];
+        cw[j] = a.w[q];
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + j >= a.k || at[j] < 0 || at[j] >= a.E) at[j] = -1;
+    };
+    if (row && a.dw) {
+      for (int i = 0; i < a.k; i += 4) {
+        chosen(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) inner += at[j] >= 0 ? g[j] * cw[j] : 0.f;
+      }
+      for (int i = 0; i < a.k; i += 4) {
+        if (a.k > 4) chosen(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = at[j] >= 0 ? cw[j] * (a.normalize ? g[j] - inner : g[j]) : 0.f;
+#pragma unroll
+          for (int e = 0; e < V; ++e) d[e] += f + e == at[j] ? x : 0.f;
+        }
+      }
+    }
     float mean = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) mean += bal[i] * p[i];
