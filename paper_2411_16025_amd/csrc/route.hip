@@ -90,18 +90,15 @@ __device__ inline float exp_of(float x) {
 template <int G, int V>
 __device__ inline bool softmax(const float (&z)[V], float (&p)[V], float* top, float* inverse) {
   float m = -INFINITY, s = 0.f;
-  bool nan = false;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    m = fmaxf(m, z[i]);
-    nan |= z[i] != z[i];
-  }
+  for (int i = 0; i < V; ++i) m = fmaxf(m, z[i]);
   m = slot_max<G>(m);
   *top = m;
   const bool any = m > -INFINITY;
+  const float from = any ? m : 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    p[i] = any || nan ? exp_of(z[i] - (any ? m : 0.f)) : 0.f;
+    p[i] = exp_of(z[i] - from);
     s += p[i];
   }
   s = slot_sum<G>(s);
@@ -257,10 +254,10 @@ __global__ __launch_bounds__(1024) void k_finish(RouteArgs a) {
   if (a.loss) write_loss<NT>(a, cp, c, rows);
 }
 
-template <class T, int NT, int G, int V>
+// KEPT: choices that a lane keeps, at least k / G.
+template <class T, int NT, int G, int V, int KEPT>
 __global__ __launch_bounds__(NT, NT == kMany && V == 8 ? 8 : 1) void k_route(RouteArgs a) {
   constexpr int kSlots = NT / G;  // rows at a time
-  constexpr int kKept = 64 / G < 8 ? (64 / G > 0 ? 64 / G : 1) : 8;  // choices of a lane: k <= min(64, 8 G)
   __shared__ uint32_t cnt[kMaxExperts + 1];
   __shared__ float sums[NT / 64][G * V];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, in = threadIdx.x % G, f = in * V;
@@ -277,10 +274,10 @@ __global__ __launch_bounds__(NT, NT == kMany && V == 8 ? 8 : 1) void k_route(Rou
     for (int i = 0; i < V; ++i) acc[i] += p[i];
     if (any && in == 0) atomicAdd(&cnt[a.E], 1u);
     Left<T, G, V> left(z, f);
-    int at[kKept];
-    float weight[kKept], sum = 0.f;
+    int at[KEPT];
+    float weight[KEPT], sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < kKept; ++c) {
+    for (int c = 0; c < KEPT; ++c) {
       Choice kept{0, -INFINITY};
       for (int i = 0; i < min(a.k - c * G, G); ++i) {
         const Choice next = left.next(f);
@@ -292,7 +289,7 @@ __global__ __launch_bounds__(NT, NT == kMany && V == 8 ? 8 : 1) void k_route(Rou
     }
     if (a.normalize) sum = slot_sum<G>(sum);
 #pragma unroll
-    for (int c = 0; c < kKept; ++c) {
+    for (int c = 0; c < KEPT; ++c) {
       const int i = c * G + in;
       if (t >= a.n || i >= a.k) continue;
       a.experts[t * a.k + i] = at[c];
@@ -421,8 +418,10 @@ gcn_status launch(const RouteArgs& a, int blocks, hipStream_t s) {
     constexpr int G = decltype(lanes)::value, V = decltype(values)::value;
     if constexpr (BWD)
       hipLaunchKernelGGL((k_route_bwd<T, NT, G, V>), dim3(blocks), dim3(NT), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_route<T, NT, G, V>), dim3(blocks), dim3(NT), 0, s, a);
+    else if (a.k <= G)
+      hipLaunchKernelGGL((k_route<T, NT, G, V, 1>), dim3(blocks), dim3(NT), 0, s, a);
+    else if constexpr (G < 64)  // (k is at most 64, and 8 G)
+      hipLaunchKernelGGL((k_route<T, NT, G, V, (G <= 8 ? 8 : 64 / G)>), dim3(blocks), dim3(NT), 0, s, a);
   };
   std::integral_constant<int, 8> v8;
   switch (route_lanes(a.E)) {
@@ -540,6 +539,6 @@ extern "C" gcn_status gcn_route_bwd(int64_t n, int64_t E, const void* logits, in
   a.ldd = ldd;
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps("route_bwd", s);
-  const int blocks = (int)std::min<int64_t>(2048, ceil_div(n, (int64_t)(kFew / route_lanes(E))));
+  const int blocks = (int)std::min<int64_t>(1024, ceil_div(n, (int64_t)(kFew / route_lanes(E))));
   return launch<true>(a, dtype, blocks, s);
 }
