@@ -34,6 +34,8 @@ struct RouteArgs {
     float p;
   };
   Part* part;
+  double* part_loss;  // three sums of each workgroup of k_finish
+  uint32_t* ticket;
   int blocks;
   double coef;
   int64_t* counts;
@@ -184,74 +186,84 @@ struct Left<bf16, G, V> {
   }
 };
 
-// The loss, from every thread's part of sum_e c_e P_e and of sum_e c_e, and the rows with a choice.
+// Sums over the threads of a workgroup, which thread 0 gets.
 template <int NT>
-__device__ inline void write_loss(const RouteArgs& a, double cp, double c, const uint32_t& rows) {
-  __shared__ double sums[2][NT / 64];
-  const int t = threadIdx.x;
-  cp = slot_sum<64>(cp);
-  c = slot_sum<64>(c);
-  if ((t & 63) == 0) {
-    sums[0][t >> 6] = cp;
-    sums[1][t >> 6] = c;
+__device__ inline void block_sums(double (&v)[3]) {
+  __shared__ double sums[3][NT / 64];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    v[i] = slot_sum<64>(v[i]);
+    if ((threadIdx.x & 63) == 0) sums[i][threadIdx.x >> 6] = v[i];
   }
   __syncthreads();
-  if (t == 0) {
-    for (int q = 1; q < NT / 64; ++q) {
-      cp += sums[0][q];
-      c += sums[1][q];
-    }
-    // (without a choice p is 0 or, of rows that hold a NaN alone, NaN)
-    const double all = c * (double)rows;
-    *a.loss = (float)(a.coef * a.E * (all > 0.0 ? cp / all : cp));
-  }
+  if (threadIdx.x == 0)
+    for (int q = 1; q < NT / 64; ++q)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) v[i] += sums[i][q];
 }
 
-// counts, their number of rows and the loss from the workgroups' sums, by one workgroup: each
-// thread adds those of every groups-th workgroup for a column, sixteen loads at a time (they come from
-// the other XCDs), the first ones then the sums of a column.
-__global__ __launch_bounds__(1024) void k_finish(RouteArgs a) {
-  constexpr int NT = 1024;
-  __shared__ uint32_t part_c[NT];
-  __shared__ double part_p[NT];
-  __shared__ uint32_t rows;
-  const int t = threadIdx.x, cols = min(a.E + 1, NT), groups = NT / cols, col = t % cols;
-  double cp = 0.0, c = 0.0;
-  for (int e = col; e - col <= a.E; e += cols) {
-    uint32_t n = 0;
-    double p = 0.0;
-    if (e <= a.E && t / cols < groups)
-      for (int b = t / cols; b < a.blocks; b += 16 * groups) {
-        RouteArgs::Part v[16];
+// The loss from sum_e c_e P_e, sum_e c_e and the rows with a choice (without one p is 0 or, of rows
+// that hold a NaN alone, NaN).
+__device__ inline void write_loss(const RouteArgs& a, const double (&v)[3]) {
+  const double all = v[1] * v[2];
+  *a.loss = (float)(a.coef * a.E * (all > 0.0 ? v[0] / all : v[0]));
+}
+
+// counts, their number of rows and the loss from the workgroups' sums. A workgroup has 16 experts;
+// its threads add the sums of every 32nd workgroup, sixteen loads at a time (they come from the
+// other XCDs). The last one to end adds up the loss, in the experts' order: the ticket that tells it
+// was set to 0 by the kernel before (by one workgroup alone, 131,072 rows of 64: 9 us).
+constexpr int kCols = 16, kFinish = 512;
+__global__ __launch_bounds__(kFinish) void k_finish(RouteArgs a) {
+  constexpr int kGroups = kFinish / kCols;
+  __shared__ uint32_t part_c[kFinish];
+  __shared__ double part_p[kFinish];
+  const int t = threadIdx.x, e = blockIdx.x * kCols + t % kCols, g = t / kCols;
+  uint32_t n = 0;
+  double p = 0.0;
+  if (e <= a.E)
+    for (int b = g; b < a.blocks; b += 16 * kGroups) {
+      RouteArgs::Part v[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          v[i] = a.part[(int64_t)min(b + i * groups, a.blocks - 1) * (a.E + 1) + e];
+      for (int i = 0; i < 16; ++i)
+        v[i] = a.part[(int64_t)min(b + i * kGroups, a.blocks - 1) * (a.E + 1) + e];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (b + i * groups < a.blocks) {
-            n += v[i].count;
-            p += (double)v[i].p;
-          }
-      }
-    part_c[t] = n;
-    part_p[t] = p;
-    __syncthreads();
-    if (t < cols && e <= a.E) {
-      for (int q = t + cols; q < groups * cols; q += cols) {
-        n += part_c[q];
-        p += part_p[q];
-      }
-      a.counts[e] = n;
-      if (e == a.E) {
-        rows = n;
-      } else {
-        cp += (double)n * p;
-        c += (double)n;
-      }
+      for (int i = 0; i < 16; ++i)
+        if (b + i * kGroups < a.blocks) {
+          n += v[i].count;
+          p += (double)v[i].p;
+        }
     }
-    __syncthreads();
+  part_c[t] = n;
+  part_p[t] = p;
+  __syncthreads();
+  double v[3] = {0.0, 0.0, 0.0};
+  if (t < kCols && e <= a.E) {
+    for (int q = 1; q < kGroups; ++q) {
+      n += part_c[t + q * kCols];
+      p += part_p[t + q * kCols];
+    }
+    a.counts[e] = n;
+    if (e < a.E) {
+      v[0] = (double)n * p;
+      v[1] = (double)n;
+    } else {
+      v[2] = (double)n;
+    }
   }
-  if (a.loss) write_loss<NT>(a, cp, c, rows);
+  if (!a.loss) return;
+  block_sums<kFinish>(v);
+  if (t > 0) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) a.part_loss[3 * blockIdx.x + i] = v[i];
+  __threadfence();
+  if (atomicAdd(a.ticket, 1u) != gridDim.x - 1) return;
+  __threadfence();
+  v[0] = v[1] = v[2] = 0.0;
+  for (uint32_t b = 0; b < gridDim.x; ++b)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] += a.part_loss[3 * b + i];
+  write_loss(a, v);
 }
 
 // KEPT: choices that a lane keeps, at least k / G.
@@ -308,7 +320,8 @@ __global__ __launch_bounds__(NT, NT == kMany && V == 8 ? 8 : 1) void k_route(Rou
   }
   __syncthreads();
   const bool only = NT == kFew && gridDim.x == 1;  // no other workgroup: its sums are all
-  double cp = 0.0, c = 0.0;
+  if (!only && a.loss && blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+  double v[3] = {0.0, 0.0, 0.0};
   for (int e = threadIdx.x; e <= a.E; e += NT) {
     float s = 0.f;
     if (a.loss && e < a.E)
@@ -316,14 +329,18 @@ __global__ __launch_bounds__(NT, NT == kMany && V == 8 ? 8 : 1) void k_route(Rou
       for (int q = 0; q < NT / 64; ++q) s += sums[q][e];
     if (only) {
       a.counts[e] = cnt[e];
-      cp += e < a.E ? (double)cnt[e] * (double)s : 0.0;
-      c += e < a.E ? (double)cnt[e] : 0.0;
+      v[0] += e < a.E ? (double)cnt[e] * (double)s : 0.0;
+      v[1] += e < a.E ? (double)cnt[e] : 0.0;
     } else {
       a.part[(int64_t)blockIdx.x * (a.E + 1) + e] = RouteArgs::Part{cnt[e], s};
     }
   }
   if constexpr (NT == kFew)
-    if (only && a.loss) write_loss<NT>(a, cp, c, cnt[a.E]);
+    if (only && a.loss) {
+      block_sums<NT>(v);
+      v[2] = (double)cnt[a.E];
+      if (threadIdx.x == 0) write_loss(a, v);
+    }
 }
 
 template <class T, int NT, int G, int V>
@@ -497,13 +514,18 @@ extern "C" gcn_status gcn_route_fwd(int64_t n, int64_t E, const void* logits, in
   a.coef = coef;
   a.counts = counts;
   a.loss = loss;
-  a.blocks = route_blocks(n, E, 512);
-  if (a.blocks > 0) GCN_CHECK(scratch.alloc(&a.part, a.blocks * (E + 1), "sums of workgroups"));
+  a.blocks = std::max(1, route_blocks(n, E, 512));  // (no rows: zeros)
+  const int64_t finish = ceil_div(E + 1, (int64_t)kCols);
+  if (a.blocks > 1) {
+    GCN_CHECK(scratch.alloc(&a.part, a.blocks * (E + 1), "sums of workgroups"));
+    GCN_CHECK(scratch.alloc(&a.part_loss, 3 * finish, "sums of the loss"));
+    GCN_CHECK(scratch.alloc(&a.ticket, 1, "a ticket"));
+  }
   if (scratch.asked()) return GCN_OK;
   ProfScope ps("route_fwd", s);
-  if (a.blocks > 0) GCN_CHECK(launch<false>(a, dtype, a.blocks, s));
+  GCN_CHECK(launch<false>(a, dtype, a.blocks, s));
   if (a.blocks == 1) return GCN_OK;
-  hipLaunchKernelGGL(k_finish, dim3(1), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(k_finish, dim3((unsigned)finish), dim3(kFinish), 0, s, a);
   GCN_HIP(hipGetLastError());
   return GCN_OK;
 }

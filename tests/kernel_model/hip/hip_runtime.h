@@ -86,11 +86,10 @@ inline int __clzll(long long v) { return v ? __builtin_clzll((unsigned long long
 
 inline int __popcll(unsigned long long v) { return __builtin_popcountll(v); }
 template <class T>
-T atomicAdd(T* p, T v) {  // (of a workgroup's own memory: threads run one at a time)
-  const T old = *p;
-  *p += v;
-  return old;
+T atomicAdd(T* p, T v) {  // (workgroups run in processes that share the arrays)
+  return __atomic_fetch_add(p, v, __ATOMIC_SEQ_CST);
 }
+inline void __threadfence() { __atomic_thread_fence(__ATOMIC_SEQ_CST); }
 // the lanes of a wavefront do what stands before it before any does what stands behind it
 inline void __builtin_amdgcn_fence(int, const char*) {
   const char c = 0;
