@@ -82,13 +82,16 @@ def check_embed_fwd(e, n, F, V, per=1, kt="f32", ky="f32", pad=0, shift=0, scale
     r = np.random.default_rng(seed)
     T = rounded(r.standard_normal((V, F)), kt)
     ids = some_ids(r, n, V * per, "none")
+    used = np.zeros(V, bool)
+    used[ids[(ids >= 0) & (ids.astype(np.int64) < V * per)] // per] = True
+    T[~used] = np.nan
     t, y = e.rows(T, kt, pad, shift), e.rows(np.full((n, F), 7.0), ky, pad + 1, shift, fill=9.0)
     i = e.put(ids)
     assert e.lib.gcn_embed_fwd(n, F, V, i.ptr, per, t.ptr, t.ld, CODE[kt], scale, y.ptr, y.ld, CODE[ky],
                                e.stream) == 0, e.error()
     real = (ids >= 0) & (ids.astype(np.int64) < V * per)
     at = np.where(real, ids, 0) // per
-    want = rounded(np.where(real[:, None], np.float32(scale) * T[at], np.float32(0)), ky)
+    want = rounded(np.where(real[:, None], np.float32(scale) * np.nan_to_num(T[at]), np.float32(0)), ky)
     got = y.get()
     assert np.array_equal(got, want), (n, F, V, per, kt, ky)
     assert not np.signbit(got[~real]).any()
@@ -100,7 +103,8 @@ def check_embed_bwd(e, n, F, V, how="spread", kd="f32", kt="f32", pad=0, shift=0
     r = np.random.default_rng(seed)
     dY = rounded(r.standard_normal((n, F)), kd)
     ids = some_ids(r, n, V, how)
-    offsets, order, _ = group_ids(ids, V)
+    offsets, order, slots = group_ids(ids, V)
+    dY[slots < 0] = np.nan  # (of no row of the table)
     old = rounded(r.standard_normal((V, F)), kt)
     dy = e.rows(dY, kd, pad, shift)
     dt = e.rows(old if add else np.full((V, F), np.nan), kt, pad + 2, shift, fill=9.0)
@@ -273,13 +277,16 @@ def check_combine(e, n, k, F, rows, kind="f32", weighted=True, pad=0, shift=0, i
     w = r.standard_normal((n, k)).astype(np.float32)
     real = (slot >= 0) & (slot < rows)
     at = np.where(real, slot, 0)
+    used = np.zeros(rows, bool)
+    used[slot[real]] = True
+    Z[~used] = np.nan
     W = np.where(real, w if weighted else 1, 0).astype(np.float64)
     z, y = e.rows(Z, kind, pad, shift), e.rows(np.full((n, F), 7.0), kind, pad + 1, shift, fill=9.0)
     sd, wd = e.put(slot), e.put(w)
     what = (n, k, F, rows, kind, weighted)
     assert e.lib.gcn_combine_fwd(n, k, F, z.ptr, rows, z.ld, CODE[kind], sd.ptr, wd.ptr if weighted else None,
                                  y.ptr, y.ld, e.stream) == 0, e.error()
-    Zk = Z[at] if rows else np.zeros((n, k, F), np.float32)
+    Zk = np.where(real[:, :, None], Z[at], 0) if rows else np.zeros((n, k, F), np.float32)
     terms = W[:, :, None] * Zk
     want, bound = terms.sum(1), (k + 1) * U * np.abs(terms).sum(1)
     bound = bound + HALF[kind] * (np.abs(want) + bound)
@@ -296,7 +303,7 @@ def check_combine(e, n, k, F, rows, kind="f32", weighted=True, pad=0, shift=0, i
     want = Z.copy() if in_place else np.full((rows, F), 5.0, np.float32)
     t, i = np.nonzero(real)
     want[slot[t, i]] = rounded((w[t, i] if weighted else np.ones(len(t), np.float32))[:, None] * dY[t], kind)
-    assert np.array_equal(dz.get(), want), what
+    assert np.array_equal(dz.get(), want, equal_nan=True), what
     terms = np.where(real[:, :, None], Zk.astype(np.float64) * dY[:, None, :], 0)
     # at least 8 lanes share a row: chains of F / 8 + 8, six joins
     bound = (F / 8 + 24) * U * np.abs(terms).sum(2)
@@ -446,3 +453,40 @@ def check_grad8_special(e, rows, K, N, kind="f32", seed=0):
     ok = near | (big & np.isinf(got) & (np.sign(got) == np.sign(want)))
     assert ok[rest, 2:].all(), (what, np.argwhere(~ok[rest, 2:])[:4])
     assert (got[rest, 5] == 0).all() and not np.signbit(got[rest, 5]).any(), what
+
+
+def check_embed_bwd_unordered(e, n, F, V, kd="f32", seed=0):
+    """Offsets and an order of any values: nothing is read or written outside of the arrays."""
+    r = np.random.default_rng(seed)
+    dY = rounded(r.standard_normal((n, F)), kd)
+    offsets = np.where(r.random(V + 1) < 0.8, r.integers(0, n + 1, V + 1), r.integers(-2 ** 62, 2 ** 62, V + 1))
+    order = np.where(r.random(n) < 0.8, r.integers(0, n, n), r.integers(-2 ** 31, 2 ** 31, n))
+    dy, dt = e.rows(dY, kd, 1), e.rows(np.zeros((V, F)), "f32", 1, fill=9.0)
+    o, p = e.put(offsets.astype(np.int64)), e.put(order.astype(np.int32))
+    for memory in (0, 1):
+        Call(e, memory)(e.lib.gcn_embed_bwd, n, F, V, o.ptr, p.ptr, dy.ptr, dy.ld, CODE[kd], 1.0, dt.ptr, dt.ld, 0, 0)
+    dt.check_margins()
+
+
+def check_grad8_unordered(e, G, rows, K, N, kind="f32", seed=0):
+    r = np.random.default_rng(seed)
+    offsets = np.where(r.random(G + 1) < 0.8, r.integers(0, rows + 1, G + 1), r.integers(-2 ** 62, 2 ** 62, G + 1))
+    q, s = pack8(r.standard_normal((rows, K)))
+    qd, sd = e.rows(q, "i8", 0), e.rows(s, "u8", 0)
+    bd, c = e.rows(rounded(r.standard_normal((rows, N)), kind), kind, 0), e.rows(np.zeros((G * K, N)), "f32", 0)
+    o = e.put(offsets.astype(np.int64))
+    for memory in (0, 1):
+        Call(e, memory)(e.lib.gcn_gemm_grouped_q8, G, o.ptr, rows, N, K, qd.ptr, qd.ld, sd.ptr, sd.ld, bd.ptr, bd.ld,
+                        CODE[kind], c.ptr, c.ld, K * c.ld)
+
+
+def check_route_bwd_any(e, n, E, k, kind="f32", seed=0):
+    """Experts of any values: nothing is read or written outside of the arrays."""
+    r = np.random.default_rng(seed)
+    z = e.rows(rounded(r.standard_normal((n, E)), kind), kind, 1)
+    ex = e.put(r.integers(-2 ** 31, 2 ** 31, (n, k)).astype(np.int32) >> r.integers(0, 31, (n, k)).astype(np.int32))
+    w, c = e.put(r.random((n, k)).astype(np.float32)), e.put(r.integers(0, 9, E + 1))
+    dz = e.rows(np.zeros((n, E)), kind, 1, fill=9.0)
+    assert e.lib.gcn_route_bwd(n, E, z.ptr, z.ld, CODE[kind], k, 1, ex.ptr, w.ptr, c.ptr, 1.0, w.ptr, None, dz.ptr,
+                               dz.ld, e.stream) == 0
+    dz.check_margins()

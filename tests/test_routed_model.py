@@ -138,3 +138,17 @@ def test_grad8(model):
 def test_grad8_special(model):
     model([["check_grad8_special", [rows, K, N], dict(kind=kind, seed=K)] for kind in ("f32", "bf16")
            for rows, K, N in ((40, 64, 8), (100, 150, 20), (300, 260, 264), (9, 40, 7))])
+
+
+def test_any_plan(model):
+    """Offsets, orders and experts that no call gives: no address leaves the arrays."""
+    cases = []
+    for seed in range(12):
+        kind = ("f32", "bf16")[seed & 1]
+        cases.append(["check_embed_bwd_unordered", [40 + 70 * seed, 3 + 11 * seed, 1 + 9 * seed],
+                      dict(kd=kind, seed=seed)])
+        cases.append(["check_grad8_unordered", [1 + 3 * seed, 30 + 90 * seed, 8 + 12 * seed, 5 + 9 * seed],
+                      dict(kind=kind, seed=seed)])
+        cases.append(["check_route_bwd_any", [20, 2 + 9 * seed, 1 + seed % 2], dict(kind=kind, seed=seed)])
+    cases.append(["check_grad8_unordered", [1040, 600, 20, 9], dict(kind="bf16", seed=3)])
+    model(cases)
