@@ -95,6 +95,7 @@ struct SumArgs {
   void* dt;
   int64_t lddt;
   bool add;
+  bool zeroed;          // dT is 0
   uint32_t parts;       // places / chunk
   int32_t* owner;       // [parts]
   float* part;          // [parts][ldp]
@@ -140,11 +141,27 @@ __device__ inline void write_piece(const SumArgs& a, int64_t row, int f, float (
   store_raw(to, f, (int)a.F, v);
 }
 
-// A workgroup has up to kRows rows, or a part of a long one, in pieces of 16 bytes of dT. Most rows of
-// a large table have no place, and writing their zeros bounds the pass: they are written first,
-// without a look at anything but the offsets in LDS; then the rows that have some, which were
-// listed, so that all lanes gather (2,449,029 x 100 fp32, 250,000 places: 318 us where each piece
-// looked for its row's places, 245 so; with stores past the caches 282, and rows of 47 258 instead of 128).
+// Zeros over `bytes` bytes from an element's address on: in pieces of 16 bytes where memory has them.
+constexpr int kZeroEach = 8;
+__global__ __launch_bounds__(kThreads) void k_zero(char* p, int64_t bytes) {
+  const int64_t head = std::min<int64_t>(-(int64_t)reinterpret_cast<uintptr_t>(p) & 15, bytes);
+  const int64_t pieces = (bytes - head) / 16, tail = head + 16 * pieces;
+  const int64_t at = (int64_t)blockIdx.x * (kThreads * kZeroEach) + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kZeroEach; ++i)
+    if (at + i * kThreads < pieces)
+      reinterpret_cast<u4*>(p + head)[at + i * kThreads] = u4{0, 0, 0, 0};
+  if (blockIdx.x == 0 && threadIdx.x < 16) {  // (elements: 2 or 4 bytes)
+    if (2 * (int)threadIdx.x < head) *reinterpret_cast<uint16_t*>(p + 2 * threadIdx.x) = 0;
+    if (tail + 2 * threadIdx.x < bytes) *reinterpret_cast<uint16_t*>(p + tail + 2 * threadIdx.x) = 0;
+  }
+}
+
+// A workgroup has up to kRows rows, or a part of a long one, in pieces of 16 bytes of dT. Rows without
+// a place, most of a large table's, are zeros, which bound the pass; those that have some are listed, so
+// that all lanes gather. A large table whose rows lie beside each other is zeroed by a launch before,
+// which knows nothing of rows and writes at 6.8 TB/s (2,449,029 x 100 fp32, 250,000 places: 318 us where
+// each piece looked for its row's places, 245 with the zeros of a workgroup's rows written first, .. so).
 constexpr int kRows = 1024;
 
 template <class T, class TT, int kRowTile>
@@ -181,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void k_sum_rows(SumArgs a) {
       longs = l;
     }
   }
-  if (!a.add) {
+  if (!a.add && !a.zeroed) {
     const float zero[N] = {};
     for (uint32_t q = threadIdx.x; q < rows * pieces; q += kThreads) {
       const uint32_t r = pieces == 1 ? q : (rows > 1 ? (uint32_t)((uint64_t)q * t.magic >> 32) : 0);
@@ -309,6 +326,9 @@ gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
   const bool sparse = a.by.n > 4 * a.by.rows;
   a.tiles = row_tiles(a.by.n, ceil_div((int64_t)a.F, (int64_t)kPiece<TT>), sparse ? 4096 : 1024);
   a.tiles.rows = std::min<uint32_t>(a.tiles.rows, kRows);
+  a.zeroed = a.by.n > 32 * a.by.rows && !a.add && a.lddt == a.F;
+  if (a.zeroed && a.tiles.parts == 1)  // more rows, of which few are listed
+    a.tiles.rows = std::min(512u, std::max(1u, 16384 / a.tiles.pieces));
   a.shift = a.by.rows <= (1 << 18) ? 5 : 7;
   GCN_CHECK(launch_fits(a.tiles.blocks(), kThreads));
   a.parts = (uint32_t)(a.by.rows >> a.shift);
@@ -320,6 +340,14 @@ gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
   if (scratch->asked()) return GCN_OK;
   ProfScope ps("embed_bwd", s);
   const dim3 rows((unsigned)a.tiles.blocks());
+  const int64_t bytes = (int64_t)a.by.n * a.F * (int64_t)sizeof(TT);
+  if (a.zeroed) {
+    const int64_t blocks = ceil_div(bytes, (int64_t)16 * kThreads * kZeroEach);
+    GCN_CHECK(launch_fits(blocks, kThreads));
+    hipLaunchKernelGGL(k_zero, dim3((unsigned)blocks), dim3(kThreads), 0, s, static_cast<char*>(a.dt),
+                       bytes);
+    GCN_HIP(hipGetLastError());
+  }
   if (sparse)
     hipLaunchKernelGGL((k_sum_rows<T, TT, 4096>), rows, dim3(kThreads), 0, s, a);
   else

@@ -106,7 +106,7 @@ def check_embed_bwd(e, n, F, V, how="spread", kd="f32", kt="f32", pad=0, shift=0
     offsets, order, slots = group_ids(ids, V)
     dY[slots < 0] = np.nan  # (of no row of the table)
     old = rounded(r.standard_normal((V, F)), kt)
-    dy = e.rows(dY, kd, pad, shift)
+    dy = e.rows(dY, kd, max(pad, 0), shift)
     dt = e.rows(old if add else np.full((V, F), np.nan), kt, pad + 2, shift, fill=9.0)
     o, p = e.put(offsets.astype(np.int64)), e.put(order.astype(np.int32))
     Call(e, memory)(e.lib.gcn_embed_bwd, n, F, V, o.ptr, p.ptr, dy.ptr, dy.ld, CODE[kd], scale, dt.ptr,

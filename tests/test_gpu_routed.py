@@ -149,6 +149,14 @@ def test_embed_bwd(E, n, F, V, how, kd, kt):
             seed=n + F)
 
 
+@pytest.mark.parametrize("kt", KINDS)
+@pytest.mark.parametrize("n,F,V", [(30, 7, 3000), (5, 100, 900), (40, 3, 2001), (1, 1, 9), (500, 47, 30000)])
+def test_embed_bwd_sparse(E, n, F, V, kt):
+    """Most rows without a place, rows of dT beside each other, from an address of any element."""
+    for shift in (0, 1, 3):
+        run(E, "check_embed_bwd", n, F, V, how="skew", kt=kt, pad=-2, shift=shift, seed=n + F)
+
+
 # ---- the router --------------------------------------------------------------------
 
 ROUTES = [(1, 1, 1), (3, 2, 2), (70, 8, 3), (65, 9, 8), (500, 16, 2), (33, 47, 5), (400, 64, 8), (90, 100, 64),

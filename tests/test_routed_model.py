@@ -84,8 +84,11 @@ def test_embed_bwd(model):
             cases.append(["check_embed_bwd", [n, F, V], dict(how=("spread", "skew", "one", "none")[i], kd=kd, kt=kt,
                                                              pad=(0, 3, 8, 1)[i], add=bool(i & 1),
                                                              memory=i >> 1, seed=n + F)])
-    # a large table, pieces of four rows to a thread
-    cases.append(["check_embed_bwd", [60, 1, 530000], dict(how="skew", seed=1)])
+    # large tables, with rows beside each other (zeroed as one) and apart
+    for i, (n, F, V, pad) in enumerate(((60, 1, 530000, 0), (30, 7, 3000, -2), (5, 100, 900, -2), (40, 3, 1001, -2),
+                                        (1, 1, 9, -2), (2, 33, 1000, 0))):
+        for kt in ("f32", "bf16"):
+            cases.append(["check_embed_bwd", [n, F, V], dict(how="skew", kt=kt, pad=pad, seed=i)])
     model(cases)
 
 
