@@ -165,69 +165,6 @@ struct CodeLoader {
   }
 };
 
-// BK rows of X columns of fp32, split into three tiles: pieces of 8, read as two of 4 (as
-// Loader's: from before a row's end, and moved down).
-template <int X, int BK, int NT>
-struct PartLoader {
-  using T = Tile<false, X, BK>;
-  static constexpr int kCount = T::kPieces / NT, kPerLine = T::kPerLine;
-  static_assert(T::kPieces % NT == 0, "every thread has as many pieces");
-  const float* base;
-  int64_t ld;
-  int have;
-  int64_t had;
-  u4 v[kCount][2];
-
-  __device__ static inline int line_of(int p) { return (int)(threadIdx.x + p * NT) / kPerLine; }
-  __device__ static inline int element_of(int p) { return 8 * ((int)(threadIdx.x + p * NT) % kPerLine); }
-  __device__ inline void init(const float* b, int64_t ld_, int have_) {
-    base = b;
-    ld = ld_;
-    have = have_;
-  }
-  __device__ inline void load(char*, int64_t k0, int64_t left) {
-    had = left;
-    if (left <= 0) return;  // past the last stage
-#pragma unroll
-    for (int p = 0; p < kCount; ++p) {
-      const float* row = base + (k0 + std::min<int64_t>(line_of(p), left - 1)) * ld;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        v[p][i] = *reinterpret_cast<const Unaligned<float>::type*>(
-            row + std::min(element_of(p) + 4 * i, have - 4));
-    }
-  }
-  __device__ inline void store(char* lds_to) {
-#pragma unroll
-    for (int p = 0; p < kCount; ++p) {
-      const int line = line_of(p), e = element_of(p);
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        u4 r = v[p][i];
-        if (have < X) r = move_down<float>(r, std::min(4, std::max(0, e + 4 * i + 4 - have)));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[4 * i + j] = line < had ? __uint_as_float(r[j]) * kUp : 0.f;
-      }
-      u4 parts[3];
-      split8(x, parts);
-      char* to = lds_to + line * (X * 2) + ((e / 8) ^ T::swz(line)) * 16;
-#pragma unroll
-      for (int i = 0; i < 3; ++i) *reinterpret_cast<u4*>(to + i * T::kBytes) = parts[i];
-    }
-  }
-};
-
-// bf16 rows: as in gemm_grouped.hip.
-template <class TB, int X, int BK, int NT>
-struct RowLoader : Loader<false, X, BK, NT, false> {
-  static constexpr int kParts = 1;
-};
-template <int X, int BK, int NT>
-struct RowLoader<float, X, BK, NT> : PartLoader<X, BK, NT> {
-  static constexpr int kParts = 3;
-};
-
 // A workgroup's part of C and its chunk of a group's rows.
 struct Place {
   bool any, whole;  // whether there is one; whether the chunk is the whole group
@@ -338,16 +275,15 @@ __device__ inline void write_sums(const Q8Args& a, const Place& pl, int m0, int 
 }
 
 // A workgroup of WR x WC wavefronts, RB x CB blocks of 32 x 32 of C each.
-template <class TB, int BK, int WR, int WC, int RB, int CB>
+// bf16 rows of any alignment.
+template <int BK, int WR, int WC, int RB, int CB>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
   constexpr int NT = 64 * WR * WC, BM = 32 * WR * RB, BN = 32 * WC * CB;
   using LA = CodeLoader<BM, BK, NT>;
-  using LB = RowLoader<TB, BN, BK, NT>;
+  using LB = Loader<false, BN, BK, NT, false>;
   using TA = Tile<false, BM, BK>;
   using TN = Tile<false, BN, BK>;
-  constexpr int NP = LB::kParts;
-  __shared__ __align__(16) char a0[TA::kBytes], a1[TA::kBytes], b0[NP * TN::kBytes],
-      b1[NP * TN::kBytes];
+  __shared__ __align__(16) char a0[TA::kBytes], a1[TA::kBytes], b0[TN::kBytes], b1[TN::kBytes];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = w / WC, wc = w % WC;
   const Place pl = place(a, BM, BN);
@@ -357,7 +293,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
   LA la;
   LB lb;
   la.init(a.q + m0, a.ldq, a.s + m0 / 32, a.lds, a.K - m0);
-  lb.init(static_cast<const TB*>(a.b) + n0, a.ldb, a.N - n0);
+  lb.init(static_cast<const bf16*>(a.b) + n0, a.ldb, a.N - n0);
   // (the matrix core's rounding has one sign: every other chunk's sums are of negated products)
   const uint32_t sign = pl.chunk & 1 ? 0x80000000u : 0;
 
@@ -373,25 +309,20 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
   // stage too (gemm_grouped.hip).
   constexpr int STEPS = BK / 16;
   static_assert(STEPS % 2 == 0, "the fragments' buffers alternate over the stages");
-  bf8 fa[2][RB], fb[2][CB][NP];
+  bf8 fa[2][RB], fb[2][CB];
   auto read = [&](int to, int step, const char* ca, const char* cb) {
 #pragma unroll
     for (int i = 0; i < RB; ++i) fa[to][i] = TA::read(ca, wr * RB + i, step, lane);
 #pragma unroll
-    for (int j = 0; j < CB; ++j)
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-        fb[to][j][p] = TN::read(cb + p * TN::kBytes, wc * CB + j, step, lane);
+    for (int j = 0; j < CB; ++j) fb[to][j] = TN::read(cb, wc * CB + j, step, lane);
   };
   auto multiply = [&](int from) {
 #pragma unroll
-    for (int p = NP - 1; p >= 0; --p)  // the small parts first
+    for (int i = 0; i < RB; ++i)
 #pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int j = 0; j < CB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[from][i], fb[from][j][p],
-                                                              acc[i][j], 0, 0, 0);
+      for (int j = 0; j < CB; ++j)
+        acc[i][j] =
+            __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[from][i], fb[from][j], acc[i][j], 0, 0, 0);
   };
   const int64_t stages = (k_end - k_beg + BK - 1) / BK;
   auto load = [&](int64_t s, char* to) {
@@ -430,33 +361,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
     wait_loads();  // those past the last stage
   }
 
-  float down = NP == 3 ? 1.f / kUp : 1.f;
-  if (pl.chunk & 1) down = -down;
-  if constexpr (NP == 3) {
-    if (not_finite<RB, CB>(acc)) {
-      down = 1.f;
-      auto again = [&](int64_t k, float (*x)[4], float (*y)[4]) {
-#pragma unroll
-        for (int i = 0; i < RB; ++i) {
-          const int m = std::min(m0 + (wr * RB + i) * 32 + (lane & 31), a.K - 1);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            x[i][j] = k + j < k_end ? scale_of(a.s[(k + j) * a.lds + m / 32]) *
-                                          (float)a.q[(k + j) * a.ldq + m]
-                                    : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < CB; ++i) {
-          const int n = std::min(n0 + (wc * CB + i) * 32 + (lane & 31), a.N - 1);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            y[i][j] = k + j < k_end ? static_cast<const float*>(a.b)[(k + j) * a.ldb + n] : 0.f;
-        }
-      };
-      mul_again<RB, CB>(k_beg, k_end, again, acc);
-    }
-  }
-  write_sums<RB, CB>(a, pl, m0 + wr * RB * 32, n0 + wc * CB * 32, acc, down);
+  write_sums<RB, CB>(a, pl, m0 + wr * RB * 32, n0 + wc * CB * 32, acc, pl.chunk & 1 ? -1.f : 1.f);
 }
 
 // bf16 rows that start on 16 bytes and hold whole pieces. The codes' way to LDS is through
@@ -611,6 +516,194 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8_direct(Q8Args a) {
   write_sums<RB, CB>(a, pl, m0 + wr * RB * 32, n0 + wc * CB * 32, acc, pl.chunk & 1 ? -1.f : 1.f);
 }
 
+// fp32 rows, split into three parts on their way to LDS (8 to 9 vector instructions an element), three
+// products of a code's value and a part. Rows of 32 a stage; the codes and rows of stage s + 1 are in
+// registers when stage s begins, are decoded and split between its products, and the loads of
+// stage s + 3 follow in the same registers. ODD: rows that do not end with a unit of 8 codes, or with 4
+// columns.
+template <bool ODD, int WR, int WC, int RB, int CB>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8_parts(Q8Args a) {
+  constexpr int BK = 32, NT = 64 * WR * WC, BM = 32 * WR * RB, BN = 32 * WC * CB;
+  using TA = Tile<false, BM, BK>;
+  using TN = Tile<false, BN, BK>;
+  constexpr int UA = BM * BK / 8 / NT, PB = BN * BK / 8 / NT;  // units of 8 codes, pieces of 8 columns
+  constexpr int LA = NT / (BM / 8), LB = NT / (BN / 8);        // rows between a thread's
+  static_assert(BM * BK / 8 % NT == 0 && BN * BK / 8 % NT == 0 && LA % 4 == 0 && LB % 4 == 0,
+                "every thread has as many, in the same columns and places in their lines");
+  __shared__ __align__(16) char a0[TA::kBytes], a1[TA::kBytes], b0[3 * TN::kBytes], b1[3 * TN::kBytes];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = w / WC, wc = w % WC;
+  const Place pl = place(a, BM, BN);
+  if (!pl.any) return;
+  const int m0 = pl.m0, n0 = pl.n0;
+
+  const int line_a = threadIdx.x / (BM / 8), line_b = threadIdx.x / (BN / 8);
+  const int e_a = 8 * (threadIdx.x % (BM / 8)), have_a = a.K - m0;
+  const int e_b = 8 * (threadIdx.x % (BN / 8)), have_b = a.N - n0;
+  // (from 8 codes, or 4 columns, before the tile on, where one at a row's end may begin)
+  const uint32_t qo = line_a * (uint32_t)a.ldq + (uint32_t)(std::min(e_a, have_a - 8) + 8);
+  const uint32_t so = line_a * (uint32_t)a.lds + (uint32_t)std::min(e_a, have_a - 1) / 32;
+  const uint32_t bo0 = 4 * (line_b * (uint32_t)a.ldb + (uint32_t)(std::min(e_b, have_b - 4) + 4));
+  const uint32_t bo1 = 4 * (line_b * (uint32_t)a.ldb + (uint32_t)(std::min(e_b + 4, have_b - 4) + 4));
+  const uint32_t ao = line_a * (BM * 2) + ((e_a / 8) ^ TA::swz(line_a)) * 16;
+  const uint32_t to_b = line_b * (BN * 2) + ((e_b / 8) ^ TN::swz(line_b)) * 16;
+  const int down_a = std::min(8, std::max(0, e_a + 8 - have_a));
+  const int8_t* q = a.q + pl.beg * a.ldq + m0 - 8;
+  const uint8_t* sc = a.s + pl.beg * a.lds + m0 / 32;
+  const float* b = static_cast<const float*>(a.b) + pl.beg * a.ldb + n0 - 4;
+  const int rows = (int)(pl.end - pl.beg), stages = (rows + BK - 1) / BK;
+  const uint32_t sign = pl.chunk & 1 ? 0x80000000u : 0;
+
+  f16 acc[RB][CB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  struct Raw {
+    u2b code[UA];
+    uint32_t scale[UA];
+    u4 v[PB][2];
+  } r0, r1;
+  // unit or piece p of a stage (in the last one of the rows that there are)
+  auto load_a = [&](Raw& r, int s, int p) {
+    s = std::min(s, stages - 1);
+    const int over = s * BK + BK - rows;  // rows past the chunk's end
+    const uint32_t on = p * LA - std::max(0, line_a + p * LA + over - (BK - 1));
+    const int8_t* qs = q + (int64_t)(s * BK) * a.ldq;
+    const uint8_t* ss = sc + (int64_t)(s * BK) * a.lds;
+    r.code[p] = *reinterpret_cast<const u2b*>(qs + (uint32_t)(qo + on * (uint32_t)a.ldq));
+    r.scale[p] = ss[(uint32_t)(so + on * (uint32_t)a.lds)];
+  };
+  auto load_b = [&](Raw& r, int s, int p) {
+    s = std::min(s, stages - 1);
+    const int over = s * BK + BK - rows;
+    const uint32_t on = 4 * (p * LB - std::max(0, line_b + p * LB + over - (BK - 1))) * (uint32_t)a.ldb;
+    const char* bs = reinterpret_cast<const char*>(b + (int64_t)(s * BK) * a.ldb);
+    r.v[p][0] = *reinterpret_cast<const Unaligned<float>::type*>(bs + (uint32_t)(bo0 + on));
+    r.v[p][1] = *reinterpret_cast<const Unaligned<float>::type*>(bs + (uint32_t)(bo1 + on));
+  };
+  auto decode = [&](char* to, const Raw& r, int s, int p) {
+    uint64_t c = r.code[p][0] | (uint64_t)r.code[p][1] << 32;
+    if constexpr (ODD) c = down_a < 8 ? c >> 8 * down_a : 0;
+    const float unit =
+        line_a + p * LA + s * BK < rows ? __uint_as_float(r.scale[p] << 23 ^ sign) : 0.f;
+    *reinterpret_cast<u4*>(to + (ao + p * LA * BM * 2)) =
+        decode8((uint32_t)c, (uint32_t)(c >> 32), unit);
+  };
+  auto split = [&](char* to, const Raw& r, int s, int p) {
+    const bool in = line_b + p * LB + s * BK < rows;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      u4 v = r.v[p][i];
+      if constexpr (ODD) v = move_down<float>(v, std::min(4, std::max(0, e_b + 4 * i + 4 - have_b)));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[4 * i + j] = in ? __uint_as_float(v[j]) * kUp : 0.f;
+    }
+    u4 parts[3];
+    split8(x, parts);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      *reinterpret_cast<u4*>(to + (to_b + p * LB * BN * 2 + i * TN::kBytes)) = parts[i];
+  };
+  bf8 fa[2][RB], fb[2][CB][3];
+  auto read = [&](int step, const char* ca, const char* cb) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i) fa[step][i] = TA::read(ca, wr * RB + i, step, lane);
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+        fb[step][j][p] = TN::read(cb + p * TN::kBytes, wc * CB + j, step, lane);
+  };
+  auto multiply = [&](int step) {
+#pragma unroll
+    for (int p = 2; p >= 0; --p)  // the small parts first
+#pragma unroll
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[step][i], fb[step][j][p],
+                                                              acc[i][j], 0, 0, 0);
+  };
+  // Stage s, whose first fragments are read, in (ca, cb): stage s + 1 goes from r to (na, nb).
+  constexpr int MULS = 3 * RB * CB;
+  auto stage = [&](int s, char* ca, char* cb, char* na, char* nb, Raw& r) {
+    read(1, ca, cb);
+#pragma unroll
+    for (int p = 0; p < UA; ++p) {
+      decode(na, r, s + 1, p);
+      load_a(r, s + 3, p);
+    }
+#pragma unroll
+    for (int p = 0; p < PB; ++p) {
+      split(nb, r, s + 1, p);
+      load_b(r, s + 3, p);
+    }
+    multiply(0);
+    multiply(1);
+#pragma unroll
+    for (int p = 0; p < 2 * MULS; ++p) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 8, 0);
+    }
+    __syncthreads();
+    read(0, na, nb);
+  };
+  if (stages > 0) {
+    auto load = [&](Raw& r, int s) {
+#pragma unroll
+      for (int p = 0; p < UA; ++p) load_a(r, s, p);
+#pragma unroll
+      for (int p = 0; p < PB; ++p) load_b(r, s, p);
+    };
+    load(r0, 0);
+    load(r1, 1);
+#pragma unroll
+    for (int p = 0; p < UA; ++p) decode(a0, r0, 0, p);
+#pragma unroll
+    for (int p = 0; p < PB; ++p) split(b0, r0, 0, p);
+    load(r0, 2);
+    __syncthreads();
+    read(0, a0, b0);
+    for (int s = 0; s < stages; s += 2) {
+      stage(s, a0, b0, a1, b1, r1);
+      if (s + 1 >= stages) break;
+      stage(s + 1, a1, b1, a0, b0, r0);
+    }
+  }
+
+  const int wm = m0 + wr * RB * 32, wn = n0 + wc * CB * 32;
+  float down = pl.chunk & 1 ? -1.f / kUp : 1.f / kUp;
+  if (not_finite<RB, CB>(acc)) {
+    down = 1.f;
+    auto again = [&](int64_t k, float (*x)[4], float (*y)[4]) {
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        const int m = std::min(wm + i * 32 + (lane & 31), a.K - 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[i][j] = k + j < pl.end ? scale_of(a.s[(k + j) * a.lds + m / 32]) *
+                                         (float)a.q[(k + j) * a.ldq + m]
+                                   : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < CB; ++i) {
+        const int n = std::min(wn + i * 32 + (lane & 31), a.N - 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          y[i][j] = k + j < pl.end ? static_cast<const float*>(a.b)[(k + j) * a.ldb + n] : 0.f;
+      }
+    };
+    mul_again<RB, CB>(pl.beg, pl.end, again, acc);
+  }
+  write_sums<RB, CB>(a, pl, wm, wn, acc, down);
+}
+
 template <int WR, int WC, int RB, int CB, class Kernel>
 gcn_status launch(Kernel kernel, Q8Args a, hipStream_t s) {
   constexpr int BM = 32 * WR * RB, BN = 32 * WC * CB;
@@ -639,10 +732,12 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   // chunks as gemm_grouped.hip's
   const bool direct = dtype == GCN_DT_BF16 && reinterpret_cast<uintptr_t>(a.b) % 16 == 0 &&
                       a.ldb % 8 == 0 && N % 8 == 0;
+  const bool f32 = dtype == GCN_DT_F32;
   const bool wide = N > 128 && K > 128 && rows / a.by.n >= 192 && direct;
-  const int64_t tm = wide ? 256 : 128, tn = wide ? 256 : dtype == GCN_DT_F32 && N > 128 ? 256 : 128;
+  const int64_t tm = wide ? 256 : f32 && K <= 64 ? 64 : 128;
+  const int64_t tn = wide ? 256 : !f32 ? 128 : N <= 64 ? 64 : tm == 64 ? 128 : (N - 1) % 256 < 128 ? 128 : 256;
   const int64_t tiles = ceil_div(K, tm) * ceil_div(N, tn);
-  const int64_t want = wide || tn == 256 ? 240 : 480;
+  const int64_t want = tn == 256 ? 240 : 480;
   const double even = (double)rows * (double)tiles / (double)want;
   const double sums = std::sqrt(2e-4 * (double)rows * (double)K * (double)N);
   const double chunk = std::min(
@@ -652,10 +747,21 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * K * N, "grouped GEMM partials"));
   if (scratch->asked()) return GCN_OK;
   ProfScope ps("grouped_q8", s);
-  const bool odd = K % 16 != 0;
-  if (dtype == GCN_DT_F32)
-    GCN_CHECK((tn == 256 ? launch<2, 4, 2, 2>(k_mul8<float, 32, 2, 4, 2, 2>, a, s)
-                         : launch<2, 2, 2, 2>(k_mul8<float, 32, 2, 2, 2, 2>, a, s)));
+  const bool odd = K % (f32 ? 8 : 16) != 0 || (f32 && N % 4 != 0);
+  auto parts_of = [&](auto waves_r, auto waves_c, auto blocks_r, auto blocks_c) {
+    constexpr int WR = decltype(waves_r)::value, WC = decltype(waves_c)::value;
+    constexpr int RB = decltype(blocks_r)::value, CB = decltype(blocks_c)::value;
+    return odd ? launch<WR, WC, RB, CB>(k_mul8_parts<true, WR, WC, RB, CB>, a, s)
+               : launch<WR, WC, RB, CB>(k_mul8_parts<false, WR, WC, RB, CB>, a, s);
+  };
+  std::integral_constant<int, 1> n1;
+  std::integral_constant<int, 2> n2;
+  std::integral_constant<int, 4> n4;
+  if (f32)
+    GCN_CHECK(tm == 64 ? (tn == 64 ? parts_of(n2, n2, n1, n1) : parts_of(n2, n2, n1, n2))
+              : tn == 64 ? parts_of(n2, n2, n2, n1)
+              : tn == 128 ? parts_of(n2, n2, n2, n2)
+                          : parts_of(n2, n4, n2, n2));
   else if (wide)
     GCN_CHECK((odd ? launch<4, 2, 2, 4>(k_mul8_direct<true, 64, 4, 2, 2, 4>, a, s)
                    : launch<4, 2, 2, 4>(k_mul8_direct<false, 64, 4, 2, 2, 4>, a, s)));
@@ -663,7 +769,7 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
     GCN_CHECK((odd ? launch<2, 2, 2, 2>(k_mul8_direct<true, 64, 2, 2, 2, 2>, a, s)
                    : launch<2, 2, 2, 2>(k_mul8_direct<false, 64, 2, 2, 2, 2>, a, s)));
   else
-    GCN_CHECK((launch<2, 2, 2, 2>(k_mul8<bf16, 64, 2, 2, 2, 2>, a, s)));
+    GCN_CHECK((launch<2, 2, 2, 2>(k_mul8<64, 2, 2, 2, 2>, a, s)));
   return parts > 0 ? sum_group_partials(a.by, a.split, K, N, a.part, a.c, a.ldc, a.stride_c, s)
                    : GCN_OK;
 }
