@@ -27,7 +27,9 @@ struct Q8Args {
   float* part;    // of the others here
   int col_tiles, row_tiles;
   uint32_t slots;
-  bool by_chunk;  // each chunk's tiles on one XCD
+  bool by_chunk;  // each chunk's tiles on one XCD; else every XCD has a rectangle of them,
+  int across;     // so many beside each other, of rect_rows x rect_cols (across 0: an eighth of them in a row)
+  int rect_rows, rect_cols;
 };
 
 // The general kernel: 64 x 64 of C per workgroup, fp32 products, any size.
@@ -209,8 +211,16 @@ __device__ inline Place place(const Q8Args& a, int BM, int BN) {
   if (!a.by_chunk) {
     slot = (blockIdx.x >> 3) / share;
     const uint32_t x = (xcd + slot) & 7;  // (which XCD has one tile less than others changes)
-    t = per * x / 8 + (blockIdx.x >> 3) % share;
-    if (t >= per * (x + 1) / 8) return r;
+    const uint32_t in = (blockIdx.x >> 3) % share;
+    if (a.across > 0) {
+      const int row = (int)x / a.across * a.rect_rows + (int)in / a.rect_cols;
+      const int col = (int)x % a.across * a.rect_cols + (int)in % a.rect_cols;
+      if (row >= a.row_tiles || col >= a.col_tiles) return r;
+      t = row * a.col_tiles + col;
+    } else {
+      t = per * x / 8 + in;
+      if (t >= per * (x + 1) / 8) return r;
+    }
   } else {
     const uint32_t turn = blockIdx.x / (8 * per);  // there and back, as the chunks get shorter
     slot = turn * 8 + (turn & 1 ? 7 - xcd : xcd);
@@ -705,13 +715,24 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8_parts(Q8Args a) {
 }
 
 template <int WR, int WC, int RB, int CB, class Kernel>
-gcn_status launch(Kernel kernel, Q8Args a, hipStream_t s) {
+gcn_status launch(Kernel kernel, Q8Args a, int b_bytes, hipStream_t s) {
   constexpr int BM = 32 * WR * RB, BN = 32 * WC * CB;
   a.col_tiles = (int)ceil_div((int64_t)a.N, (int64_t)BN);
   a.row_tiles = (int)ceil_div((int64_t)a.K, (int64_t)BM);
   const int64_t slots = group_slots(a.by, a.split);
   const int64_t per = (int64_t)a.col_tiles * a.row_tiles;
   a.by_chunk = per < 8 || slots >= 32;
+  // rectangles of which the XCDs read the fewest bytes, where they divide the tiles as evenly
+  int64_t least = 0;
+  for (int across = 1; across <= 8; across *= 2) {
+    const int64_t rr = ceil_div(a.row_tiles, 8 / across), rc = ceil_div(a.col_tiles, across);
+    const int64_t bytes = rr * BM + rc * BN * b_bytes;
+    if (rr * rc > ceil_div(per, (int64_t)8) || (a.across > 0 && bytes >= least)) continue;
+    least = bytes;
+    a.across = across;
+    a.rect_rows = (int)rr;
+    a.rect_cols = (int)rc;
+  }
   const int64_t blocks =
       8 * (a.by_chunk ? ceil_div(slots, (int64_t)8) * per : slots * ceil_div(per, (int64_t)8));
   GCN_CHECK(launch_fits(blocks, 64 * WR * WC));
@@ -751,8 +772,8 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   auto parts_of = [&](auto waves_r, auto waves_c, auto blocks_r, auto blocks_c) {
     constexpr int WR = decltype(waves_r)::value, WC = decltype(waves_c)::value;
     constexpr int RB = decltype(blocks_r)::value, CB = decltype(blocks_c)::value;
-    return odd ? launch<WR, WC, RB, CB>(k_mul8_parts<true, WR, WC, RB, CB>, a, s)
-               : launch<WR, WC, RB, CB>(k_mul8_parts<false, WR, WC, RB, CB>, a, s);
+    return odd ? launch<WR, WC, RB, CB>(k_mul8_parts<true, WR, WC, RB, CB>, a, 4, s)
+               : launch<WR, WC, RB, CB>(k_mul8_parts<false, WR, WC, RB, CB>, a, 4, s);
   };
   std::integral_constant<int, 1> n1;
   std::integral_constant<int, 2> n2;
@@ -763,13 +784,13 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
               : tn == 128 ? parts_of(n2, n2, n2, n2)
                           : parts_of(n2, n4, n2, n2));
   else if (wide)
-    GCN_CHECK((odd ? launch<4, 2, 2, 4>(k_mul8_direct<true, 64, 4, 2, 2, 4>, a, s)
-                   : launch<4, 2, 2, 4>(k_mul8_direct<false, 64, 4, 2, 2, 4>, a, s)));
+    GCN_CHECK((odd ? launch<4, 2, 2, 4>(k_mul8_direct<true, 64, 4, 2, 2, 4>, a, 2, s)
+                   : launch<4, 2, 2, 4>(k_mul8_direct<false, 64, 4, 2, 2, 4>, a, 2, s)));
   else if (direct)
-    GCN_CHECK((odd ? launch<2, 2, 2, 2>(k_mul8_direct<true, 64, 2, 2, 2, 2>, a, s)
-                   : launch<2, 2, 2, 2>(k_mul8_direct<false, 64, 2, 2, 2, 2>, a, s)));
+    GCN_CHECK((odd ? launch<2, 2, 2, 2>(k_mul8_direct<true, 64, 2, 2, 2, 2>, a, 2, s)
+                   : launch<2, 2, 2, 2>(k_mul8_direct<false, 64, 2, 2, 2, 2>, a, 2, s)));
   else
-    GCN_CHECK((launch<2, 2, 2, 2>(k_mul8<64, 2, 2, 2, 2>, a, s)));
+    GCN_CHECK((launch<2, 2, 2, 2>(k_mul8<64, 2, 2, 2, 2>, a, 2, s)));
   return parts > 0 ? sum_group_partials(a.by, a.split, K, N, a.part, a.c, a.ldc, a.stride_c, s)
                    : GCN_OK;
 }
@@ -808,7 +829,7 @@ extern "C" gcn_status gcn_gemm_grouped_q8(int64_t n_groups, const int64_t* offse
     return GCN_EINVAL;
   }
   Q8Args a{Groups{(int)n_groups, offsets, rows}, (int)N, (int)K, Q, ldq, S, lds, B, ldb, C, ldc,
-           stride_w, 0, nullptr, 0, 0, 0, false};
+           stride_w, 0, nullptr, 0, 0, 0, false, 0, 0, 0};
   if (mul8_takes(a)) return mul8(a, dtype, &scratch, s);
   // four workgroups to a CU, chunks of 128 to 4096 rows (4096 where the groups' tiles are enough, longer
   // for more than a launch would take)

@@ -223,7 +223,8 @@ __global__ __launch_bounds__(NT) void k_place(SortArgs a) {
   }
 }
 
-// Few ids and groups: all of it by one workgroup, in one launch (48 ids: .. us).
+// Few ids and groups: all of it by one workgroup, in one launch (4096 ids of 64 groups: 9 us a
+// call of the binding; 65,536 in three launches 13).
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kOneItems = 4, kOneMost = kThreads * kOneItems;
 constexpr uint32_t kOneDigits = kThreads;
