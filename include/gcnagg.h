@@ -454,7 +454,9 @@ gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t
                                     float* dgamma, float* dbeta, void* work, int64_t* work_bytes,
                                     void* stream);
 
-/* ---- routed layers: rows to their groups and back ------------------------------ */
+/* ---- routed layers: rows to their groups and back ------------------------------
+ * Calls of this section whose rows need more threads than one launch takes (2^32) return
+ * GCN_ERANGE before any work. */
 
 /* Positions sorted by group: the plan that the calls below share. For ids[i], i < n:
  *   offsets  int64 [n_groups + 1]: group g's positions are the places

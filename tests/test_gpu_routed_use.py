@@ -326,3 +326,58 @@ def test_empty_and_single(G):
     assert host(off).tolist() == [0, 0, 0] and host(order).tolist() == [-1] and host(slot).tolist() == [-1]
     assert not bool(G.gcn_embed_fwd(T, order).any())
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_route_gradient_in_place_and_in_parts(G, kind):
+    """The logits' gradient in the logits' place; that of the weights alone and that of the loss alone, whose
+    sum it is."""
+    import torch
+    note("router gradient in place")
+    n, E, k = 513, 20, 3
+    r = np.random.default_rng(2)
+    z = dev(r.standard_normal((n, E)).astype(np.float32)).to(torch.float32 if kind == "f32" else torch.bfloat16)
+    dw = dev(r.standard_normal((n, k)).astype(np.float32))
+    for normalize in (False, True):
+        ex, w, c, _ = G.gcn_route_fwd(z, k, coef=0.5, normalize=normalize)
+        both = G.gcn_route_bwd(z, ex, w, c, dweights=dw, coef=0.5, normalize=normalize)
+        one = G.gcn_route_bwd(z, ex, w, dweights=dw, normalize=normalize).double()
+        two = G.gcn_route_bwd(z, ex, w, c, coef=0.5, normalize=normalize).double()
+        # three roundings to the type, and those of fp32 sums of some terms of this size
+        unit = (one.abs() + two.abs()) * (ref.HALF[kind] if kind == "bf16" else 0) * 2 + 200 * ref.U
+        assert bool(((one + two - both.double()).abs() <= unit).all())
+        assert not bool(G.gcn_route_bwd(z, ex, w, normalize=normalize).any())
+        y = z.clone()
+        assert G.gcn_route_bwd(y, ex, w, c, dweights=dw, coef=0.5, normalize=normalize, dlogits=y) is y
+        assert torch.equal(y, both)
+
+
+def test_only_what_is_asked_for(G):
+    """Outputs that are left out, and given ones: rows of a wider matrix, whose other columns stay."""
+    import torch
+    note("outputs left out")
+    n, k, F, rows = 50, 2, 40, 100
+    r = np.random.default_rng(4)
+    Z, dY = dev(r.standard_normal((rows, F)).astype(np.float32)), dev(r.standard_normal((n, F)).astype(np.float32))
+    slot = dev(r.permutation(rows)[:n * k].reshape(n, k).astype(np.int32))
+    w = dev(r.random((n, k)).astype(np.float32))
+    dZ, dw = G.gcn_combine_bwd(Z, slot, w, dY)
+    a, none = G.gcn_combine_bwd(Z, slot, w, dY, weight_grad=False)
+    assert none is None and torch.equal(a, dZ)
+    none, b = G.gcn_combine_bwd(Z, slot, w, dY, input_grad=False)
+    assert none is None and torch.equal(b, dw)
+    assert torch.equal(G.gcn_combine_fwd(Z, slot), G.gcn_combine_fwd(Z, slot, torch.ones_like(w)))
+    wide = torch.full((n, F + 7), 3.0, device="cuda:0")
+    G.gcn_combine_fwd(Z, slot, w, Y=wide[:, 3:3 + F])
+    assert torch.equal(wide[:, 3:3 + F], G.gcn_combine_fwd(Z, slot, w))
+    assert bool((wide[:, :3] == 3).all()) and bool((wide[:, 3 + F:] == 3).all())
+    ids = dev(r.integers(0, 9, n).astype(np.int32))
+    off, order, slots = G.gcn_group_ids(ids, 9, slots=False)
+    assert slots is None
+    dT = torch.ones((9, F), device="cuda:0").bfloat16()
+    G.gcn_embed_bwd(dY, off, order, dT=dT, accumulate=True)
+    want = 1 + G.gcn_embed_bwd(dY, off, order).double()
+    # the sum rounded to fp32, and with the one to bf16: half a step of each
+    assert bool(((dT.double() - want).abs() <= want.abs() * 1.01 * 2.0 ** -8 + 1e-5).all())
+    ex, w2, c, loss = G.gcn_route_fwd(Z, 3)
+    assert loss is None and torch.equal(ex, G.gcn_route_fwd(Z, 3, coef=1.0)[0])
