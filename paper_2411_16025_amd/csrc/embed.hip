@@ -161,9 +161,11 @@ __global__ __launch_bounds__(kThreads) void k_zero(char* p, int64_t bytes) {
 
 // A workgroup has up to kRows rows, or a part of a long one, in pieces of 16 bytes of dT. Rows without
 // a place, most of a large table's, are zeros, which bound the pass; those that have some are listed, so
-// that all lanes gather. A large table whose rows lie beside each other is zeroed by a launch before,
-// which knows nothing of rows and writes at 6.8 TB/s (2,449,029 x 100 fp32, 250,000 places: 318 us where
-// each piece looked for its row's places, 245 with the zeros of a workgroup's rows written first, .. so).
+// that all lanes gather (2,449,029 x 100 fp32, 250,000 places: 318 us where each piece looked for its
+// row's places, 245 with the zeros of a workgroup's rows written first; 282 with zeros past the caches).
+// A table with a place for fewer than every 32nd row, whose rows lie beside each other, is zeroed by a
+// launch before, which knows nothing of rows and writes at 6.8 TB/s (25,000 places: 244 and 204 us;
+// 250,000 places at 128 columns: 274 and 305, so not there).
 constexpr int kRows = 1024;
 
 template <class T, class TT, int kRowTile>

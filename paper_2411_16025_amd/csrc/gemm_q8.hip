@@ -4,8 +4,8 @@
 // of bf16 rows (gemm_grouped.hip), or of one bf16 operand with the three parts of an fp32 one
 // (gemm_split.hip). Decoding takes 2.75 instructions an element of X for every 256 columns of B;
 // between the products it costs little. bf16, 32,768 rows of 16 ragged groups, 2048 x 4096: 615 to 645 us,
-// 41% of the cycles in the matrix cores, half a millisecond of them; in one group 902 TFLOP/s. fp32,
-// 500,000 rows of 4 groups, 100 x 256: 143 us, bound by its bytes (4.2 TB/s).
+// 41% of the cycles in the matrix cores; in one group 902 TFLOP/s. fp32, 500,000 rows of
+// 4 groups, 100 x 256: 143 us, bound by its bytes (4.2 TB/s).
 
 #include <algorithm>
 #include <cmath>
@@ -757,7 +757,9 @@ bool mul8_takes(const Q8Args& a) {
 
 gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   const int64_t N = a.N, K = a.K, rows = a.by.rows;
-  // chunks as gemm_grouped.hip's
+  // chunks as gemm_grouped.hip's, but shorter where few groups leave units idle: there a chunk's time
+  // weighs more than its sums (32,768 rows of 16 groups, 2048 x 4096 bf16: 673 us, 857 with the few's
+  // 1e-4; 200,000 of 8, 256 x 512: 95 so, 114 with the others' 2e-4)
   const bool direct = dtype == GCN_DT_BF16 && reinterpret_cast<uintptr_t>(a.b) % 16 == 0 &&
                       a.ldb % 8 == 0 && N % 8 == 0;
   const bool f32 = dtype == GCN_DT_F32;
@@ -766,10 +768,11 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   const int64_t tn = wide ? 256 : !f32 ? 128 : N <= 64 ? 64 : tm == 64 ? 128 : (N - 1) % 256 < 128 ? 128 : 256;
   const int64_t tiles = ceil_div(K, tm) * ceil_div(N, tn);
   const int64_t want = tn == 256 ? 240 : 480;
+  const bool few = a.by.n * tiles < want;
   const double even = (double)rows * (double)tiles / (double)want;
-  const double sums = std::sqrt(2e-4 * (double)rows * (double)K * (double)N);
-  const double chunk = std::min(
-      65536.0, std::max({256.0, sums, a.by.n * tiles < want ? std::min(even, 4096.0) : 4096.0}));
+  const double sums = std::sqrt((few ? 1e-4 : 2e-4) * (double)rows * (double)K * (double)N);
+  const double chunk =
+      std::min(65536.0, std::max({256.0, sums, few ? std::min(even, 4096.0) : 4096.0}));
   a.split = ceil_div((int64_t)chunk, (int64_t)64) * 64;
   const int64_t parts = rows / a.split;
   if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * K * N, "grouped GEMM partials"));

@@ -146,7 +146,7 @@ struct Left {
 // bf16: value and index in one whole number, the value's bits in an order that grows with it (-0 as
 // +0), below them the index from the end; 0 for a logit that cannot be chosen. A lane's are sorted
 // once (Batcher's odd-even merge), so that the next one is its first, or another lane's
-// (131,072 rows of 64, 8 chosen: 30 us with a search of the eight each time, 21 so, and with exp2).
+// (131,072 rows of 64, 8 chosen: 30 us with a search of the eight each time, 19 so and with exp2).
 template <int G, int V>
 struct Left<bf16, G, V> {
   uint32_t key[V];
