@@ -363,8 +363,8 @@ extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_gro
                                     int64_t* work_bytes, void* stream) {
   clear_error();
   CallScope scope(stream);
-  if (n < 0 || n_groups < 1 || !offsets || (n > 0 && !ids)) {
-    set_error("need n >= 0, n_groups >= 1 and non-NULL ids and offsets");
+  if (n < 0 || n_groups < 1 || !offsets || (n > 0 && (!ids || order == ids || slot == ids))) {
+    set_error("need n >= 0, n_groups >= 1, non-NULL ids and offsets, and order and slot apart from ids");
     return GCN_EINVAL;
   }
   if (n >= (int64_t(1) << 31) || n_groups > (int64_t(1) << 30)) {

@@ -27,7 +27,7 @@ def test_group_ids_refusals(L):
     d = dict(n=4, ids=A, groups=3, offsets=B, order=C, slot=C, work=None, size=None, stream=None)
     some = ctypes.byref(ctypes.c_int64(1 << 30))
     refused(L.gcn_group_ids, d, [dict(n=-1), dict(groups=0), dict(groups=-5), dict(ids=None), dict(offsets=None),
-                                 dict(work=A), dict(work=ODD, size=some)])
+                                 dict(work=A), dict(work=ODD, size=some), dict(order=A), dict(slot=A)])
     refused(L.gcn_group_ids, d, [dict(n=1 << 31), dict(groups=(1 << 30) + 1)], ERANGE)
     size = ctypes.c_int64(-1)
     ask = dict(size=ctypes.byref(size))
