@@ -165,7 +165,9 @@ __global__ __launch_bounds__(kThreads) void k_zero(char* p, int64_t bytes) {
 // row's places, 245 with the zeros of a workgroup's rows written first; 282 with zeros past the caches).
 // A table with a place for fewer than every 32nd row, whose rows lie beside each other, is zeroed by a
 // launch before, which knows nothing of rows and writes at 6.8 TB/s (25,000 places: 244 and 204 us;
-// 250,000 places at 128 columns: 274 and 305, so not there).
+// 250,000 places at 128 columns: 274 and 305, so not there). Rows that are no whole pieces cost the pass
+// more, which then is for every 8th (245,000 places at 47 columns: 217 and 149, at 101: 300 and 284;
+// 490,000 at 101: 338 and 348).
 constexpr int kRows = 1024;
 
 template <class T, class TT, int kRowTile>
@@ -330,7 +332,8 @@ gcn_status embed_bwd(SumArgs a, Scratch* scratch, hipStream_t s) {
   const bool sparse = a.by.n > 4 * a.by.rows;
   a.tiles = row_tiles(a.by.n, ceil_div((int64_t)a.F, (int64_t)kPiece<TT>), sparse ? 4096 : 1024);
   a.tiles.rows = std::min<uint32_t>(a.tiles.rows, kRows);
-  a.zeroed = a.by.n > 32 * a.by.rows && !a.add && a.lddt == a.F;
+  const bool whole = a.lddt % kPiece<TT> == 0;
+  a.zeroed = a.by.n > (whole ? 32 : 8) * a.by.rows && !a.add && a.lddt == a.F;
   if (a.zeroed && a.tiles.parts == 1)  // more rows, of which few are listed
     a.tiles.rows = std::min(512u, std::max(1u, 16384 / a.tiles.pieces));
   a.shift = a.by.rows <= (1 << 18) ? 5 : 7;

@@ -150,7 +150,8 @@ def test_embed_bwd(E, n, F, V, how, kd, kt):
 
 
 @pytest.mark.parametrize("kt", KINDS)
-@pytest.mark.parametrize("n,F,V", [(30, 7, 3000), (5, 100, 900), (40, 3, 2001), (1, 1, 9), (500, 47, 30000)])
+@pytest.mark.parametrize("n,F,V", [(30, 7, 3000), (5, 100, 900), (40, 3, 2001), (1, 1, 9), (500, 47, 30000),
+                                   (500, 47, 6000), (2000, 101, 20000)])
 def test_embed_bwd_sparse(E, n, F, V, kt):
     """Most rows without a place, rows of dT beside each other, from an address of any element."""
     for shift in (0, 1, 3):
