@@ -2,8 +2,8 @@
 //
 // The codes' values are exact in bf16, so they are decoded on their way to LDS, and the product is that
 // of bf16 rows (gemm_grouped.hip), or of one bf16 operand with the three parts of an fp32 one
-// (gemm_split.hip). Decoding takes 2.75 instructions an element of X for every 256 columns of B;
-// between the products it costs little. bf16, 32,768 rows of 16 ragged groups, 2048 x 4096: 615 to 645 us,
+// (gemm_split.hip). Decoding takes 2.5 instructions an element of X for every 256 columns of B;
+// between the products it costs little. bf16, 32,768 rows of 16 ragged groups, 2048 x 4096: 595 to 615 us,
 // 41% of the cycles in the matrix cores; in one group 902 TFLOP/s. fp32, 500,000 rows of
 // 4 groups, 100 x 256: 143 us, bound by its bytes (4.2 TB/s).
 
@@ -101,17 +101,19 @@ __device__ inline u4 bytes_down(u4 v, int n) {
   return u4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)};
 }
 
-// The values of eight codes, exact in bf16: codes + 128 are bytes, which fp32 takes in one
-// instruction, and u unit - 128 unit is exact.
+// The values of eight codes, exact in bf16: a signed byte becomes fp32 in one instruction, its product with
+// the unit is another. (Unsigned bytes less an offset of 128 units would take as many, but at the largest unit,
+// 2^121, that offset is no fp32 number. With 0 added: of plain products the compiler forms a stage's early and
+// spills 27 registers of the 256 x 256 tile, 790 us for the 607 of the ragged groups above; signed bytes
+// as unsigned ones less 128, times the unit: 635.)
 __device__ inline u4 decode8(uint32_t c0, uint32_t c1, float unit) {
-  const float off = -128.f * unit;
   u4 r;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint32_t u = (i ? c1 : c0) ^ 0x80808080u;
+    const uint32_t c = i ? c1 : c0;
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)(u >> (8 * e) & 255), unit, off);
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)(int8_t)(c >> (8 * e)), unit, 0.f);
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       r[2 * i + e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]),
@@ -382,7 +384,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_mul8(Q8Args a) {
 }
 
 // bf16 rows that start on 16 bytes and hold whole pieces. The codes' way to LDS is through
-// registers, three stages long, so that decoding them (22 vector instructions for 8) stands between
+// registers, three stages long, so that decoding them (20 vector instructions for 8) stands between
 // the products of the stage before theirs: their loads are issued with the direct loads of the
 // other operand, waited for with them one stage later, and decoded during the next one. No branch
 // divides a stage: past the last one its loads are repeated, rows past the chunk's end have a unit of

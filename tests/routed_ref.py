@@ -490,3 +490,45 @@ def check_route_bwd_any(e, n, E, k, kind="f32", seed=0):
     assert e.lib.gcn_route_bwd(n, E, z.ptr, z.ld, CODE[kind], k, 1, ex.ptr, w.ptr, c.ptr, 1.0, w.ptr, None, dz.ptr,
                                dz.ld, e.stream) == 0
     dz.check_margins()
+
+
+def check_grad8_scales(e, sizes, K, N, kind="f32", small=-10, large=None, seed=0):
+    """Rows of X at both ends of the scale bytes: the first 32 columns with finite values up to the largest ones
+    (bytes 247 and 248, codes of 0 and of all sizes under them), the last block of columns with the smallest (byte
+    1). B is of size 2^small, from column N / 2 on 2^large where that is given."""
+    r = np.random.default_rng(seed)
+    rows = int(np.sum(sizes))
+    x = r.standard_normal((rows, K))
+    last = (K - 1) // 32 * 32
+    top = r.choice(np.array([2e38, -2e38, 3.3e38, -3.3e38, 1e38, -1e38]), rows)
+    at = r.integers(0, min(K, 32), rows)
+    big = r.random(rows) < 0.4
+    big[:2] = True, rows < 2
+    x[big, at[big]] = top[big]
+    spread = big & (r.random(rows) < 0.5)  # codes of all sizes beside it
+    c = slice(0, min(K, 32))
+    x[spread, c] = r.uniform(-1, 1, (rows, min(K, 32)))[spread] * 3.3e38
+    if last:
+        x[:, last:] *= 2.0 ** -125
+    q, s = pack8(x.astype(np.float32))
+    assert (s[big, 0] >= 246).all() and (s[0, 0] >= 247) and (not last or (s[:, -1] <= 2).all())
+    b = r.standard_normal((rows, N)) * 2.0 ** small
+    if large is not None:
+        b[:, N // 2:] *= 2.0 ** (large - small)
+    b = rounded(b, kind)
+    qd, sd, bd = e.rows(q, "i8", 0), e.rows(s, "u8", 0), e.rows(b, kind, 0)
+    G, ends = len(sizes), np.concatenate([[0], np.cumsum(sizes)])
+    o, c = e.put(ends.astype(np.int64)), e.rows(np.full((G * K, N), 7.0), "f32", 0)
+    Call(e, 0)(e.lib.gcn_gemm_grouped_q8, G, o.ptr, rows, N, K, qd.ptr, qd.ld, sd.ptr, sd.ld, bd.ptr, bd.ld,
+               CODE[kind], c.ptr, c.ld, K * N)
+    got = c.get().reshape(G, K, N)
+    for g in range(G):
+        rng = slice(ends[g], ends[g + 1])
+        u, v = unpack8(q[rng], s[rng]), b[rng].astype(np.float64)
+        want, mag = u.T @ v, np.abs(u).T @ np.abs(v)
+        # a chain of sums; products below 2^-126 and their sums may be lost. Sums of magnitudes that fp32
+        # does not hold may be infinities or NaN
+        near = np.abs(got[g] - want) <= (sizes[g] + 8) * U * mag + sizes[g] * 2.0 ** -126
+        bad = ~near & (mag < 3e38)
+        assert not bad.any(), (sizes, K, N, kind, small, large, g, bad.sum(), np.argwhere(bad)[:3], got[g][bad][:3],
+                               want[bad][:3])

@@ -276,6 +276,16 @@ def test_grad8_special(E, rows, K, N, kind):
     run(E, "check_grad8_special", rows, K, N, kind=kind, seed=K)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("sizes,K,N", [([12], 7, 3), ([40], 64, 9), ([40], 64, 8), ([700], 40, 16), ([600], 33, 20),
+                                       ([300], 260, 264), ([300], 256, 136), ([40, 0, 30], 150, 20),
+                                       ([2000, 900], 512, 1000), ([3000], 100, 47), ([2000], 261, 257)])
+def test_grad8_scales(E, sizes, K, N, kind):
+    """Scale bytes from 1 to 248, which packing gives to finite values."""
+    for how in (dict(), dict(small=-100), dict(large=100)):
+        run(E, "check_grad8_scales", sizes, K, N, kind=kind, seed=K, **how)
+
+
 # ---- a layer --------------------------------------------------------------------------
 
 def test_layer(G):

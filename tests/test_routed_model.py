@@ -143,6 +143,18 @@ def test_grad8_special(model):
            for rows, K, N in ((40, 64, 8), (100, 150, 20), (300, 260, 264), (9, 40, 7))])
 
 
+# (K, N): the general kernel; through registers; direct loads, with whole units of 16 codes and without, in
+# tiles of 128 and 256; more than one chunk, whose products alternate in sign
+SCALES = [([12], 7, 3), ([40], 64, 9), ([40], 64, 8), ([700], 40, 16), ([600], 33, 20), ([300], 260, 264),
+          ([300], 256, 136), ([40, 0, 30], 150, 20)]
+
+
+def test_grad8_scales(model):
+    """Scale bytes from 1 to 248, which packing gives to finite values."""
+    model([["check_grad8_scales", [sizes, K, N], dict(kind=kind, seed=K, **how)] for kind in ("f32", "bf16")
+           for sizes, K, N in SCALES for how in (dict(), dict(small=-100), dict(large=100))])
+
+
 def test_any_plan(model):
     """Offsets, orders and experts that no call gives: no address leaves the arrays."""
     cases = []
