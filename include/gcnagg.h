@@ -466,7 +466,7 @@ gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t
  * An id outside [0, n_groups) (padding, a dropped choice) belongs to no group: its slot is
  * -1, and the places from offsets[n_groups] on hold -1 in `order`. So the sizes of what
  * follows are those of n, whatever the ids are, and a captured call follows them.
- *  ids  int32 device [n], which no output may overlap; 0 <= n < 2^31, 1 <= n_groups <= 2^30.
+ *  ids  int32 device [n]; 0 <= n < 2^31, 1 <= n_groups <= 2^30. Arrays that overlap are refused.
  *  work, work_bytes  scratch memory, as for gcn_gemm_grouped.
  * No atomics on results: the one stable order. Asynchronous on `stream`. */
 gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_groups, int64_t* offsets,

@@ -106,6 +106,12 @@ inline gcn_status launch_fits(int64_t blocks, int64_t threads) {
   return GCN_ERANGE;
 }
 
+// Whether two arrays of so many bytes share any.
+inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a && b && a_bytes > 0 && b_bytes > 0 && (p <= q ? q - p < (uint64_t)a_bytes : p - q < (uint64_t)b_bytes);
+}
+
 // n rows of F columns of a known type.
 inline gcn_status check_rows(int64_t n, int64_t F, int dtype) {
   if (n < 0 || F <= 0 || F > (int64_t(1) << 30) ||

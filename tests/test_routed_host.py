@@ -41,6 +41,28 @@ def test_group_ids_refusals(L):
     refused(L.gcn_group_ids, d, [dict(n=100000, work=A, size=less)])
 
 
+def at(address):
+    return ctypes.c_void_p(address)
+
+
+def test_group_ids_refuses_arrays_over_each_other(L):
+    """Wherever one begins in the other (nothing is launched); the question for the scratch memory's size
+    looks at no array."""
+    n, G = 1000, 99
+    d = dict(n=n, ids=at(0x10000), groups=G, offsets=at(0x20000), order=at(0x30000), slot=at(0x40000), work=None, size=None,
+             stream=None)
+    first = dict(ids=0x10000, offsets=0x20000, order=0x30000, slot=0x40000)
+    size = dict(ids=4 * n, offsets=8 * (G + 1), order=4 * n, slot=4 * n)
+    for a in first:
+        for b in first:
+            if a != b:
+                refused(L.gcn_group_ids, d, [{a: at(first[b])}, {a: at(first[b] + size[b] - 8)},
+                                             {a: at(first[b] - size[a] + 8)}])
+    want = ctypes.c_int64(-1)
+    assert L.gcn_group_ids(*{**d, "groups": 5000, "slot": d["order"], "size": ctypes.byref(want)}.values()) == 0
+    assert want.value > 0
+
+
 def test_embed_refusals(L):
     d = dict(n=4, F=8, V=5, ids=A, per=1, T=B, ldt=8, dt=0, scale=1.0, Y=C, ldy=8, dy=0, stream=None)
     refused(L.gcn_embed_fwd, d, [dict(n=-1), dict(F=0), dict(F=(1 << 30) + 1), dict(V=0), dict(V=-1), dict(ids=None),
