@@ -456,7 +456,9 @@ gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t
 
 /* ---- routed layers: rows to their groups and back ------------------------------
  * Calls of this section whose rows need more threads than one launch takes (2^32) return
- * GCN_ERANGE before any work. */
+ * GCN_ERANGE before any work. Their outputs may overlap neither an input nor another output, but
+ * where a call says so; they may lie between an input's rows. Calls whose arrays share a byte
+ * otherwise are refused. */
 
 /* Positions sorted by group: the plan that the calls below share. For ids[i], i < n:
  *   offsets  int64 [n_groups + 1]: group g's positions are the places
@@ -466,7 +468,7 @@ gcn_status gcn_layernorm_affine_bwd(int64_t n, int64_t F, const void* X, int64_t
  * An id outside [0, n_groups) (padding, a dropped choice) belongs to no group: its slot is
  * -1, and the places from offsets[n_groups] on hold -1 in `order`. So the sizes of what
  * follows are those of n, whatever the ids are, and a captured call follows them.
- *  ids  int32 device [n]; 0 <= n < 2^31, 1 <= n_groups <= 2^30. Arrays that overlap are refused.
+ *  ids  int32 device [n]; 0 <= n < 2^31, 1 <= n_groups <= 2^30.
  *  work, work_bytes  scratch memory, as for gcn_gemm_grouped.
  * No atomics on results: the one stable order. Asynchronous on `stream`. */
 gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_groups, int64_t* offsets,
@@ -478,7 +480,7 @@ gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_groups, int64_
  *  per    >= 1: 1 for a lookup. With the `order` of gcn_group_ids over the k choices of
  *         each token, per = k brings the tokens' rows into the groups' order.
  *  T [V x F] (ldt) of type dtype, Y [n x F] (ldy) of type dtype_y: GCN_DT_F32 or
- *  GCN_DT_BF16 each; Y may not overlap T. ids int32 device [n]. n < 2^31,
+ *  GCN_DT_BF16 each. ids int32 device [n]. n < 2^31,
  *  1 <= V < 2^31, F <= 2^30, scale finite. Asynchronous. */
 gcn_status gcn_embed_fwd(int64_t n, int64_t F, int64_t V, const int32_t* ids, int64_t per,
                          const void* T, int64_t ldt, int dtype, double scale, void* Y, int64_t ldy,
@@ -493,7 +495,7 @@ enum { GCN_ACCUMULATE = 1u /* add to what dT holds */ };
  * occur become 0; with GCN_ACCUMULATE the sums are added to dT, whose other rows are not
  * touched. Sums in fp32 over at most 128 rows, those sums in double, one rounding to dT's
  * type; each in an order that n, offsets and order decide, so results repeat bit for bit.
- *  dY [n x F] (lddy) of type dtype, dT [V x F] (lddt) of type dtype_t, which may not overlap.
+ *  dY [n x F] (lddy) of type dtype, dT [V x F] (lddt) of type dtype_t.
  *  Entries of `order` outside [0, n) are left out; offsets outside [0, n] are taken as 0 or n.
  *  Where they decrease no values are defined in dT, but nothing is read or written outside of
  *  the arrays.
@@ -551,7 +553,7 @@ gcn_status gcn_route_bwd(int64_t n, int64_t E, const void* logits, int64_t ldz, 
  * part; a row without any becomes +0.
  *  Z [rows x F] (ldz), Y [n x F] (ldy) of type dtype; slot int32 [n k]; weights fp32 [n k], or
  *  NULL for 1: then it is the gradient of gcn_embed_fwd with per = k.
- *  n < 2^31, 0 <= rows < 2^31, 1 <= k <= 2^16, F <= 2^30. Y may not overlap Z. Asynchronous. */
+ *  n < 2^31, 0 <= rows < 2^31, 1 <= k <= 2^16, F <= 2^30. Asynchronous. */
 gcn_status gcn_combine_fwd(int64_t n, int64_t k, int64_t F, const void* Z, int64_t rows,
                            int64_t ldz, int dtype, const int32_t* slot, const float* weights,
                            void* Y, int64_t ldy, void* stream);
@@ -559,8 +561,8 @@ gcn_status gcn_combine_fwd(int64_t n, int64_t k, int64_t F, const void* Z, int64
 /* Gradients of gcn_combine_fwd: dZ[slot[t k + i]] = weights[t k + i] dY[t] and
  * dweights[t k + i] = <dY[t], Z[slot[t k + i]]> (0 for a slot outside [0, rows)).
  * No slot may occur twice. Rows of dZ that are no slot's are left as they were.
- *  dZ [rows x F] (lddz) or NULL, may be Z itself (same ld); dweights fp32 [n k] or NULL (Z may
- *  be NULL then); not both NULL. Products and sums in fp32. Asynchronous. */
+ *  dZ [rows x F] (lddz) or NULL, may be Z itself (same ld); dweights fp32 [n k], may be the
+ *  weights themselves, or NULL (Z may be NULL then); not both NULL. Products and sums in fp32. Asynchronous. */
 gcn_status gcn_combine_bwd(int64_t n, int64_t k, int64_t F, const void* Z, int64_t rows,
                            int64_t ldz, int dtype, const int32_t* slot, const float* weights,
                            const void* dY, int64_t lddy, void* dZ, int64_t lddz, float* dweights,

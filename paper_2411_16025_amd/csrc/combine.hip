@@ -152,6 +152,9 @@ extern "C" gcn_status gcn_combine_fwd(int64_t n, int64_t k, int64_t F, const voi
     set_error("Z, slot and Y must be non-NULL, Y and Z apart, with ldz, ldy >= F");
     return GCN_EINVAL;
   }
+  GCN_CHECK(check_apart({rows_of(Y, n, ldy, F, size_of(dtype))},
+                        {rows_of(Z, rows, ldz, F, size_of(dtype)), array_of(slot, 4 * n * k),
+                         array_of(weights, 4 * n * k)}));
   CombineArgs a{};
   a.n = n;
   a.k = (int)k;
@@ -184,6 +187,13 @@ extern "C" gcn_status gcn_combine_bwd(int64_t n, int64_t k, int64_t F, const voi
               "strides >= F (and one stride where dZ is Z)");
     return GCN_EINVAL;
   }
+  // (dweights in the weights' place: each one is read before its gradient is written)
+  const Span none{}, z = rows_of(dweights ? Z : nullptr, rows, ldz, F, size_of(dtype));
+  const Span dy = rows_of(dY, n, lddy, F, size_of(dtype)), at = array_of(slot, 4 * n * k);
+  const Span w = array_of(weights, 4 * n * k), dw = array_of(dweights, 4 * n * k);
+  GCN_CHECK(check_apart({rows_of(dZ, rows, lddz, F, size_of(dtype)), dw},
+                        {dZ == Z ? none : z, dy, at, weights == dweights ? none : w}));
+  GCN_CHECK(check_apart({dw}, {z}));
   CombineArgs a{};
   a.n = n;
   a.k = (int)k;

@@ -1,6 +1,9 @@
 // Element types of the calls that take a dtype.
 #pragma once
 
+#include <algorithm>
+#include <initializer_list>
+
 #include "common.h"
 
 namespace gcn {
@@ -106,10 +109,45 @@ inline gcn_status launch_fits(int64_t blocks, int64_t threads) {
   return GCN_ERANGE;
 }
 
-// Whether two arrays of so many bytes share any.
-inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-  return a && b && a_bytes > 0 && b_bytes > 0 && (p <= q ? q - p < (uint64_t)a_bytes : p - q < (uint64_t)b_bytes);
+// Rows of so many bytes, `stride` bytes apart, or one array.
+struct Span {
+  const void* p;
+  int64_t rows, stride, bytes;
+};
+inline Span array_of(const void* p, int64_t bytes) { return Span{p, 1, bytes, bytes}; }
+inline Span rows_of(const void* p, int64_t n, int64_t ld, int64_t F, int64_t size) {
+  return Span{p, n, ld * size, F * size};
+}
+inline int64_t size_of(int dtype) { return dtype == GCN_DT_BF16 ? 2 : 4; }
+
+// Whether they share a byte; rows may lie between the other's.
+inline bool overlap(const Span& a, const Span& b) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+  if (p > q) return overlap(b, a);
+  if (!p || a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
+  const uint64_t end = (uint64_t)(a.rows - 1) * a.stride + a.bytes;
+  // (rows of the same stride all lie as the first one does; of others the ways to lie repeat)
+  const int64_t ways = a.stride == b.stride ? 1 : std::min(b.rows, a.stride);
+  uint64_t at = q - p;
+  for (int64_t i = 0; i < ways && at < end; ++i, at += b.stride) {
+    if (a.rows == 1) return true;
+    const uint64_t in = at % (uint64_t)a.stride;
+    if (in < (uint64_t)a.bytes || in + b.bytes > (uint64_t)a.stride) return true;
+  }
+  return false;
+}
+
+// Outputs apart from the inputs and from each other.
+inline gcn_status check_apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+  for (const Span* a = outputs.begin(); a != outputs.end(); ++a) {
+    bool bad = false;
+    for (const Span& b : inputs) bad = bad || overlap(*a, b);
+    for (const Span* b = outputs.begin(); b != a; ++b) bad = bad || overlap(*a, *b);
+    if (!bad) continue;
+    set_error("an output may not overlap an input or another output");
+    return GCN_EINVAL;
+  }
+  return GCN_OK;
 }
 
 // n rows of F columns of a known type.

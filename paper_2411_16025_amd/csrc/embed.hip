@@ -393,6 +393,8 @@ extern "C" gcn_status gcn_embed_fwd(int64_t n, int64_t F, int64_t V, const int32
     set_error("ids, T and Y must be non-NULL, T and Y apart, with ldt, ldy >= F");
     return GCN_EINVAL;
   }
+  GCN_CHECK(check_apart({rows_of(Y, n, ldy, F, size_of(dtype_y))},
+                        {rows_of(T, V, ldt, F, size_of(dtype)), array_of(ids, 4 * n)}));
   const TakeArgs a{{}, (uint32_t)F, (uint32_t)V, (uint32_t)per, ids, T, ldt, (float)scale, Y, ldy};
   hipStream_t s = (hipStream_t)stream;
   if (dtype == GCN_DT_F32)
@@ -423,6 +425,10 @@ extern "C" gcn_status gcn_embed_bwd(int64_t n, int64_t F, int64_t V, const int64
     set_error("offsets, order, dY and dT must be non-NULL, dY and dT apart, with lddy, lddt >= F");
     return GCN_EINVAL;
   }
+  if (!scratch.asked())
+    GCN_CHECK(check_apart({rows_of(dT, V, lddt, F, size_of(dtype_t))},
+                          {rows_of(dY, n, lddy, F, size_of(dtype)), array_of(offsets, 8 * (V + 1)),
+                           array_of(order, 4 * n)}));
   SumArgs a{};
   a.by = Groups{(int)V, offsets, n};
   a.n = (int32_t)n;

@@ -751,6 +751,20 @@ gcn_status launch(Kernel kernel, Q8Args a, int b_bytes, hipStream_t s) {
   return GCN_OK;
 }
 
+// C_g apart from what the product reads.
+gcn_status apart(const Q8Args& a, int dtype) {
+  const int64_t rows = a.by.rows, K = a.K, N = a.N;
+  const Span in[4] = {array_of(a.by.offsets, 8 * ((int64_t)a.by.n + 1)), rows_of(a.q, rows, a.ldq, K, 1),
+                      rows_of(a.s, rows, a.lds, ceil_div(K, (int64_t)32), 1),
+                      rows_of(a.b, rows, a.ldb, N, size_of(dtype))};
+  // (matrices as long rows first: most lie nowhere near)
+  for (const Span& x : in)
+    if (overlap(rows_of(a.c, a.by.n, a.by.n > 1 ? a.stride_c : 1, (K - 1) * a.ldc + N, 4), x))
+      for (int g = 0; g < a.by.n; ++g)
+        GCN_CHECK(check_apart({rows_of(a.c + g * a.stride_c, K, a.ldc, N, 4)}, {x}));
+  return GCN_OK;
+}
+
 // Rows of sixteen codes, and strides whose offsets over a stage's rows are 32 bits.
 bool mul8_takes(const Q8Args& a) {
   return a.N >= 8 && a.K >= 16 && a.ldb < (int64_t(1) << 22) && a.ldq < (int64_t(1) << 24) &&
@@ -779,6 +793,7 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   const int64_t parts = rows / a.split;
   if (parts > 0) GCN_CHECK(scratch->alloc(&a.part, parts * K * N, "grouped GEMM partials"));
   if (scratch->asked()) return GCN_OK;
+  GCN_CHECK(apart(a, dtype));
   ProfScope ps("grouped_q8", s);
   const bool odd = K % (f32 ? 8 : 16) != 0 || (f32 && N % 4 != 0);
   auto parts_of = [&](auto waves_r, auto waves_c, auto blocks_r, auto blocks_c) {
@@ -856,6 +871,7 @@ extern "C" gcn_status gcn_gemm_grouped_q8(int64_t n_groups, const int64_t* offse
   GCN_CHECK(launch_fits(blocks, kThreads));
   if (parts > 0) GCN_CHECK(scratch.alloc(&a.part, parts * K * N, "grouped GEMM partials"));
   if (scratch.asked()) return GCN_OK;
+  GCN_CHECK(apart(a, dtype));
   ProfScope ps("grouped_q8", s);
   if (dtype == GCN_DT_F32)
     hipLaunchKernelGGL(k_q8<float>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);

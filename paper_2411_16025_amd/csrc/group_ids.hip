@@ -375,14 +375,9 @@ extern "C" gcn_status gcn_group_ids(int64_t n, const int32_t* ids, int64_t n_gro
   hipStream_t s = (hipStream_t)stream;
   Scratch scratch(work, work_bytes, s);
   const int64_t zero_blocks = ceil_div(n_groups + 1, (int64_t)kThreads);
-  const int64_t places = 4 * n, ends = 8 * (n_groups + 1);
-  if (!scratch.asked() &&
-      (overlap(ids, places, offsets, ends) || overlap(ids, places, order, places) ||
-       overlap(ids, places, slot, places) || overlap(offsets, ends, order, places) ||
-       overlap(offsets, ends, slot, places) || overlap(order, places, slot, places))) {
-    set_error("ids, offsets, order and slot may not overlap");
-    return GCN_EINVAL;
-  }
+  if (!scratch.asked())
+    GCN_CHECK(check_apart({array_of(offsets, 8 * (n_groups + 1)), array_of(order, 4 * n), array_of(slot, 4 * n)},
+                          {array_of(ids, 4 * n)}));
   if (n == 0) {
     if (scratch.asked()) return GCN_OK;
     ProfScope ps("group_ids", s);

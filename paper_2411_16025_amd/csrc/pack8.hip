@@ -86,6 +86,8 @@ extern "C" gcn_status gcn_pack8(int64_t n, int64_t F, const void* X, int64_t ldx
   clear_error();
   GCN_CHECK(check_pack(n, F, dtype, X, ldx, Q, ldq, S, lds));
   if (n == 0) return GCN_OK;
+  GCN_CHECK(check_apart({rows_of(Q, n, ldq, F, 1), rows_of(S, n, lds, ceil_div(F, (int64_t)32), 1)},
+                        {rows_of(X, n, ldx, F, size_of(dtype))}));
   // (whole scale bytes, in each workgroup too)
   PackArgs a{row_tiles(n, ceil_div(F, (int64_t)32) * 4, kThreads), (uint32_t)F, X, ldx, Q, ldq, S,
              lds, nullptr, 0};
@@ -107,6 +109,8 @@ extern "C" gcn_status gcn_unpack8(int64_t n, int64_t F, const int8_t* Q, int64_t
   clear_error();
   GCN_CHECK(check_pack(n, F, dtype, Y, ldy, Q, ldq, S, lds));
   if (n == 0) return GCN_OK;
+  GCN_CHECK(check_apart({rows_of(Y, n, ldy, F, size_of(dtype))},
+                        {rows_of(Q, n, ldq, F, 1), rows_of(S, n, lds, ceil_div(F, (int64_t)32), 1)}));
   PackArgs a{row_tiles(n, ceil_div(F, (int64_t)8), kThreads), (uint32_t)F, nullptr, 0,
              const_cast<int8_t*>(Q), ldq, const_cast<uint8_t*>(S), lds, Y, ldy};
   GCN_CHECK(launch_fits(a.tiles.blocks(), kThreads));

@@ -502,6 +502,10 @@ extern "C" gcn_status gcn_route_fwd(int64_t n, int64_t E, const void* logits, in
     set_error("logits, experts, weights and counts must be non-NULL with ldz >= E");
     return GCN_EINVAL;
   }
+  if (!scratch.asked())
+    GCN_CHECK(check_apart({array_of(experts, 4 * n * k), array_of(weights, 4 * n * k),
+                           array_of(counts, 8 * (E + 1)), array_of(loss, 4)},
+                          {rows_of(logits, n, ldz, E, size_of(dtype)), array_of(mask, n)}));
   RouteArgs a{};
   a.n = n;
   a.E = (int)E;
@@ -545,6 +549,10 @@ extern "C" gcn_status gcn_route_bwd(int64_t n, int64_t E, const void* logits, in
               "non-NULL, with ldz, ldd >= E (and one stride where dlogits are the logits)");
     return GCN_EINVAL;
   }
+  const Span none{}, z = rows_of(logits, n, ldz, E, size_of(dtype));
+  GCN_CHECK(check_apart({rows_of(dlogits, n, ldd, E, size_of(dtype))},
+                        {logits == dlogits ? none : z, array_of(experts, 4 * n * k), array_of(weights, 4 * n * k),
+                         array_of(counts, 8 * (E + 1)), array_of(dweights, 4 * n * k), array_of(dloss, 4)}));
   RouteArgs a{};
   a.n = n;
   a.E = (int)E;

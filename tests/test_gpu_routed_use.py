@@ -381,3 +381,50 @@ def test_only_what_is_asked_for(G):
     assert bool(((dT.double() - want).abs() <= want.abs() * 1.01 * 2.0 ** -8 + 1e-5).all())
     ex, w2, c, loss = G.gcn_route_fwd(Z, 3)
     assert loss is None and torch.equal(ex, G.gcn_route_fwd(Z, 3, coef=1.0)[0])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_neighbouring_columns(G, dtype):
+    """Outputs that lie in other columns of their inputs' rows, and at their end."""
+    import torch
+    note("neighbouring columns %s" % dtype)
+    n, F, k = 60, 40, 2
+    r = np.random.default_rng(6)
+    dt = getattr(torch, dtype)
+    both = dev(r.standard_normal((2 * n, 2 * F + 8)).astype(np.float32)).to(dt)
+    ids = dev(r.permutation(n).astype(np.int32))
+    left, right, below = both[:n, :F], both[:n, F:2 * F], both[n:, :F]
+    want = G.gcn_embed_fwd(left.clone(), ids, scale=0.5)
+    for Y in (right, below, both[n - 1:2 * n - 1, F:2 * F]):
+        keep = left.clone()
+        assert torch.equal(G.gcn_embed_fwd(left, ids, scale=0.5, Y=Y), want) and torch.equal(left, keep)
+    off, order, slot = G.gcn_group_ids(ids, n)
+    assert torch.equal(G.gcn_embed_bwd(left, off, order, dT=right), G.gcn_embed_bwd(left.clone(), off, order, out_dtype=dt))
+    slot = slot[:n // k * k].view(-1, k)
+    w = dev(r.random(slot.shape).astype(np.float32))
+    want = G.gcn_combine_fwd(left.clone(), slot, w)
+    assert torch.equal(G.gcn_combine_fwd(left, slot, w, Y=right[:n // k]), want)
+    dY = right[:n // k].clone()
+    dZ, dw = G.gcn_combine_bwd(left, slot, w, dY, dZ=torch.zeros_like(left))
+    right.zero_()
+    got, dw2 = G.gcn_combine_bwd(left, slot, w, dY, dZ=right)
+    assert torch.equal(got, dZ) and torch.equal(dw2, dw)
+    # the weights' gradients in the weights' place
+    st = G.lib().gcn_combine_bwd(n // k, k, F, left.data_ptr(), n, left.stride(0), 0 if dtype == "float32" else 1, slot.data_ptr(),
+                                 w.data_ptr(), dY.data_ptr(), F, right.data_ptr(), right.stride(0), w.data_ptr(), None)
+    torch.cuda.synchronize()
+    assert st == 0 and torch.equal(w, dw) and torch.equal(right, dZ)
+    z = both[:n, :F]
+    ex, wt, c, _ = G.gcn_route_fwd(z, k, coef=1.0)
+    want = G.gcn_route_bwd(z.clone(), ex, wt, c, coef=1.0)
+    assert torch.equal(G.gcn_route_bwd(z, ex, wt, c, coef=1.0, dlogits=right), want)
+    Q, S = G.gcn_pack8(left)
+    assert torch.equal(G.gcn_unpack8(Q, S, Y=right), G.gcn_unpack8(Q, S, out_dtype=dt))
+    for f in (lambda: G.gcn_embed_fwd(left, ids, Y=both[1:n + 1, :F]), lambda: G.gcn_embed_fwd(left, ids, Y=both[:n, 1:F + 1]),
+              lambda: G.gcn_embed_bwd(left, off, order, dT=both[:n, F - 1:2 * F - 1]),
+              lambda: G.gcn_combine_fwd(left, slot, w, Y=both[n - 1:n - 1 + n // k, :F]),
+              lambda: G.gcn_combine_bwd(left, slot, w, dY, dZ=both[1:n + 1, :F]),
+              lambda: G.gcn_route_bwd(z, ex, wt, c, coef=1.0, dlogits=both[1:n + 1, :F])):
+        with pytest.raises(G.GcnError):
+            f()
+    torch.cuda.synchronize()

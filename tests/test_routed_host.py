@@ -63,6 +63,67 @@ def test_group_ids_refuses_arrays_over_each_other(L):
     assert want.value > 0
 
 
+X, Y, Z, W, V = (0x100000 * (i + 1) for i in range(5))
+
+
+def both_ways(f, d, out, at_in, out_bytes, in_bytes):
+    """Output `out` refused over the input at `at_in`, from either end (nothing is launched)."""
+    refused(f, d, [{out: at(at_in + in_bytes - 2)}, {out: at(at_in - out_bytes + 2)}, {out: at(at_in + 2)}])
+
+
+def test_matrices_over_each_other_are_refused(L):
+    n, F, V_ = 50, 40, 60
+    d = dict(n=n, F=F, V=V_, ids=at(X), per=1, T=at(Y), ldt=F + 3, dt=0, scale=1.0, Y=at(Z), ldy=F, dy=1, stream=None)
+    t = 4 * ((V_ - 1) * (F + 3) + F)
+    both_ways(L.gcn_embed_fwd, d, "Y", Y, 2 * n * F, t)
+    both_ways(L.gcn_embed_fwd, d, "Y", X, 2 * n * F, 4 * n)
+    # rows between the other's rows, of the same stride, that reach into the next one or begin in the last one
+    wide = {**d, "ldt": 2 * F, "ldy": 4 * F}
+    refused(L.gcn_embed_fwd, wide, [dict(Y=at(Y + 8 * F - 2)), dict(Y=at(Y + 4 * F - 2)), dict(Y=at(Y - 2 * F + 2))])
+    # of another stride, whose first rows lie between them
+    refused(L.gcn_embed_fwd, wide, [dict(Y=at(Y + 4 * F), ldy=4 * F + 2), dict(Y=at(Y + 4 * F), ldy=3 * F)])
+    d = dict(n=n, F=F, V=V_, offsets=at(X), order=at(W), dY=at(Y), lddy=F, dt=1, scale=1.0, dT=at(Z), lddt=F, dtt=0, flags=0,
+             work=None, size=None, stream=None)
+    for a, b in ((Y, 2 * n * F), (X, 8 * (V_ + 1)), (W, 4 * n)):
+        both_ways(L.gcn_embed_bwd, d, "dT", a, 4 * V_ * F, b)
+    E, k = 20, 3
+    d = dict(n=n, E=E, z=at(X), ldz=E, dt=0, k=k, flags=0, mask=at(X + 0x8000), coef=0.1, experts=at(Y), weights=at(Z),
+             counts=at(W), loss=at(V), work=None, size=None, stream=None)
+    size = dict(z=4 * n * E, mask=n, experts=4 * n * k, weights=4 * n * k, counts=8 * (E + 1), loss=4)
+    for out in ("experts", "weights", "counts", "loss"):
+        for other in size:
+            if other != out:
+                a = d[other].value
+                refused(L.gcn_route_fwd, d, [{out: at(a)}, {out: at(a + size[other] - 1)}, {out: at(a - size[out] + 1)}])
+    b = dict(n=n, E=E, z=at(X), ldz=E, dt=0, k=k, flags=0, experts=at(Y), weights=at(Z), counts=at(W), coef=0.1, dw=at(V),
+             dloss=None, dz=at(V + 0x8000), ldd=E, stream=None)
+    for a, m in ((X, 4 * n * E), (Y, 4 * n * k), (Z, 4 * n * k), (W, 8 * (E + 1)), (V, 4 * n * k)):
+        both_ways(L.gcn_route_bwd, b, "dz", a, 4 * n * E, m)
+    rows = 200
+    d = dict(n=n, k=k, F=F, Z=at(X), rows=rows, ldz=F, dt=1, slot=at(Y), w=at(Z), Y=at(W), ldy=F, stream=None)
+    for a, m in ((X, 2 * rows * F), (Y, 4 * n * k), (Z, 4 * n * k)):
+        both_ways(L.gcn_combine_fwd, d, "Y", a, 2 * n * F, m)
+    b = dict(n=n, k=k, F=F, Z=at(X), rows=rows, ldz=F, dt=1, slot=at(Y), w=at(Z), dY=at(W), lddy=F, dZ=at(V), lddz=F,
+             dw=at(V + 0x8000), stream=None)
+    for a, m in ((X, 2 * rows * F), (Y, 4 * n * k), (Z, 4 * n * k), (W, 2 * n * F), (V + 0x8000, 4 * n * k)):
+        both_ways(L.gcn_combine_bwd, b, "dZ", a, 2 * rows * F, m)
+    for a, m in ((X, 2 * rows * F), (Y, 4 * n * k), (W, 2 * n * F)):
+        both_ways(L.gcn_combine_bwd, b, "dw", a, 4 * n * k, m)
+    d = dict(n=n, F=F, X=at(X), ldx=F, dt=0, Q=at(Y), ldq=F, S=at(Z), lds=2, stream=None)
+    both_ways(L.gcn_pack8, d, "Q", X, n * F, 4 * n * F)
+    both_ways(L.gcn_pack8, d, "S", X, n * 2, 4 * n * F)
+    both_ways(L.gcn_pack8, d, "S", Y, n * 2, n * F)
+    refused(L.gcn_pack8, d, [dict(Q=at(X)), dict(S=at(Y)), dict(ldq=F + 2, lds=F + 2, S=at(Y + F + 1))])
+    u = dict(n=n, F=F, Q=at(Y), ldq=F, S=at(Z), lds=2, Y=at(X), ldy=F, dt=0, stream=None)
+    both_ways(L.gcn_unpack8, u, "Y", Y, 4 * n * F, n * F)
+    both_ways(L.gcn_unpack8, u, "Y", Z, 4 * n * F, n * 2)
+    G, N, K = 2, 8, 40
+    d = dict(G=G, off=at(X), rows=n, N=N, K=K, Q=at(Y), ldq=K, S=at(Z), lds=2, B=at(W), ldb=N, dt=0, C=at(V), ldc=N, sw=K * N,
+             work=None, size=None, stream=None)
+    for a, m in ((X, 8 * (G + 1)), (Y, n * K), (Z, n * 2), (W, 4 * n * N)):
+        both_ways(L.gcn_gemm_grouped_q8, d, "C", a, 4 * G * K * N, m)
+
+
 def test_embed_refusals(L):
     d = dict(n=4, F=8, V=5, ids=A, per=1, T=B, ldt=8, dt=0, scale=1.0, Y=C, ldy=8, dy=0, stream=None)
     refused(L.gcn_embed_fwd, d, [dict(n=-1), dict(F=0), dict(F=(1 << 30) + 1), dict(V=0), dict(V=-1), dict(ids=None),
