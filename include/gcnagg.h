@@ -493,8 +493,10 @@ enum { GCN_ACCUMULATE = 1u /* add to what dT holds */ };
  *   dT[v] = scale * sum over offsets[v] <= j < offsets[v + 1] of dY[order[j]]
  * with offsets [V + 1] and order [n] of gcn_group_ids(ids, V). Rows of ids that do not
  * occur become 0; with GCN_ACCUMULATE the sums are added to dT, whose other rows are not
- * touched. Sums in fp32 over at most 128 rows, those sums in double, one rounding to dT's
- * type; each in an order that n, offsets and order decide, so results repeat bit for bit.
+ * touched. Sums in fp32 over at most 32 rows (128 for n above 2^18), those sums in double, in an
+ * order that n, offsets and order decide, so results repeat bit for bit. The sum, its product
+ * with scale and, with GCN_ACCUMULATE, that plus dT's value are each rounded to fp32, the last of
+ * them to dT's type.
  *  dY [n x F] (lddy) of type dtype, dT [V x F] (lddt) of type dtype_t.
  *  Entries of `order` outside [0, n) are left out; offsets outside [0, n] are taken as 0 or n.
  *  Where they decrease no values are defined in dT, but nothing is read or written outside of
