@@ -117,6 +117,15 @@ def test_group_ids(E, n, groups, how):
         run(E, "check_group_ids", n, groups, how, memory=memory, seed=n + groups)
 
 
+# tiles of 16,384 ids in one, two and three passes; of 4096 and 1024 ids in three
+@pytest.mark.parametrize("how", ["spread", "skew", "one", "none"])
+@pytest.mark.parametrize("n,groups", [((1 << 20) + 1, 37), ((1 << 20) + 777, 2047), ((1 << 20) + 777, 5000),
+                                      ((1 << 20) + 777, (1 << 22) + 5), (5000003, 300), (3000001, 1 << 23),
+                                      (1 << 20, (1 << 22) + 5), (1 << 18, 1 << 24), (20000, (1 << 25) + 1)])
+def test_group_ids_of_many(E, n, groups, how):
+    run(E, "check_group_ids", n, groups, how, memory=1, seed=n + groups)
+
+
 @pytest.mark.parametrize("only", ["slot", "order"])
 def test_group_ids_one_output(E, only):
     for groups in (9, 3000):

@@ -65,6 +65,12 @@ def test_group_ids_many(model):
            ["check_group_ids", [(1 << 19) + 1, 3000, "skew"], dict(memory=1, seed=2)]])
 
 
+@pytest.mark.parametrize("groups,how", [(37, "none"), (5000, "skew")])
+def test_group_ids_in_the_largest_tiles(model, groups, how):
+    """Tiles of 16,384 ids: one pass, and two."""
+    model([["check_group_ids", [(1 << 20) + 777, groups, how], dict(memory=1, seed=groups)]])
+
+
 SHAPES = [(1, 1, 1), (3, 5, 2), (7, 8, 9), (40, 47, 11), (33, 100, 64), (5, 264, 3), (2, 2100, 4), (3, 2049, 2)]
 
 
