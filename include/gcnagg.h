@@ -523,6 +523,7 @@ enum { GCN_ROUTE_NORMALIZE = 1u /* a row's weights are divided by their sum */ }
  * are left, the rest of `experts` is -1 (no group to gcn_group_ids) with weight 0. A row
  * with mask[t] = 0, or of -inf alone, chooses none, and its p is 0. A row that holds a NaN,
  * or +inf, has NaN as p and weights, and the loss is NaN. Without any choice the loss is 0.
+ * Where e^(z - the row's largest logit) is below 2^-126 (87.3 below it), p is 0, in the gradient too.
  *  logits [n x E] (ldz) of type dtype (GCN_DT_F32 or GCN_DT_BF16); 1 <= E <= 1024,
  *  1 <= k <= min(E, 64), n k < 2^31. mask uint8 [n] or NULL. experts int32 [n k], weights fp32
  *  [n k], counts int64 [E + 1], loss fp32 or NULL (device). fp32; sums over rows in an order
