@@ -162,12 +162,15 @@ __global__ __launch_bounds__(kThreads) void k_zero(char* p, int64_t bytes) {
 // A workgroup has up to kRows rows, or a part of a long one, in pieces of 16 bytes of dT. Rows without
 // a place, most of a large table's, are zeros, which bound the pass; those that have some are listed, so
 // that all lanes gather (2,449,029 x 100 fp32, 250,000 places: 318 us where each piece looked for its
-// row's places, 245 with the zeros of a workgroup's rows written first; 282 with zeros past the caches).
+// row's places, 245 with the zeros of a workgroup's rows written first; 282 with zeros past the caches; all these without the
+// sort).
 // A table with a place for fewer than every 32nd row, whose rows lie beside each other, is zeroed by a
 // launch before, which knows nothing of rows and writes at 6.8 TB/s (25,000 places: 244 and 204 us;
 // 250,000 places at 128 columns: 274 and 305, so not there). Rows that are no whole pieces cost the pass
 // more, which then is for every 8th (245,000 places at 47 columns: 217 and 149, at 101: 300 and 284;
-// 490,000 at 101: 338 and 348).
+// 490,000 at 101: 338 and 348; 408,000 at 47, in the pass by this rule: 239 and 173). bf16 outputs go by it too, a place for
+// every 6th, 24th and 48th row in the pass and zeroed before: 47 columns 178 and 116, 117 and 60, 114 and 54; 48 columns 97
+// and 93, 61 and 59, 45 and 52; 128 columns 178 and 212, 139 and 147, 130 and 137.
 constexpr int kRows = 1024;
 
 template <class T, class TT, int kRowTile>

@@ -3,9 +3,9 @@
 // The codes' values are exact in bf16, so they are decoded on their way to LDS, and the product is that
 // of bf16 rows (gemm_grouped.hip), or of one bf16 operand with the three parts of an fp32 one
 // (gemm_split.hip). Decoding takes 2.5 instructions an element of X for every 256 columns of B;
-// between the products it costs little. bf16, 32,768 rows of 16 ragged groups, 2048 x 4096: 595 to 615 us,
-// 41% of the cycles in the matrix cores; in one group 902 TFLOP/s. fp32, 500,000 rows of
-// 4 groups, 100 x 256: 143 us, bound by its bytes (4.2 TB/s).
+// between the products it costs little. bf16, 32,768 rows of 16 ragged groups, 2048 x 4096: 595 to 637 us,
+// 41% of the cycles in the matrix cores; in one group 918 TFLOP/s. fp32, 500,000 rows of
+// 4 groups, 100 x 256: 143 to 150 us, bound by its bytes (3.9 to 4.2 TB/s).
 
 #include <algorithm>
 #include <cmath>
@@ -779,6 +779,10 @@ gcn_status mul8(Q8Args a, int dtype, Scratch* scratch, hipStream_t s) {
   const bool direct = dtype == GCN_DT_BF16 && reinterpret_cast<uintptr_t>(a.b) % 16 == 0 &&
                       a.ldb % 8 == 0 && N % 8 == 0;
   const bool f32 = dtype == GCN_DT_F32;
+  // tiles of 256 x 256 from 192 rows of a group on: 170 groups of 192, 1024 x 1024: 182 us, 227 in tiles of
+  // 128; 208 of 192, 256 x 256: 24 and 28. (Large matrices gain from fewer rows on, 341 groups of 96, 1024 x 1024: 317 and
+  // 419, small ones do not, 312 of 128, 256 x 256: 37 and 35; and where few groups have few tiles, tiles of 128
+  // fill more units: four of 2048, 2048 x 1024: 88 and 50.)
   const bool wide = N > 128 && K > 128 && rows / a.by.n >= 192 && direct;
   const int64_t tm = wide ? 256 : f32 && K <= 64 ? 64 : 128;
   const int64_t tn = wide ? 256 : !f32 ? 128 : N <= 64 ? 64 : tm == 64 ? 128 : (N - 1) % 256 < 128 ? 128 : 256;
